@@ -280,6 +280,103 @@ int fibq_attn_decode_noalloc(const void* q, int q_dtype, const uint8_t* k_payloa
                              int64_t T_stride, int d, int k, double b, int N, const float* R,
                              const float* C, float scale, float* out, void* stream);
 
+/* --------------------------------------------------------------- serving --
+ * Operators of a serving loop on the compressed cache, for groups of different
+ * lengths: a group g (layer, sequence, kv-head) holds lens[g] cached tokens
+ * (device, int32) in rows 0 .. lens[g] - 1 of its T_stride rows.  Lengths live
+ * on the device, so a captured call follows them.  Common limits (else
+ * FIBQ_EINVAL): 0 <= n_groups <= 65535, T_stride < 2^30.  Layouts, dtypes and
+ * the scale are those of fibq_attn_decode.  Rows behind a group's last token
+ * may hold anything. */
+
+/* Ancestor masks of a tree of M drafted tokens, host memory.  parents[i] is
+ * the drafted token that token i follows, or -1 for one that follows the last
+ * cached token; -1 <= parents[i] < i (parents come first), 1 <= M <= 64, else
+ * FIBQ_EINVAL.  masks_out[i] gets bit i and the bits of i's ancestors. */
+int fibq_tree_masks(const int32_t* parents, int M, uint64_t* masks_out);
+
+/* Workspace bytes of fibq_attn_tree (0 for an invalid problem). */
+size_t fibq_attn_tree_workspace_bytes(int64_t n_groups, int M, int G, int d, int k, int N);
+
+/* Attention of a tree of drafted tokens over the compressed cache (the
+ * verification step of speculative decoding; Eq. lattn with a mask, over the
+ * decoded cache).  The M drafted tokens' keys and values have been encoded
+ * into rows lens[g] .. lens[g] + M - 1 of their group, so an accepted token
+ * has seen exactly the rows that decoding it by itself would have read:
+ *   o_{g,i,h} = sum_{t in A} softmax_{t in A}(scale <q_{g,i,h}, K_hat_{g,t}>) V_hat_{g,t},
+ *   A = {t < lens[g]} and {lens[g] + j : bit j of the mask of (g, i)}.
+ * q: device [n_groups][M][G][d] of q_dtype; out: device, the same shape, float.
+ * masks: device uint64 (bits from M on are ignored); the mask of (g, i) is
+ * masks[g * mask_stride + i], mask_stride 0 (one tree for all groups) or >= M.
+ * A row that sees no token gives zeros.  The rows of a group whose length is
+ * outside [0, T_stride - M] are NaN, and nothing of its cache is read.
+ * 1 <= M <= 64, 1 <= G <= 16.  M = 1 with mask 1 is single-query attention
+ * over lens[g] + 1 tokens.  workspace: device, at least
+ * fibq_attn_tree_workspace_bytes(...) bytes, 256-byte aligned, else
+ * FIBQ_EWORKSPACE; calls that overlap in time need one each. */
+int fibq_attn_tree(const void* q, int q_dtype, const uint8_t* k_payload,
+                   const uint16_t* k_norms, const uint8_t* v_payload, const uint16_t* v_norms,
+                   const int32_t* lens, const uint64_t* masks, int64_t mask_stride,
+                   int64_t n_groups, int M, int G, int64_t T_stride, int d, int k, double b, int N,
+                   const float* R, const float* C, float scale, float* out, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/* Acceptance of a drafted path, in place: row lens[g] + i of K and V (payload
+ * and norm) becomes row lens[g] + path[g * path_len + i] for i < n_acc[g] (all
+ * are read before any is written), and new_lens[g] = lens[g] + n_acc[g].
+ * new_lens may be lens.  P: payload bytes of a row (fibq_payload_bytes),
+ * 1 <= P <= 256; 1 <= M <= 64 drafted tokens, 1 <= path_len <= 64.  A group
+ * with a length outside [0, T_stride - M], a count outside
+ * [0, min(path_len, M)] or a path entry (of the first n_acc[g]) outside [0, M)
+ * keeps its rows and gets new_lens[g] = -1, which every operator of this
+ * section treats as a bad length. */
+int fibq_accept_draft(uint8_t* k_payload, uint16_t* k_norms, uint8_t* v_payload,
+                      uint16_t* v_norms, const int32_t* lens, int64_t n_groups, int64_t T_stride,
+                      int P, int M, const int32_t* path, int path_len, const int32_t* n_acc,
+                      int32_t* new_lens, void* stream);
+
+/* Workspace bytes of fibq_attn_decode_accum (0 for an invalid problem). */
+size_t fibq_attn_decode_accum_workspace_bytes(int64_t n_groups, int G, int d, int k, int N);
+
+/* fibq_attn_decode over groups of different lengths that also accumulates
+ * every token's attention weight:
+ *   out as fibq_attn_decode with T = lens[g];
+ *   acc[g * T_stride + t] += sum_h softmax_t(scale <q_{g,h}, K_hat_{g,t}>), t < lens[g].
+ * acc: device float [n_groups][T_stride], in place; elements from lens[g] on
+ * are left as they are.  Each token's sum is taken in a fixed order (no
+ * atomics).  lens[g] = 0 gives zeros; a length outside [0, T_stride] gives NaN
+ * rows and leaves the group's acc.  workspace as in fibq_attn_tree. */
+int fibq_attn_decode_accum(const void* q, int q_dtype, const uint8_t* k_payload,
+                           const uint16_t* k_norms, const uint8_t* v_payload,
+                           const uint16_t* v_norms, const int32_t* lens, float* acc,
+                           int64_t n_groups, int G, int64_t T_stride, int d, int k, double b,
+                           int N, const float* R, const float* C, float scale, float* out,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of fibq_evict (0 if it needs none). */
+size_t fibq_evict_workspace_bytes(int64_t n_groups, int64_t T_stride);
+
+/* Eviction by accumulated attention weight, into another cache.  A group of
+ * lens[g] <= keep tokens keeps them all; a longer one keeps its last `recent`
+ * tokens and, of the others, the keep - recent with the largest acc (equal
+ * ones: lowest index first; NaN ranks below everything).  Kept tokens stay in
+ * order: row i of the new cache is row index[g * keep + i] of the old one.
+ * Payloads [n_groups][T_stride][P], norms and acc [n_groups][T_stride] are
+ * copied to the *_out arrays of T_out >= keep rows per group; new_lens[g] is
+ * the number kept, index (device int32 [n_groups][keep]) is -1 behind it, and
+ * rows of the new cache behind it are left as they are.  A length outside
+ * [0, T_stride] gives new_lens[g] = -1, an index of -1 and no rows.
+ * 1 <= keep < 2^30, 0 <= recent <= keep, 1 <= P <= 256.  No output may overlap
+ * an input (FIBQ_EINVAL for the same address).  workspace: device, at least
+ * fibq_evict_workspace_bytes(...) bytes, 256-byte aligned, else
+ * FIBQ_EWORKSPACE. */
+int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t* v_payload,
+               const uint16_t* v_norms, const float* acc, const int32_t* lens, int64_t n_groups,
+               int64_t T_stride, int P, int64_t keep, int64_t recent, int64_t T_out,
+               uint8_t* k_payload_out, uint16_t* k_norms_out, uint8_t* v_payload_out,
+               uint16_t* v_norms_out, float* acc_out, int32_t* new_lens, int32_t* index,
+               void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

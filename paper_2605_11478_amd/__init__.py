@@ -78,6 +78,22 @@ def lib():
             "fibq_attn_decode_noalloc": (c_i, [c_p, c_i, c_p, c_p, c_p, c_p, c_i64, c_i, c_i64,
                                                c_i64, c_i, c_i, c_d, c_i, c_p, c_p, c_f, c_p,
                                                c_p]),
+            "fibq_tree_masks": (c_i, [c_p, c_i, c_p]),
+            "fibq_attn_tree_workspace_bytes": (ctypes.c_size_t, [c_i64, c_i, c_i, c_i, c_i, c_i]),
+            "fibq_attn_tree": (c_i, [c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_p, c_i64, c_i64, c_i,
+                                     c_i, c_i64, c_i, c_i, c_d, c_i, c_p, c_p, c_f, c_p, c_p,
+                                     ctypes.c_size_t, c_p]),
+            "fibq_accept_draft": (c_i, [c_p, c_p, c_p, c_p, c_p, c_i64, c_i64, c_i, c_i, c_p, c_i,
+                                        c_p, c_p, c_p]),
+            "fibq_attn_decode_accum_workspace_bytes": (ctypes.c_size_t, [c_i64, c_i, c_i, c_i,
+                                                                         c_i]),
+            "fibq_attn_decode_accum": (c_i, [c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_p, c_i64, c_i,
+                                             c_i64, c_i, c_i, c_d, c_i, c_p, c_p, c_f, c_p, c_p,
+                                             ctypes.c_size_t, c_p]),
+            "fibq_evict_workspace_bytes": (ctypes.c_size_t, [c_i64, c_i64]),
+            "fibq_evict": (c_i, [c_p, c_p, c_p, c_p, c_p, c_p, c_i64, c_i64, c_i, c_i64, c_i64,
+                                 c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p, ctypes.c_size_t,
+                                 c_p]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -468,4 +484,209 @@ def attn_decode_noalloc(q, k_payload, k_norms, v_payload, v_norms, T, k, N, R, C
                                         _dev(R, "R"), _dev(C, "C"), scale, _dev(out, "out"),
                                         _stream())
     _check(st, "fibq_attn_decode_noalloc")
+    return out
+
+
+# -------------------------------------------------------------- serving ----
+# Operators of a serving loop: groups of different lengths (``lens``, int32
+# [n_groups] on the device) over one compressed cache.
+def tree_masks(parents):
+    """Ancestor masks (int64 [M], host) of a tree of M <= 64 drafted tokens:
+    ``parents[i]`` < i is the drafted token that token i follows, -1 the last
+    cached one."""
+    p = np.ascontiguousarray(parents, dtype=np.int32)
+    if p.ndim != 1:
+        raise ValueError("parents must be one-dimensional")
+    masks = np.empty(p.shape[0], dtype=np.int64)
+    _check(lib().fibq_tree_masks(p.ctypes.data, p.shape[0], masks.ctypes.data),
+           "fibq_tree_masks")
+    return masks
+
+
+def attn_tree_workspace_bytes(n_groups, M, G, d, k, N):
+    return lib().fibq_attn_tree_workspace_bytes(n_groups, M, G, d, k, N)
+
+
+def attn_decode_accum_workspace_bytes(n_groups, G, d, k, N):
+    return lib().fibq_attn_decode_accum_workspace_bytes(n_groups, G, d, k, N)
+
+
+def evict_workspace_bytes(n_groups, T_stride):
+    return lib().fibq_evict_workspace_bytes(n_groups, T_stride)
+
+
+def _here(t, **tensors):
+    """All tensors on t's device, and that the current one (whose stream the call goes to)."""
+    _same_device(**tensors)
+    if t.device.index != _torch().cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, which is not the current device")
+
+
+def _check_cache(k_payload, k_norms, v_payload, v_norms, lens, P=None):
+    """One cache of groups and its lengths; returns (n_groups, T_stride, P)."""
+    torch = _torch()
+    _want(k_payload, "k_payload", (torch.uint8,), (None, None, P))
+    n_groups, T_stride, P = k_payload.shape
+    _want(v_payload, "v_payload", (torch.uint8,), (n_groups, T_stride, P))
+    _want(k_norms, "k_norms", _norm_dtypes(), (n_groups, T_stride))
+    _want(v_norms, "v_norms", _norm_dtypes(), (n_groups, T_stride))
+    _want(lens, "lens", (torch.int32,), (n_groups,))
+    return n_groups, T_stride, P
+
+
+def _workspace(workspace, need, device):
+    torch = _torch()
+    if workspace is None:
+        workspace = torch.empty((max(need, 1),), dtype=torch.uint8, device=device)
+    _want(workspace, "workspace", (torch.uint8,), (None,))
+    if workspace.numel() < need:
+        raise ValueError(f"workspace holds {workspace.numel()} bytes, {need} needed")
+    return workspace
+
+
+def attn_tree(q, k_payload, k_norms, v_payload, v_norms, lens, masks, k, N, R, C, scale=0.0,
+              workspace=None, out=None):
+    """Attention of drafted token trees over the compressed cache.
+
+    q [n_groups, M, G, d]; the M drafted tokens' rows are cache rows
+    lens[g] .. lens[g] + M - 1; masks int64 [M] or [n_groups, M]: bit j of row i
+    lets drafted token i see drafted token j (``tree_masks``).
+    -> out float32 [n_groups, M, G, d]; rows of a group whose length is outside
+    [0, T_stride - M] are NaN.  ``workspace`` as for ``attn_decode``
+    (``attn_tree_workspace_bytes``).
+    """
+    torch = _torch()
+    _want(q, "q", (torch.float32, torch.float16, torch.bfloat16), (None, None, None, None))
+    n_groups, M, G, d = q.shape
+    _, T_stride, _ = _check_cache(k_payload, k_norms, v_payload, v_norms, lens,
+                                  payload_bytes(d, k, N))
+    _want(lens, "lens", (torch.int32,), (n_groups,))
+    _want(masks, "masks", (torch.int64,), contiguous=False)
+    _want(masks, "masks", (torch.int64,), (M,) if masks.dim() == 1 else (n_groups, M))
+    _check_rc(R, C, d, k, N)
+    if out is None:
+        out = torch.empty((n_groups, M, G, d), dtype=torch.float32, device=q.device)
+    _want(out, "out", (torch.float32,), (n_groups, M, G, d))
+    workspace = _workspace(workspace, attn_tree_workspace_bytes(n_groups, M, G, d, k, N),
+                           q.device)
+    _here(q, q=q, k_payload=k_payload, k_norms=k_norms, v_payload=v_payload, v_norms=v_norms,
+          lens=lens, masks=masks, R=R, C=C, out=out, workspace=workspace)
+    st = lib().fibq_attn_tree(q.data_ptr(), _dtype_code(q), k_payload.data_ptr(),
+                              k_norms.data_ptr(), v_payload.data_ptr(), v_norms.data_ptr(),
+                              lens.data_ptr(), masks.data_ptr(), 0 if masks.dim() == 1 else M,
+                              n_groups, M, G, T_stride, d, k, rate(k, N), N, R.data_ptr(),
+                              C.data_ptr(), scale, out.data_ptr(), workspace.data_ptr(),
+                              workspace.numel(), _stream())
+    _check(st, "fibq_attn_tree")
+    return out
+
+
+def accept_draft(k_payload, k_norms, v_payload, v_norms, lens, M, path, n_acc, new_lens=None):
+    """Moves the accepted path of M drafted tokens to the end of each group's
+    context, in place: row lens[g] + i <- row lens[g] + path[g, i] for
+    i < n_acc[g].  path int32 [n_groups, A], n_acc int32 [n_groups].
+    -> new_lens = lens + n_acc (pass ``new_lens=lens`` to update it in place);
+    -1 for a group with a bad length, count or path, whose rows stay.
+    """
+    torch = _torch()
+    n_groups, T_stride, P = _check_cache(k_payload, k_norms, v_payload, v_norms, lens)
+    _want(path, "path", (torch.int32,), (n_groups, None))
+    _want(n_acc, "n_acc", (torch.int32,), (n_groups,))
+    if new_lens is None:
+        new_lens = torch.empty_like(lens)
+    _want(new_lens, "new_lens", (torch.int32,), (n_groups,))
+    _here(lens, k_payload=k_payload, k_norms=k_norms, v_payload=v_payload, v_norms=v_norms,
+          lens=lens, path=path, n_acc=n_acc, new_lens=new_lens)
+    st = lib().fibq_accept_draft(k_payload.data_ptr(), k_norms.data_ptr(), v_payload.data_ptr(),
+                                 v_norms.data_ptr(), lens.data_ptr(), n_groups, T_stride, P, M,
+                                 path.data_ptr(), path.shape[1], n_acc.data_ptr(),
+                                 new_lens.data_ptr(), _stream())
+    _check(st, "fibq_accept_draft")
+    return new_lens
+
+
+def attn_decode_accum(q, k_payload, k_norms, v_payload, v_norms, lens, acc, k, N, R, C, scale=0.0,
+                      workspace=None, out=None):
+    """``attn_decode`` over groups of different lengths that adds every cached
+    token's attention weight, summed over the group's heads, to ``acc``
+    (float32 [n_groups, T_stride], in place; elements from lens[g] on stay).
+
+    q [n_groups, G, d] -> out float32 [n_groups, G, d]; a length outside
+    [0, T_stride] gives NaN rows and leaves the group's acc.
+    """
+    torch = _torch()
+    _want(q, "q", (torch.float32, torch.float16, torch.bfloat16), (None, None, None))
+    n_groups, G, d = q.shape
+    _, T_stride, _ = _check_cache(k_payload, k_norms, v_payload, v_norms, lens,
+                                  payload_bytes(d, k, N))
+    _want(lens, "lens", (torch.int32,), (n_groups,))
+    _want(acc, "acc", (torch.float32,), (n_groups, T_stride))
+    _check_rc(R, C, d, k, N)
+    if out is None:
+        out = torch.empty((n_groups, G, d), dtype=torch.float32, device=q.device)
+    _want(out, "out", (torch.float32,), (n_groups, G, d))
+    workspace = _workspace(workspace, attn_decode_accum_workspace_bytes(n_groups, G, d, k, N),
+                           q.device)
+    _here(q, q=q, k_payload=k_payload, k_norms=k_norms, v_payload=v_payload, v_norms=v_norms,
+          lens=lens, acc=acc, R=R, C=C, out=out, workspace=workspace)
+    st = lib().fibq_attn_decode_accum(q.data_ptr(), _dtype_code(q), k_payload.data_ptr(),
+                                      k_norms.data_ptr(), v_payload.data_ptr(),
+                                      v_norms.data_ptr(), lens.data_ptr(), acc.data_ptr(),
+                                      n_groups, G, T_stride, d, k, rate(k, N), N, R.data_ptr(),
+                                      C.data_ptr(), scale, out.data_ptr(), workspace.data_ptr(),
+                                      workspace.numel(), _stream())
+    _check(st, "fibq_attn_decode_accum")
+    return out
+
+
+def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=None,
+          workspace=None):
+    """Eviction by accumulated attention weight, into another cache.
+
+    A group of at most ``keep`` tokens keeps them all; a longer one its last
+    ``recent`` and, of the others, the keep - recent with the largest ``acc``
+    (float32 [n_groups, T_stride]; ties: lowest index; NaN last), in order.
+    -> (k_payload, k_norms, v_payload, v_norms, acc, lens, index): the new cache
+    of T_out rows per group (keep, or what ``out`` has), its lengths and the old
+    index of every row (int32 [n_groups, keep], -1 behind the last).  Rows
+    behind the new length are not written.  ``out``: seven such tensors, none
+    sharing memory with an input.
+    """
+    torch = _torch()
+    n_groups, T_stride, P = _check_cache(k_payload, k_norms, v_payload, v_norms, lens)
+    _want(acc, "acc", (torch.float32,), (n_groups, T_stride))
+    if out is None:
+        if not 1 <= keep < 1 << 30:
+            raise ValueError(f"keep = {keep} must lie in [1, 2^30)")
+        dev = lens.device
+        new = [torch.empty((n_groups, keep, P), dtype=torch.uint8, device=dev) for _ in range(2)]
+        nrm = [torch.empty((n_groups, keep), dtype=t.dtype, device=dev) for t in (k_norms, v_norms)]
+        out = (new[0], nrm[0], new[1], nrm[1],
+               torch.empty((n_groups, keep), dtype=torch.float32, device=dev),
+               torch.empty_like(lens), torch.empty((n_groups, keep), dtype=torch.int32, device=dev))
+    out = tuple(out)
+    if len(out) != 7:
+        raise ValueError("out must hold seven tensors")
+    kpo, kno, vpo, vno, acco, lenso, index = out
+    _, T_out, _ = _check_cache(kpo, kno, vpo, vno, lenso, P)
+    _want(kpo, "out k_payload", (torch.uint8,), (n_groups, T_out, P))
+    _want(acco, "out acc", (torch.float32,), (n_groups, T_out))
+    _want(index, "index", (torch.int32,), (n_groups, keep))
+    workspace = _workspace(workspace, evict_workspace_bytes(n_groups, T_stride), lens.device)
+    ins = dict(k_payload=k_payload, k_norms=k_norms, v_payload=v_payload, v_norms=v_norms,
+               acc=acc, lens=lens)
+    outs = dict(k_payload_out=kpo, k_norms_out=kno, v_payload_out=vpo, v_norms_out=vno,
+                acc_out=acco, new_lens=lenso, index=index)
+    _here(lens, workspace=workspace, **ins, **outs)
+    for x, a in ins.items():
+        for y, b in outs.items():
+            if (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size()
+                    and b.data_ptr() < a.data_ptr() + a.numel() * a.element_size()):
+                raise ValueError(f"{y} overlaps {x}")
+    st = lib().fibq_evict(k_payload.data_ptr(), k_norms.data_ptr(), v_payload.data_ptr(),
+                          v_norms.data_ptr(), acc.data_ptr(), lens.data_ptr(), n_groups, T_stride,
+                          P, keep, recent, T_out, kpo.data_ptr(), kno.data_ptr(), vpo.data_ptr(),
+                          vno.data_ptr(), acco.data_ptr(), lenso.data_ptr(), index.data_ptr(),
+                          workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "fibq_evict")
     return out

@@ -19,7 +19,8 @@ BINDING = os.path.join(PKG, "_binding.so")
 BUILD = os.path.join(PKG, "_build")
 
 HOST_SRC = ["api.cpp", "host_builder.cpp"]
-HIP_SRC = ["codec_kernels.hip", "encode_mfma.hip", "encode_mf4.hip", "encode_gen.hip", "attn_kernels.hip", "attn_w4.hip", "attn_k4.hip", "attn_noalloc.hip"]
+HIP_SRC = ["codec_kernels.hip", "encode_mfma.hip", "encode_mf4.hip", "encode_gen.hip", "attn_kernels.hip", "attn_w4.hip", "attn_k4.hip", "attn_noalloc.hip",
+           "serve_attn.hip", "serve_cache.hip"]
 
 HIP_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

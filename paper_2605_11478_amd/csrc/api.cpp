@@ -339,4 +339,150 @@ int fibq_attn_decode_noalloc(const void* q, int q_dtype, const uint8_t* k_payloa
                                            FIBQ_ATTN_SCRATCH_BYTES, stream));
 }
 
+// --------------------------------------------------------------- serving ----
+static bool serve_sizes(int64_t n_groups, int64_t T_stride) {
+  return n_groups >= 0 && n_groups <= 65535 && T_stride >= 0 && T_stride < (1LL << 30);
+}
+
+// The workspace holds float records: 256-byte aligned, as every allocator of
+// device memory gives it.
+static int check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return FIBQ_OK;
+  if (!ws || bytes < need || reinterpret_cast<uintptr_t>(ws) % 256 != 0) return FIBQ_EWORKSPACE;
+  return FIBQ_OK;
+}
+
+int fibq_tree_masks(const int32_t* parents, int M, uint64_t* masks_out) {
+  if (!parents || !masks_out || M < 1 || M > 64) return FIBQ_EINVAL;
+  for (int i = 0; i < M; ++i)
+    if (parents[i] < -1 || parents[i] >= i) return FIBQ_EINVAL;
+  for (int i = 0; i < M; ++i)
+    masks_out[i] = (1ull << i) | (parents[i] >= 0 ? masks_out[parents[i]] : 0);
+  return FIBQ_OK;
+}
+
+size_t fibq_attn_tree_workspace_bytes(int64_t n_groups, int M, int G, int d, int k, int N) {
+  Shape s;
+  if (check_shape(d, k, N, &s) != FIBQ_OK || check_supported(s) != FIBQ_OK) return 0;
+  if (!serve_sizes(n_groups, 0) || M < 1 || M > 64 || G < 1 || G > 16) return 0;
+  return fibq::dev::serve_attn_workspace_bytes(n_groups, M, G, s);
+}
+
+size_t fibq_attn_decode_accum_workspace_bytes(int64_t n_groups, int G, int d, int k, int N) {
+  Shape s;
+  if (check_shape(d, k, N, &s) != FIBQ_OK || check_supported(s) != FIBQ_OK) return 0;
+  if (!serve_sizes(n_groups, 0) || G < 1 || G > 16) return 0;
+  return fibq::dev::serve_attn_workspace_bytes(n_groups, 0, G, s);
+}
+
+// What both attention forms check; a.s is set.
+static int serve_attn_check(fibq::dev::ServeAttn* a, int d, int k, double b, int N, bool* done) {
+  *done = false;
+  int rc = check_shape(d, k, N, &a->s);
+  if (rc != FIBQ_OK) return rc;
+  if ((rc = check_rate(b, a->s)) != FIBQ_OK) return rc;
+  if (a->q_dtype != FIBQ_F32 && a->q_dtype != FIBQ_F16 && a->q_dtype != FIBQ_BF16)
+    return FIBQ_EINVAL;
+  if (!serve_sizes(a->n_groups, a->T_stride) || a->G < 1 || a->G > 16 || !std::isfinite(a->scale))
+    return FIBQ_EINVAL;
+  if ((rc = check_supported(a->s)) != FIBQ_OK) return rc;
+  if (a->n_groups == 0) {
+    *done = true;
+    return FIBQ_OK;
+  }
+  if (!a->q || !a->R || !a->C || !a->out || !a->lens) return FIBQ_EINVAL;
+  if (a->T_stride > 0 && (!a->kp || !a->kn || !a->vp || !a->vn)) return FIBQ_EINVAL;
+  if (a->scale <= 0.0f) a->scale = 1.0f / std::sqrt((float)d);
+  return FIBQ_OK;
+}
+
+int fibq_attn_tree(const void* q, int q_dtype, const uint8_t* k_payload,
+                   const uint16_t* k_norms, const uint8_t* v_payload, const uint16_t* v_norms,
+                   const int32_t* lens, const uint64_t* masks, int64_t mask_stride,
+                   int64_t n_groups, int M, int G, int64_t T_stride, int d, int k, double b, int N,
+                   const float* R, const float* C, float scale, float* out, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+  if (M < 1 || M > 64 || (mask_stride != 0 && mask_stride < M)) return FIBQ_EINVAL;
+  fibq::dev::ServeAttn a{q, q_dtype, k_payload, k_norms, v_payload, v_norms, lens, masks,
+                         mask_stride, nullptr, n_groups, M, G, T_stride, Shape{}, R, C, scale,
+                         out, workspace};
+  bool done = false;
+  int rc = serve_attn_check(&a, d, k, b, N, &done);
+  if (rc != FIBQ_OK || done) return rc;
+  if (!masks) return FIBQ_EINVAL;
+  rc = check_workspace(workspace, workspace_bytes,
+                       fibq::dev::serve_attn_workspace_bytes(n_groups, M, G, a.s));
+  if (rc != FIBQ_OK) return rc;
+  return hip_status(fibq::dev::launch_serve_attn(a, stream));
+}
+
+int fibq_attn_decode_accum(const void* q, int q_dtype, const uint8_t* k_payload,
+                           const uint16_t* k_norms, const uint8_t* v_payload,
+                           const uint16_t* v_norms, const int32_t* lens, float* acc,
+                           int64_t n_groups, int G, int64_t T_stride, int d, int k, double b,
+                           int N, const float* R, const float* C, float scale, float* out,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  fibq::dev::ServeAttn a{q, q_dtype, k_payload, k_norms, v_payload, v_norms, lens, nullptr,
+                         0, acc, n_groups, 0, G, T_stride, Shape{}, R, C, scale, out, workspace};
+  bool done = false;
+  int rc = serve_attn_check(&a, d, k, b, N, &done);
+  if (rc != FIBQ_OK || done) return rc;
+  if (T_stride > 0 && !acc) return FIBQ_EINVAL;
+  rc = check_workspace(workspace, workspace_bytes,
+                       fibq::dev::serve_attn_workspace_bytes(n_groups, 0, G, a.s));
+  if (rc != FIBQ_OK) return rc;
+  return hip_status(fibq::dev::launch_serve_attn(a, stream));
+}
+
+int fibq_accept_draft(uint8_t* k_payload, uint16_t* k_norms, uint8_t* v_payload,
+                      uint16_t* v_norms, const int32_t* lens, int64_t n_groups, int64_t T_stride,
+                      int P, int M, const int32_t* path, int path_len, const int32_t* n_acc,
+                      int32_t* new_lens, void* stream) {
+  if (!serve_sizes(n_groups, T_stride) || P < 1 || P > 256 || M < 1 || M > 64 || path_len < 1 ||
+      path_len > 64)
+    return FIBQ_EINVAL;
+  if (n_groups == 0) return FIBQ_OK;
+  if (!lens || !path || !n_acc || !new_lens) return FIBQ_EINVAL;
+  if (T_stride > 0 && (!k_payload || !k_norms || !v_payload || !v_norms)) return FIBQ_EINVAL;
+  return hip_status(fibq::dev::launch_accept(k_payload, k_norms, v_payload, v_norms, lens,
+                                             n_groups, T_stride, P, M, path, path_len, n_acc,
+                                             new_lens, stream));
+}
+
+size_t fibq_evict_workspace_bytes(int64_t n_groups, int64_t T_stride) {
+  if (!serve_sizes(n_groups, T_stride)) return 0;
+  return fibq::dev::evict_workspace_bytes(n_groups, T_stride);
+}
+
+int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t* v_payload,
+               const uint16_t* v_norms, const float* acc, const int32_t* lens, int64_t n_groups,
+               int64_t T_stride, int P, int64_t keep, int64_t recent, int64_t T_out,
+               uint8_t* k_payload_out, uint16_t* k_norms_out, uint8_t* v_payload_out,
+               uint16_t* v_norms_out, float* acc_out, int32_t* new_lens, int32_t* index,
+               void* workspace, size_t workspace_bytes, void* stream) {
+  if (!serve_sizes(n_groups, T_stride) || P < 1 || P > 256 || keep < 1 || keep >= (1LL << 30) ||
+      recent < 0 || recent > keep || T_out < keep || T_out >= (1LL << 30))
+    return FIBQ_EINVAL;
+  if (n_groups == 0) return FIBQ_OK;
+  if (!lens || !k_payload_out || !k_norms_out || !v_payload_out || !v_norms_out || !acc_out ||
+      !new_lens || !index)
+    return FIBQ_EINVAL;
+  if (T_stride > 0 && (!k_payload || !k_norms || !v_payload || !v_norms || !acc))
+    return FIBQ_EINVAL;
+  const void* in[] = {k_payload, k_norms, v_payload, v_norms, acc, lens};
+  const void* o[] = {k_payload_out, k_norms_out, v_payload_out, v_norms_out, acc_out, new_lens,
+                     index};
+  for (const void* x : in)
+    for (const void* y : o)
+      if (x == y) return FIBQ_EINVAL;
+  const int rc = check_workspace(workspace, workspace_bytes,
+                                 fibq::dev::evict_workspace_bytes(n_groups, T_stride));
+  if (rc != FIBQ_OK) return rc;
+  return hip_status(fibq::dev::launch_evict(k_payload, k_norms, v_payload, v_norms, acc, lens,
+                                            n_groups, T_stride, P, (int)keep, (int)recent, T_out,
+                                            k_payload_out, k_norms_out, v_payload_out,
+                                            v_norms_out, acc_out, new_lens, index, workspace,
+                                            stream));
+}
+
 }  // extern "C"

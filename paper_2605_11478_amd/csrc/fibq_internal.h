@@ -84,6 +84,41 @@ int launch_attn(const void* q, int q_dtype, const uint8_t* kp, const uint16_t* k
                 const uint8_t* vp, const uint16_t* vn, int64_t n_groups, int G, int64_t T,
                 int64_t T_stride, Shape s, const float* R, const float* C, float scale,
                 float* out, void* ws, size_t ws_bytes, void* stream);
+
+// One call of fibq_attn_tree (M > 0, masks set) or fibq_attn_decode_accum
+// (M = 0, acc set).
+struct ServeAttn {
+  const void* q;
+  int q_dtype;
+  const uint8_t* kp;
+  const uint16_t* kn;
+  const uint8_t* vp;
+  const uint16_t* vn;
+  const int32_t* lens;
+  const uint64_t* masks;
+  int64_t mask_stride;
+  float* acc;
+  int64_t n_groups;
+  int M, G;
+  int64_t T_stride;
+  Shape s;
+  const float* R;
+  const float* C;
+  float scale;
+  float* out;
+  void* ws;
+};
+size_t serve_attn_workspace_bytes(int64_t n_groups, int M, int G, const Shape& s);
+int launch_serve_attn(const ServeAttn& a, void* stream);
+int launch_accept(uint8_t* kp, uint16_t* kn, uint8_t* vp, uint16_t* vn, const int32_t* lens,
+                  int64_t n_groups, int64_t T_stride, int P, int M, const int32_t* path, int A,
+                  const int32_t* n_acc, int32_t* new_lens, void* stream);
+size_t evict_workspace_bytes(int64_t n_groups, int64_t T_stride);
+int launch_evict(const uint8_t* kp, const uint16_t* kn, const uint8_t* vp, const uint16_t* vn,
+                 const float* acc, const int32_t* lens, int64_t n_groups, int64_t T_stride, int P,
+                 int keep, int recent, int64_t T_out, uint8_t* kpo, uint16_t* kno, uint8_t* vpo,
+                 uint16_t* vno, float* acco, int32_t* new_lens, int32_t* index, void* ws,
+                 void* stream);
 }  // namespace dev
 
 }  // namespace fibq
