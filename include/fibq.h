@@ -285,9 +285,9 @@ int fibq_attn_decode_noalloc(const void* q, int q_dtype, const uint8_t* k_payloa
  * lengths: a group g (layer, sequence, kv-head) holds lens[g] cached tokens
  * (device, int32) in rows 0 .. lens[g] - 1 of its T_stride rows.  Lengths live
  * on the device, so a captured call follows them.  Common limits (else
- * FIBQ_EINVAL): 0 <= n_groups <= 65535, T_stride < 2^30.  Layouts, dtypes and
- * the scale are those of fibq_attn_decode.  Rows behind a group's last token
- * may hold anything. */
+ * FIBQ_EINVAL): 0 <= n_groups <= 65535, T_stride < 2^30, fewer than 2^31
+ * output elements.  Layouts, dtypes and the scale are those of
+ * fibq_attn_decode.  Rows behind a group's last token may hold anything. */
 
 /* Ancestor masks of a tree of M drafted tokens, host memory.  parents[i] is
  * the drafted token that token i follows, or -1 for one that follows the last

@@ -385,6 +385,7 @@ static int serve_attn_check(fibq::dev::ServeAttn* a, int d, int k, double b, int
     return FIBQ_EINVAL;
   if (!serve_sizes(a->n_groups, a->T_stride) || a->G < 1 || a->G > 16 || !std::isfinite(a->scale))
     return FIBQ_EINVAL;
+  if (a->n_groups * (a->M > 0 ? a->M : 1) * a->G * d >= (1LL << 31)) return FIBQ_EINVAL;
   if ((rc = check_supported(a->s)) != FIBQ_OK) return rc;
   if (a->n_groups == 0) {
     *done = true;

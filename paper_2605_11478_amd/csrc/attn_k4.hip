@@ -46,6 +46,7 @@
 
 #include <type_traits>
 
+#include "attn_rows4.h"
 #include "attn_split.h"
 #include "device_common.h"
 #include "fibq.h"
@@ -66,11 +67,6 @@ constexpr int kHeadBlocks = 2048;  // merge: a block per head up to so many head
 constexpr float kCs = 4096.0f;   // scale of the codebook's binary16 rows
 constexpr float kVs = 16384.0f;  // scale of the weights while all value norms are below 2
 
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef short s4 __attribute__((ext_vector_type(4)));
-typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 struct Plan {
@@ -133,17 +129,6 @@ static Plan make_plan(int64_t n_groups, int64_t T, int D, int max_wgs) {
   if (!p.whole) off = al(off + (size_t)p.wgs * (p.slots + kWaves - 1) * rec_floats(D) * 4);
   p.total = off;
   return p;
-}
-
-// maximum over the wavefront of v >= 0, in registers
-__device__ __forceinline__ float wave_max_dpp(float v) {
-  float x = v;
-#define FIBQ_ROR(n) x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + n, 0xf, 0xf, false)));
-  FIBQ_ROR(8) FIBQ_ROR(4) FIBQ_ROR(2) FIBQ_ROR(1)
-#undef FIBQ_ROR
-  const int i = __float_as_int(x);
-  return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
-               fmaxf(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
 }
 
 // ---------------------------------------------------------------- query ----
@@ -250,22 +235,12 @@ __global__ __launch_bounds__(256) void prep_kernel(const void* __restrict__ q, i
 }
 
 // ----------------------------------------------------------------- main ----
-__device__ __forceinline__ h4 tr_read(const unsigned char* lds_byte_addr) {
-  s4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s4*)(lds_byte_addr));
-  return __builtin_bit_cast(h4, r);
-}
 __device__ __forceinline__ float dpp_ror8(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
 }
 __device__ __forceinline__ uint32_t dpp_ror8u(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false);
 }
-__device__ __forceinline__ float xmax(float v, int mask) {
-  return fmaxf(v, __shfl_xor(v, mask, 64));
-}
-__device__ __forceinline__ float xsum(float v, int mask) { return v + __shfl_xor(v, mask, 64); }
-
 // One lane's raw loads of a unit: a payload quarter of the token whose K rows
 // it gathers in each tile, a quarter of the token whose V rows it addresses
 // in each tile, and the binary16 norms of the four tokens of its softmax work.
@@ -274,30 +249,6 @@ struct Unit {
   uint32_t kq[2][QW], vq[2][QW];  // [tile][dword of the quarter]
   uint32_t nk[2], nv[2];          // two binary16 norms per word
 };
-
-// LDS byte offset of the 4-dim row b of a quarter: index b / KB of the quarter
-// (w-bit indices, little-endian), row b % KB of its codeword.
-template <int QW, int W, int KB>
-__device__ __forceinline__ uint32_t qrow(const uint32_t (&qq)[QW], int b, int w) {
-  if constexpr (W == 8 && KB == 1) {
-    return ((qq[b >> 2] >> (8 * (b & 3))) & 0xFFu) * 8u;
-  } else if constexpr (W == 12 && KB == 1) {  // bits 12 b .. 12 b + 11 of the quarter
-    const int bit = 12 * b, wd = bit >> 5, sh = bit & 31;
-    uint32_t v = qq[wd] >> sh;
-    if (sh > 20) v |= qq[wd + 1] << (32 - sh);
-    return (v & 0xFFFu) * 8u;
-  } else {  // the quarter starts at bit 0 of qq
-    const int i = b / KB;
-    uint32_t v;
-    if constexpr (QW == 1) {
-      v = qq[0] >> (i * w);
-    } else {
-      const uint64_t u = (uint64_t)qq[0] | ((uint64_t)qq[1] << 32);
-      v = (uint32_t)(u >> (i * w));
-    }
-    return (v & ((1u << w) - 1u)) * (8u * KB) + 8u * (b % KB);
-  }
-}
 
 // Codewords of KB 4-dim rows (k = 4 KB); W > 0: compile-time index width,
 // W == 0: width `wr` at run time.

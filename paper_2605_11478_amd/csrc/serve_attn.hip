@@ -2,8 +2,37 @@
 // sequences of different lengths: the rows of a tree of drafted tokens
 // (fibq_attn_tree), and single-token rows whose softmax weights are added to
 // an accumulator per cached token (fibq_attn_decode_accum).
+//
+// Mathematics.  In rotated space a score is nu_t <q~, c_(t)> with q~ = Pi q
+// times scale * log2 e, the softmax is base 2, and the values are
+// sum_t p_t nu_t c_(t), rotated back once per row.  q~ and the weights p nu are
+// held as two binary16 parts (22 bits together) against the binary16 codewords,
+// so the products on the matrix cores carry float32 accuracy; a codebook that
+// binary16 does not hold adds its residual rows' products.  Statistics and sums
+// are float32.
+//
+// rows_kernel.  An item is (group, tile of 16 RT query rows); its work is cut
+// into units of 32 tokens.  The units of all items, in runs of 8 (one per
+// wavefront), are split into equal contiguous ranges, one per workgroup; the
+// lengths are on the device, so every workgroup finds its range from them.  For
+// each item that its range meets, a workgroup rotates the tile's queries, keeps
+// them in registers as operands, goes over its units, combines its wavefronts'
+// states in LDS and leaves one record (m, l, acc) in rotated space.  Per unit a
+// wavefront gathers the keys' and the values' codewords once for all RT row
+// tiles:
+//   scores  S[t][r] = K_hat[t][:] . q~[r][:]  (v_mfma_f32_16x16x32_f16, A = two
+//           gathered 4-dim codeword rows per lane, B = the queries' high, then
+//           low parts): lane l holds row l % 16 and tokens 4 (l / 16) + e of
+//           both 16-token tiles,
+//   values  acc[r][dims] += W[r][t] V_hat[t][dims]: those are the lane's K
+//           slots of the A operand, so the weights need no exchange; B comes
+//           from transposing LDS reads of codeword rows.
+// merge_kernel combines an item's records by log-sum-exp and applies Pi^T.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
+#include "attn_rows4.h"
 #include "device_common.h"
 #include "fibq.h"
 #include "fibq_internal.h"
@@ -12,158 +41,918 @@ namespace fibq {
 namespace dev {
 namespace sv {
 
-// q~ = Pi q * qscale of one row, by all threads of the block; xs: D floats of LDS
-template <int D>
-__device__ void rotate_row(const void* q, int q_dtype, int64_t at, const float* R, float qscale,
-                           float* xs, float* dst) {
-  for (int i = threadIdx.x; i < D; i += blockDim.x)
-    xs[i] = q_dtype == FIBQ_F32   ? static_cast<const float*>(q)[at + i]
-            : q_dtype == FIBQ_F16 ? to_float(static_cast<const f16_t*>(q)[at + i])
-                                  : to_float(static_cast<const bf16_t*>(q)[at + i]);
-  __syncthreads();
-  for (int i = threadIdx.x; i < D; i += blockDim.x) {
-    float s = 0.0f;
-    for (int j = 0; j < D; ++j) s = fmaf(R[i * D + j], xs[j], s);
-    dst[i] = s * qscale;
-  }
-  __syncthreads();
+constexpr int kWaves = 8;              // wavefronts per workgroup
+constexpr int kThreads = 64 * kWaves;
+constexpr int kStep = 32;              // tokens per unit
+constexpr int kRun = kStep * kWaves;   // tokens per run of units
+constexpr int kTop = 64;               // partial maxima of a codebook
+constexpr float kLag = 8.0f;           // a maximum moves when a score exceeds it by this (log2)
+constexpr float kCs = 4096.0f;         // scale of the codebook's binary16 rows
+
+struct Args {
+  const void* q;
+  int q_dtype;
+  const uint8_t* kp;
+  const uint16_t* kn;
+  const uint8_t* vp;
+  const uint16_t* vn;
+  const int32_t* lens;
+  const uint64_t* masks;
+  int64_t mask_stride;
+  int n_groups, M, G, rows, tiles;  // rows of a group, row tiles of a group
+  int64_t T_stride;
+  int k, N, w, P, pair_n;
+  const float* R;
+  const float* C;
+  float qscale;
+  float* rec;
+  int32_t* bounds;    // first and last workgroup of every item
+  const float* top;   // kTop partial maxima of |C| (staged codes)
+  const float* stat;  // weights pass: m, l of every row
+  float* acc;         // weights pass
+  int lds_scratch;
+};
+
+__host__ __device__ constexpr int rec_floats(int D, int RT) { return 16 * RT * (D + 2); }
+constexpr int tile_stride(int D) { return 2 * D + 16; }  // bytes of a staged row: spreads the banks
+constexpr int state_regs(int D, int RT) { return RT * (D / 16) * 4 + 2 * RT; }
+
+// runs of units of a group; none for a bad length
+__device__ __forceinline__ int runs_of(const Args& a, int g) {
+  const int len = a.lens[g];
+  if (len < 0 || len > a.T_stride - a.M) return 0;
+  return (len + a.M + kRun - 1) / kRun;
 }
 
-template <int D>
-__device__ float score(const float* qr, const uint8_t* row, uint16_t nu, const Shape& s,
-                       const float* C) {
-  float a = 0.0f;
-  for (int m = 0; m < D / s.k; ++m) {
-    const float* c = C + (size_t)extract_index(row, m, s.w) * s.k;
-    for (int e = 0; e < s.k; ++e) a = fmaf(qr[m * s.k + e], c[e], a);
-  }
-  return a * half_bits_to_float(nu);
+// two values as binary16 pairs: high parts, and the rest taken from their bits
+__device__ __forceinline__ void split2(float a, float b, uint32_t* hi, uint32_t* lo) {
+  uint32_t u = __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
+  asm("" : "+v"(u));
+  const h2 h = __builtin_bit_cast(h2, u);
+  *hi = u;
+  *lo = __builtin_bit_cast(uint32_t, h2{(_Float16)(a - (float)h[0]), (_Float16)(b - (float)h[1])});
 }
 
-// One block per (group, row).  M = 0: single-token rows, else the drafted
-// tokens of the group.
-template <int D>
-__global__ __launch_bounds__(256) void rows_kernel(
-    const void* __restrict__ q, int q_dtype, const uint8_t* __restrict__ kp,
-    const uint16_t* __restrict__ kn, const uint8_t* __restrict__ vp,
-    const uint16_t* __restrict__ vn, const int32_t* __restrict__ lens,
-    const uint64_t* __restrict__ masks, int64_t mask_stride, int M, int G, int64_t T_stride,
-    Shape s, const float* __restrict__ R, const float* __restrict__ C, float qscale,
-    float* __restrict__ stat, float* __restrict__ out) {
-  __shared__ float xs[D], qr[D], red[4], ps[256], part[256];
-  const int rows = max(M, 1) * G, tid = threadIdx.x;
-  const int64_t g = blockIdx.x / rows;
-  const int r = (int)(blockIdx.x % rows);
-  float* o = out + (g * rows + r) * D;
-  const int len = lens[g];
-  if (len < 0 || len > T_stride - M) {
-    for (int i = tid; i < D; i += 256) o[i] = NAN;
-    if (stat && tid < 2) stat[(g * rows + r) * 2 + tid] = NAN;
-    return;
+template <typename IN>
+__device__ __forceinline__ f4 load4(const void* q, int64_t at) {
+  IN w[4];
+  __builtin_memcpy(w, static_cast<const IN*>(q) + at, sizeof(w));
+  return f4{to_float(w[0]), to_float(w[1]), to_float(w[2]), to_float(w[3])};
+}
+
+// One lane's loads of a unit: a payload quarter of the token whose K row it
+// gathers in each tile, one of the token whose V rows it addresses, and the
+// norms of its eight softmax tokens (binary16 pairs).
+template <int QW>
+struct Unit {
+  uint32_t kq[2][QW], vq[2][QW];
+  uint32_t nk[4], nv[4];
+};
+
+// W > 0: compile-time index width, W = 0: at run time; KB: 4-dim rows per
+// codeword; QW: dwords of a payload quarter, 0 for staged codes (below).
+// WT: the weights pass (scores only, added to acc).
+//
+// Staged codes (QW = 0) are those whose codewords cannot be addressed as 4-dim
+// rows of an LDS table (k = 1, most of k = 2, quarters of a payload that share
+// a codeword, tables above 64 KB): each wavefront writes the decoded rows of
+// its unit, keys and then values, into a tile of its own and reads the operands
+// from there.
+template <int D, int RT, int W, int KB, int QW, bool WT>
+__global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_kernel(const Args a) {
+  constexpr int NB = D / 4, Q = NB / 4;  // 4-dim rows, of them per quarter
+  constexpr int KS = D / 32, VM = D / 16, KQ = D / 4;
+  constexpr int ROWS = 16 * RT, QS = D + 4;  // (floats between rows of the rotated queries)
+  constexpr bool kStaged = QW == 0;
+  constexpr int QD = kStaged ? 1 : QW;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ uint64_t wsum[kWaves];
+  __shared__ uint64_t start[2];
+  __shared__ float red[kWaves];
+  __shared__ int redi[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g16 = lane >> 4, c = lane & 15;
+  const int w = W > 0 ? W : a.w;
+  const int P = a.P;
+
+  // ---- this workgroup's range of runs
+  const int per = (a.n_groups + kThreads - 1) / kThreads;
+  uint64_t mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int g = tid * per + i;
+    if (g < a.n_groups) mine += runs_of(a, g);
   }
-  rotate_row<D>(q, q_dtype, (g * rows + r) * D, R, qscale, xs, qr);
-  const uint64_t mask = M > 0 ? masks[g * mask_stride + r / G] : 0;
-  const int64_t base = g * T_stride;
-  const int tot = len + M;
-  const int dim = tid % D;
-  float m = -INFINITY, l = 0.0f, acc = 0.0f;
-  for (int t0 = 0; t0 < tot; t0 += 256) {
-    const int t = t0 + tid;
-    float sc = -INFINITY;
-    if (t < tot && (t < len || (mask >> (t - len) & 1)))
-      sc = score<D>(qr, kp + (base + t) * s.P, kn[base + t], s, C);
-    float mx = wave_max(sc);
-    if ((tid & 63) == 0) red[tid >> 6] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.0f : mn;
-    const float f = exp2f(m - ref), p = exp2f(sc - ref);
-    m = mn;
-    l = l * f + p;
-    acc *= f;
-    ps[tid] = p;
-    __syncthreads();
-    for (int i = tid / D; i < min(256, tot - t0); i += 256 / D) {
-      if (ps[i] == 0.0f) continue;
-      const int64_t v = base + t0 + i;
-      const uint32_t idx = extract_index(vp + v * s.P, dim / s.k, s.w);
-      acc = fmaf(ps[i] * half_bits_to_float(vn[v]), C[(size_t)idx * s.k + dim % s.k], acc);
+  mine *= a.tiles;
+  uint64_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t y = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) wsum[wave] = upto;
+  __syncthreads();
+  uint64_t all = 0, before = upto - mine;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < wave) before += wsum[i];
+    all += wsum[i];
+  }
+  const uint32_t nwg = gridDim.x, b = blockIdx.x;
+  const uint64_t each = all >> 32 ? all / nwg : (uint32_t)all / nwg;
+  const uint32_t rest = (uint32_t)(all - each * nwg);
+  const uint64_t from = b * each + min(b, rest);
+  uint64_t left = each + (b < rest);
+  if (left == 0) return;
+  if (from >= before && from < before + mine) {
+    uint64_t off = from - before;
+    int g = tid * per;
+    for (;; ++g) {
+      const uint64_t v = (uint64_t)runs_of(a, g) * a.tiles;
+      if (off < v) break;
+      off -= v;
     }
+    start[0] = g;
+    start[1] = off;
+  }
+
+  // ---- the codebook's binary16 rows times cs (pairs: of the pair codebook) and
+  //      their residuals.  Entries of unit vectors' blocks are at most 1; at
+  //      2^12 one above 2^-14 keeps 22 bits.  Other codebooks are staged again
+  //      at the power of two that takes their largest entry to [2^13, 2^14).
+  const int nrow = kStaged ? 0 : a.pair_n > 0 ? a.pair_n * a.pair_n : a.N * a.k / 4;
+  bool has_lo = false;
+  float cs = kCs, ci = 1.0f / kCs;
+  auto pick_scale = [&](float top) {
+    if (top == 0.0f || (top >= 0x1p-6f && top < 15.9f)) return false;
+    int e2 = 0;
+    frexpf(top, &e2);
+    e2 = top < INFINITY ? min(max(14 - e2, -100), 100) : 0;
+    cs = ldexpf(1.0f, e2);
+    ci = ldexpf(1.0f, -e2);
+    return true;
+  };
+  if constexpr (kStaged) {
+    pick_scale(wave_max_dpp(a.top[lane]));
     __syncthreads();
+  } else {
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+      bool lo_any = false;
+      float top = 0.0f;
+      for (int i = tid; i < nrow; i += kThreads) {
+        float cv[4];
+        if (a.pair_n > 0) {
+          __builtin_memcpy(cv, a.C + 2 * (i % a.pair_n), 8);
+          __builtin_memcpy(cv + 2, a.C + 2 * (i / a.pair_n), 8);
+        } else {
+          __builtin_memcpy(cv, a.C + (size_t)i * 4, 16);
+        }
+        h4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          hi[e] = (_Float16)(cv[e] * cs);
+          lo[e] = (_Float16)fmaf(cv[e], cs, -(float)hi[e]);
+          lo_any |= (float)lo[e] != 0.0f;
+          top = fmaxf(top, fabsf(cv[e]));
+        }
+        reinterpret_cast<h4*>(smem)[i] = hi;
+        reinterpret_cast<h4*>(smem)[nrow + i] = lo;
+      }
+      top = wave_max_dpp(top);
+      lo_any = __any(lo_any);
+      if (lane == 0) {
+        red[wave] = top;
+        redi[wave] = lo_any;
+      }
+      __syncthreads();
+      has_lo = __any(lane < kWaves && redi[lane & (kWaves - 1)] != 0);
+      top = wave_max_dpp(red[lane & (kWaves - 1)]);
+      if (again || !pick_scale(top)) break;
+      __syncthreads();  // (red is written again)
+    }
   }
-  float ls = wave_sum(l);
-  if ((tid & 63) == 0) red[tid >> 6] = ls;
-  part[tid] = acc;
-  __syncthreads();
-  ls = red[0] + red[1] + red[2] + red[3];
-  if (stat && tid == 0) {
-    stat[(g * rows + r) * 2] = m;
-    stat[(g * rows + r) * 2 + 1] = ls;
-  }
-  if (tid < D) {
-    float a = 0.0f;
-    for (int i = tid; i < 256; i += D) a += part[i];
-    xs[tid] = ls == 0.0f ? 0.0f : a / ls;
-  }
-  __syncthreads();
-  if (tid < D) {
-    float a = 0.0f;
-    for (int i = 0; i < D; ++i) a = fmaf(R[i * D + tid], xs[i], a);
-    o[tid] = a;
+  int g = (int)start[0];
+  uint64_t off = start[1];
+
+  float* scratch = reinterpret_cast<float*>(smem + a.lds_scratch);
+  // (staged: a tile of high parts, then of residuals, for each wavefront)
+  unsigned char* tile = smem + a.lds_scratch + (size_t)wave * 2 * kStep * tile_stride(D);
+  // quarter g16 of token c of a tile for K, quarter c % 4 of token 4 g16 + c / 4
+  // for V: 4 QW bytes inside the row that hold its bits from bit `sh` on
+  const int NI = Q / KB;
+  const int kbit = g16 * NI * w, vbit = (c & 3) * NI * w;
+  const int kst = min(kbit >> 3, P - 4 * QD), vst = min(vbit >> 3, P - 4 * QD);
+  const int ksh = kbit - 8 * kst, vsh = vbit - 8 * vst;
+  auto quarter = [&](const uint8_t* at, int sh, uint32_t (&d)[QD]) {
+    __builtin_memcpy(d, at, 4 * QD);
+    if constexpr (QD == 1) {
+      d[0] >>= sh;
+    } else if constexpr (QD == 2) {
+      const uint64_t u = ((uint64_t)d[0] | ((uint64_t)d[1] << 32)) >> sh;
+      d[0] = (uint32_t)u;
+      d[1] = (uint32_t)(u >> 32);
+    }
+  };
+
+  // ---- one item, runs r0 .. r0 + take - 1
+  auto segment = [&](int len, int rt0, int r0, int take) {
+    const int tot = len + a.M;
+    const int64_t base = (int64_t)g * a.T_stride;
+    auto load = [&](int u) -> Unit<QD> {
+      Unit<QD> x{};
+      const int tb = u * kStep, tm = tot - 1;
+      const uint16_t* kng = a.kn + base;
+      const uint16_t* vng = a.vn + base;
+      const bool whole = tb + kStep <= tot;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if constexpr (!kStaged) {
+          const int tk = whole ? tb + 16 * t + c : min(tb + 16 * t + c, tm);
+          quarter(a.kp + (base + tk) * P + kst, ksh, x.kq[t]);
+          if constexpr (!WT) {
+            const int tv0 = tb + 16 * t + 4 * g16 + (c >> 2);
+            const int tv = whole ? tv0 : min(tv0, tm);
+            quarter(a.vp + (base + tv) * P + vst, vsh, x.vq[t]);
+          }
+        }
+        const int ts = tb + 16 * t + 4 * g16;
+        if (whole) {
+          __builtin_memcpy(&x.nk[2 * t], kng + ts, 8);
+          if constexpr (!WT) __builtin_memcpy(&x.nv[2 * t], vng + ts, 8);
+        } else {  // (tokens behind the last one: norm 0)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int at = min(ts + e, tm);
+            const uint32_t in = ts + e <= tm ? 0xFFFFu : 0u;
+            x.nk[2 * t + (e >> 1)] |= (kng[at] & in) << (16 * (e & 1));
+            if constexpr (!WT) x.nv[2 * t + (e >> 1)] |= (vng[at] & in) << (16 * (e & 1));
+          }
+        }
+      }
+      return x;
+    };
+    const int u_end = min((r0 + take) * kWaves, (tot + kStep - 1) / kStep);
+    int u = r0 * kWaves + wave;
+    Unit<QD> cur{};
+    if (u < u_end) cur = load(u);  // goes out before the queries are built
+
+    // ---- the tile's queries: rotated on v_mfma_f32_16x16x4_f32 (float32 products
+    //      and sums; K slot kk of lane group gq is column KQ gq + kk), then as
+    //      operands at the power of two that takes the largest finite entry to
+    //      [2^13, 2^14), so that the low parts are normal numbers
+    const int row0 = rt0 * ROWS, live = (min(ROWS, a.rows - row0) + 15) / 16;
+    float* qt = scratch;
+    __syncthreads();  // (the scratch is free)
+    float top = 0.0f;
+    for (int it = wave; it < (D / 16) * live; it += kWaves) {
+      const int dt = it % (D / 16), t = it / (D / 16);
+      const int row = row0 + 16 * t + c;
+      f4 pa[KQ / 4], pb[KQ / 4] = {};
+#pragma unroll
+      for (int p = 0; p < KQ / 4; ++p)
+        __builtin_memcpy(&pa[p], a.R + (16 * dt + c) * D + KQ * g16 + 4 * p, 16);
+      if (row < a.rows) {
+        const int64_t at = ((int64_t)g * a.rows + row) * D + KQ * g16;
+#pragma unroll
+        for (int p = 0; p < KQ / 4; ++p)
+          pb[p] = a.q_dtype == FIBQ_F32   ? load4<float>(a.q, at + 4 * p)
+                  : a.q_dtype == FIBQ_F16 ? load4<f16_t>(a.q, at + 4 * p)
+                                          : load4<bf16_t>(a.q, at + 4 * p);
+      }
+      f4 s = {0, 0, 0, 0};
+#pragma unroll
+      for (int p = 0; p < KQ / 4; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_16x16x4f32(pa[p][e], pb[p][e], s, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] *= a.qscale;
+        top = fmaxf(top, fabsf(s[e]) < INFINITY ? fabsf(s[e]) : 0.0f);
+      }
+      *reinterpret_cast<f4*>(qt + (16 * t + c) * QS + 16 * dt + 4 * g16) = s;
+    }
+    top = wave_max_dpp(top);
+    if (lane == 0) red[wave] = top;
+    __syncthreads();
+    top = wave_max_dpp(red[lane & (kWaves - 1)]);
+    float qs = 1.0f, qi = 1.0f;
+    if (top > 0.0f) {
+      int e2 = 0;
+      frexpf(top, &e2);
+      e2 = max(e2 - 14, -100);
+      qs = ldexpf(1.0f, e2);
+      qi = ldexpf(1.0f, -e2);
+    }
+    h8 bh[RT][KS], bl[RT][KS];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int kap = 0; kap < KS; ++kap) {
+        if (t >= live) continue;
+        const float* at = qt + (16 * t + c) * QS + 4 * (g16 * Q + 2 * kap);
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split2(at[2 * i] * qi, at[2 * i + 1] * qi, &hi[i], &lo[i]);
+        __builtin_memcpy(&bh[t][kap], hi, 16);
+        __builtin_memcpy(&bl[t][kap], lo, 16);
+      }
+    if constexpr (kStaged) __syncthreads();  // (tiles overwrite qt)
+    const float ks = qs * ci;  // scores: products times nu_K times this, in log2 units
+
+    f4 acc[RT][VM];
+    float m[RT], l[RT];
+    float vlim = 0.0f, vs = 1.0f;  // bound of the value norms so far, their scale
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m[t] = -INFINITY;
+      l[t] = 0.0f;
+#pragma unroll
+      for (int mu = 0; mu < VM; ++mu) acc[t][mu] = f4{0, 0, 0, 0};
+    }
+    if constexpr (WT) {  // this row's statistics
+      const int64_t at = ((int64_t)g * a.rows + min(c, a.rows - 1)) * 2;
+      m[0] = a.stat[at] == -INFINITY ? 0.0f : a.stat[at];
+      l[0] = c < a.rows && a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
+    }
+    uint64_t mask[RT];
+    if constexpr (!WT) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+        mask[t] = a.M > 0 ? a.masks[g * a.mask_stride + min(row0 + 16 * t + c, a.rows - 1) / a.G] : 0;
+    }
+
+    // staged codes: rows of the unit's tokens into the tile; whether any has a residual
+    auto stage = [&](const uint8_t* pay, int tb) -> bool {
+      bool any = false;
+      const int nt = min(kStep, tot - tb);
+      for (int x = lane; x < kStep * NB; x += 64) {
+        const int tok = x / NB, p = x % NB;
+        const uint8_t* row = pay + (base + tb + min(tok, nt - 1)) * P;
+        const int n = a.k >= 4 ? 1 : 4 / a.k;  // codewords of the piece
+        const int bit = (a.k >= 4 ? 4 * p / a.k : p * n) * w;
+        uint64_t bits = 0;
+        if (P >= 8) {
+          const int st = min(bit >> 3, P - 8);
+          __builtin_memcpy(&bits, row + st, 8);
+          bits >>= bit - 8 * st;
+        } else {
+          for (int i = 0; i < P; ++i) bits |= (uint64_t)row[i] << (8 * i);
+          bits >>= bit;
+        }
+        const uint64_t ones = (1ull << w) - 1;
+        float cv[4];
+        if (a.k >= 4) {
+          __builtin_memcpy(cv, a.C + (size_t)(bits & ones) * a.k + 4 * p % a.k, 16);
+        } else if (a.k == 2) {
+          __builtin_memcpy(cv, a.C + 2 * (size_t)(bits & ones), 8);
+          __builtin_memcpy(cv + 2, a.C + 2 * (size_t)(bits >> w & ones), 8);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) cv[e] = a.C[bits >> (e * w) & ones];
+        }
+        uint32_t hi[2], lo[2];
+        split2(cv[0] * cs, cv[1] * cs, &hi[0], &lo[0]);
+        split2(cv[2] * cs, cv[3] * cs, &hi[1], &lo[1]);
+        any |= ((lo[0] | lo[1]) & 0x7FFF7FFFu) != 0;
+        unsigned char* to = tile + tok * tile_stride(D) + 8 * p;
+        __builtin_memcpy(to, hi, 8);
+        __builtin_memcpy(to + kStep * tile_stride(D), lo, 8);
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+      return __any(any);
+    };
+
+    auto compute = [&](const Unit<QD>& x, int tb) {
+      bool lo_now = has_lo;  // (uniform) residual rows to add
+      if constexpr (kStaged) lo_now = stage(a.kp, tb);
+      // two gathered rows per lane of tile t, K-step kap, `d` bytes behind the high parts
+      auto krow = [&](int t, int kap, int d) -> h8 {
+        if constexpr (kStaged) {
+          return *reinterpret_cast<const h8*>(tile + (16 * t + c) * tile_stride(D) + 8 * (g16 * Q + 2 * kap) + d);
+        } else {
+          const h4 a0 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(x.kq[t], 2 * kap, w) + d);
+          const h4 a1 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(x.kq[t], 2 * kap + 1, w) + d);
+          return h8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+        }
+      };
+      const int lo_at = kStaged ? kStep * tile_stride(D) : nrow * 8;
+      h8 ka[2][KS];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kap = 0; kap < KS; ++kap) ka[t][kap] = krow(t, kap, 0);
+      float nk[8], nv[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const h2 k2 = __builtin_bit_cast(h2, x.nk[i]), v2 = __builtin_bit_cast(h2, x.nv[i]);
+        nk[2 * i] = (float)k2[0] * ks;
+        nk[2 * i + 1] = (float)k2[1] * ks;
+        nv[2 * i] = (float)v2[0];
+        nv[2 * i + 1] = (float)v2[1];
+      }
+      if constexpr (!WT) {
+        // the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(nv[i]));
+        if (__any(top > vlim)) {
+          top = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            top = fmaxf(top, fabsf(nv[i]) < INFINITY ? fabsf(nv[i]) : 0.0f);
+          top = xmax(xmax(top, 16), 32);
+          if (top > vlim) {  // (uniform)
+            int e2 = 0;
+            frexpf(top, &e2);
+            const float now = ldexpf(1.0f, 7 - e2), f = now / vs;
+            vlim = ldexpf(1.0f, e2);
+            vs = now;
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+              for (int mu = 0; mu < VM; ++mu) acc[t][mu] *= f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) nv[i] *= vs;
+      }
+      const bool tail = tb + kStep > len;
+      h8 wh[RT], wl[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        if (t >= live) continue;
+        f4 s[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          s[i] = f4{0, 0, 0, 0};
+#pragma unroll
+          for (int kap = 0; kap < KS; ++kap) {
+            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[i][kap], bl[t][kap], s[i], 0, 0, 0);
+            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[i][kap], bh[t][kap], s[i], 0, 0, 0);
+          }
+        }
+        if (lo_now) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int kap = 0; kap < KS; ++kap)
+              s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(krow(i, kap, lo_at), bh[t][kap], s[i], 0, 0, 0);
+        }
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = fmaf(s[i >> 2][i & 3], nk[i], -m[t]);
+        uint32_t seen = 0xFFu;  // of this lane's tokens (tail units)
+        if (tail) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int j = tb + 16 * (i >> 2) + 4 * g16 + (i & 3) - len;
+            bool in = j < 0;
+            if constexpr (!WT) in = in || (j < a.M && (mask[t] >> (j & 63) & 1));
+            if (!in) {
+              p[i] = -INFINITY;
+              seen &= ~(1u << i);
+            }
+          }
+        }
+        if constexpr (WT) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]) * l[0];
+          // sums over the rows (lanes of a 16-lane row), each step halving the
+          // tokens that a lane keeps: bits 3, 2, 1 of c pick token i's bits 2, 1, 0
+          auto dpp = [](float v, auto ctrl) {
+            return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
+          };
+          const bool b3 = c & 8, b2 = c & 4, b1 = c & 2;
+          float x4[4], x2[2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)  // row_ror:8 swaps lanes c and c ^ 8
+            x4[i] = (b3 ? p[i + 4] : p[i]) + dpp(b3 ? p[i] : p[i + 4], std::integral_constant<int, 0x128>{});
+#pragma unroll
+          for (int i = 0; i < 2; ++i)  // row_half_mirror: lanes c and c ^ 7
+            x2[i] = (b2 ? x4[i + 2] : x4[i]) + dpp(b2 ? x4[i] : x4[i + 2], std::integral_constant<int, 0x141>{});
+          // quad_perm [2, 3, 0, 1] and [1, 0, 3, 2]: lanes c and c ^ 2, c and c ^ 1
+          float x1 = (b1 ? x2[1] : x2[0]) + dpp(b1 ? x2[0] : x2[1], std::integral_constant<int, 0x4E>{});
+          x1 += dpp(x1, std::integral_constant<int, 0xB1>{});
+          const int at = tb + 16 * (b3 ? 1 : 0) + 4 * g16 + (b2 ? 2 : 0) + (b1 ? 1 : 0);
+          if ((c & 1) == 0 && at < tot) a.acc[base + at] += x1;
+          continue;
+        }
+        float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])),
+                          fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+        // a score far above the maximum, or (not a number or infinite) no finite one yet
+        if (__any(!(top <= kLag))) {
+          const bool first = m[t] == -INFINITY;
+          float mh = top;
+          if (first) {
+            mh = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (seen >> i & 1) mh = fmaxf(mh, s[i >> 2][i & 3] * nk[i]);
+          }
+          mh = xmax(xmax(mh, 16), 32);
+          const float m_new = first ? mh : m[t] + fmaxf(mh, 0.0f);
+          const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
+          m[t] = m_new;
+          const float sub = m_new == -INFINITY ? 0.0f : m_new;  // (scores of -inf have weight 0)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            p[i] = seen >> i & 1 ? fmaf(s[i >> 2][i & 3], nk[i], -sub) : -INFINITY;
+          l[t] *= f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float fr = __shfl(f, 4 * g16 + e, 64);
+#pragma unroll
+            for (int mu = 0; mu < VM; ++mu) acc[t][mu][e] *= fr;
+          }
+        }
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) l[t] += p[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] *= nv[i];
+        if (tail) {  // (an unseen token's norm may be anything)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (!(seen >> i & 1)) p[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], &hi[i], &lo[i]);
+        __builtin_memcpy(&wh[t], hi, 16);
+        __builtin_memcpy(&wl[t], lo, 16);
+      }
+      if constexpr (!WT) {
+        if constexpr (kStaged) lo_now = stage(a.vp, tb);
+#pragma unroll
+        for (int mu = 0; mu < VM; ++mu) {
+          const unsigned char *ra, *rb;
+          if constexpr (kStaged) {
+            ra = tile + (4 * g16 + (c >> 2)) * tile_stride(D) + 8 * ((c & 3) * VM + mu);
+            rb = ra + 16 * tile_stride(D);
+          } else {
+            ra = smem + qrow<QD, W, KB>(x.vq[0], mu, w);
+            rb = smem + qrow<QD, W, KB>(x.vq[1], mu, w);
+          }
+          const h4 b0 = tr_read(ra), b1 = tr_read(rb);
+          const h8 bv = h8{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            if (t >= live) continue;
+            acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl[t], bv, acc[t][mu], 0, 0, 0);
+            acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], bv, acc[t][mu], 0, 0, 0);
+          }
+          if (lo_now) {
+            const h4 d0 = tr_read(ra + lo_at), d1 = tr_read(rb + lo_at);
+            const h8 dv = h8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+              if (t < live)
+                acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], dv, acc[t][mu], 0, 0, 0);
+          }
+        }
+      }
+      if constexpr (kStaged) {  // (the next unit writes the tile)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+      }
+    };
+
+    for (; u < u_end; u += kWaves) {
+      Unit<QD> nxt{};
+      if (u + kWaves < u_end) nxt = load(u + kWaves);
+      compute(cur, u * kStep);
+      cur = nxt;
+    }
+
+    if constexpr (!WT) {
+      // ---- the wavefronts' states, halves at a time, into wavefront 0's
+      const float vi = ci / vs;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        l[t] = xsum(xsum(l[t], 16), 32);
+#pragma unroll
+        for (int mu = 0; mu < VM; ++mu) acc[t][mu] *= vi;
+      }
+      __syncthreads();  // (staged: the tiles are done with)
+      for (int h = kWaves / 2; h > 0; h >>= 1) {
+        float* st = scratch + (size_t)(wave - (wave >= h ? h : 0)) * 64 * state_regs(D, RT) + lane;
+        if (wave >= h && wave < 2 * h) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            st[(2 * t) * 64] = m[t];
+            st[(2 * t + 1) * 64] = l[t];
+#pragma unroll
+            for (int mu = 0; mu < VM; ++mu)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) st[(2 * RT + (t * VM + mu) * 4 + e) * 64] = acc[t][mu][e];
+          }
+        }
+        __syncthreads();
+        if (wave < h) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const float mo = st[(2 * t) * 64], lo = st[(2 * t + 1) * 64];
+            const float mx = fmaxf(m[t], mo), sub = mx == -INFINITY ? 0.0f : mx;
+            const float f = __builtin_amdgcn_exp2f(m[t] - sub), fo = __builtin_amdgcn_exp2f(mo - sub);
+            m[t] = mx;
+            l[t] = l[t] * f + lo * fo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float fr = __shfl(f, 4 * g16 + e, 64), fro = __shfl(fo, 4 * g16 + e, 64);
+#pragma unroll
+              for (int mu = 0; mu < VM; ++mu)
+                acc[t][mu][e] = acc[t][mu][e] * fr + st[(2 * RT + (t * VM + mu) * 4 + e) * 64] * fro;
+            }
+          }
+        }
+        __syncthreads();
+      }
+      const int64_t item = (int64_t)g * a.tiles + rt0;
+      if (wave == 0) {
+        // items and workgroups both only grow along the units, so item + workgroup
+        // is a different number for every segment
+        float* r = a.rec + (item + b) * rec_floats(D, RT);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          if (lane < 16) {
+            r[16 * t + lane] = m[t];
+            r[ROWS + 16 * t + lane] = l[t];
+          }
+#pragma unroll
+          for (int mu = 0; mu < VM; ++mu)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              r[2 * ROWS + (16 * t + 4 * g16 + e) * D + 4 * ((c >> 2) * VM + mu) + (c & 3)] = acc[t][mu][e];
+        }
+        if (lane == 0) {
+          if (r0 == 0) a.bounds[2 * item] = b;
+          if (r0 + take == (tot + kRun - 1) / kRun) a.bounds[2 * item + 1] = b;
+        }
+      }
+    }
+  };
+
+  while (left > 0) {
+    // the next group that holds units (64 at a time)
+    for (;;) {
+      const int at = g + lane;
+      const uint64_t some = __ballot(at < a.n_groups && runs_of(a, min(at, a.n_groups - 1)) > 0);
+      if (some) {
+        g += __builtin_ctzll(some);
+        break;
+      }
+      g += 64;
+      if (g >= a.n_groups) return;  // (not reached: units are left)
+    }
+    const int len = a.lens[g], runs = runs_of(a, g);
+    const int rt0 = (int)(off / runs), r0 = (int)(off - (uint64_t)rt0 * runs);
+    const int take = (int)(left < (uint64_t)(runs - r0) ? left : (uint64_t)(runs - r0));
+    segment(len, rt0, r0, take);
+    left -= take;
+    off += take;
+    if (off == (uint64_t)runs * a.tiles) {
+      off = 0;
+      ++g;
+    }
   }
 }
 
-// acc[g][t] += sum over the heads of 2^(score - m) / l.
+// Partial maxima of |C| for staged codes, whose workgroups do not read all of it.
+__global__ __launch_bounds__(256) void top_kernel(const float* __restrict__ C, int n,
+                                                  float* __restrict__ top) {
+  __shared__ float red[4];
+  float t = 0.0f;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += kTop * 256) t = fmaxf(t, fabsf(C[i]));
+  t = wave_max_dpp(t);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) top[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+
+// Block: 256 / D rows of a group, a thread per (row, dim).  Log-sum-exp over the
+// row's records, o = Pi^T (acc / l); stat (nullable) receives m and l.
 template <int D>
-__global__ __launch_bounds__(256) void weights_kernel(
-    const void* __restrict__ q, int q_dtype, const uint8_t* __restrict__ kp,
-    const uint16_t* __restrict__ kn, const int32_t* __restrict__ lens, int G, int64_t T_stride,
-    Shape s, const float* __restrict__ R, const float* __restrict__ C, float qscale,
-    const float* __restrict__ stat, float* __restrict__ acc) {
-  __shared__ float xs[D], qr[16 * D];
-  const int64_t g = blockIdx.y;
+__global__ __launch_bounds__(256) void merge_kernel(
+    const float* __restrict__ rec, const int32_t* __restrict__ bounds,
+    const int32_t* __restrict__ lens, int64_t T_stride, int M, int rows, int tiles, int tile_rows,
+    const float* __restrict__ R, float* __restrict__ stat, float* __restrict__ out) {
+  constexpr int HB = 256 / D;
+  __shared__ float ar[HB][D];
+  const int blocks = (rows + HB - 1) / HB;
+  const int64_t g = blockIdx.x / blocks;
+  const int hr = threadIdx.x / D, dim = threadIdx.x % D;
+  const int row = (int)(blockIdx.x % blocks) * HB + hr;
   const int len = lens[g];
-  if (len < 0 || len > T_stride || (int64_t)blockIdx.x * 256 >= len) return;
-  for (int h = 0; h < G; ++h)
-    rotate_row<D>(q, q_dtype, (g * G + h) * D, R, qscale, xs, qr + h * D);
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= len) return;
-  const int64_t at = g * T_stride + t;
-  float a = 0.0f;
-  for (int h = 0; h < G; ++h) {
-    const float sc = score<D>(qr + h * D, kp + at * s.P, kn[at], s, C);
-    const float m = stat[(g * G + h) * 2], l = stat[(g * G + h) * 2 + 1];
-    a += exp2f(sc - m) / l;
+  const bool bad = len < 0 || len > T_stride - M;
+  float m = -INFINITY, l = 0.0f, s = 0.0f;
+  if (!bad && len + M > 0 && row < rows) {
+    const int64_t item = g * tiles + row / tile_rows;
+    const int rl = row % tile_rows, reclen = tile_rows * (D + 2);
+    const int first = bounds[2 * item], n = bounds[2 * item + 1] - first + 1;
+    const float* r = rec + (item + first) * reclen;
+    for (int i0 = 0; i0 < n; i0 += 4) {
+      float mk[4], lk[4], xk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* x = r + (int64_t)min(i0 + i, n - 1) * reclen;
+        mk[i] = i0 + i < n ? x[rl] : -INFINITY;
+        lk[i] = i0 + i < n ? x[tile_rows + rl] : 0.0f;
+        xk[i] = i0 + i < n ? x[2 * tile_rows + rl * D + dim] : 0.0f;
+      }
+      const float mn = fmaxf(m, fmaxf(fmaxf(mk[0], mk[1]), fmaxf(mk[2], mk[3])));
+      const float sub = mn == -INFINITY ? 0.0f : mn;
+      const float f = __builtin_amdgcn_exp2f(m - sub);
+      l *= f;
+      s *= f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float fi = __builtin_amdgcn_exp2f(mk[i] - sub);
+        l = fmaf(lk[i], fi, l);
+        s = fmaf(xk[i], fi, s);
+      }
+      m = mn;
+    }
   }
-  acc[at] += a;
+  ar[hr][dim] = l == 0.0f ? 0.0f : s / l;
+  __syncthreads();
+  if (row >= rows) return;
+  float o = 0.0f;
+#pragma unroll 16
+  for (int i = 0; i < D; ++i) o = fmaf(R[i * D + dim], ar[hr][i], o);
+  out[(g * rows + row) * D + dim] = bad ? NAN : o;
+  if (stat && dim < 2) stat[(g * rows + row) * 2 + dim] = dim == 0 ? m : l;
+}
+
+// ----------------------------------------------------------------- host ----
+// How a code's rows are gathered: through an LDS table (codes whose payload
+// quarters hold whole codewords and lie in 4, 8 or 12 bytes of the row), or
+// staged.
+struct Kind {
+  int w, kb, qw;  // template arguments (w = 0: at run time)
+  int lds;        // bytes of the table
+};
+static Kind kind_of(const Shape& s, Shape* as, int* pair_n) {
+  *as = s;
+  *pair_n = 0;
+  if (s.k == 2 && (s.w == 4 || s.w == 6)) {  // pairs of blocks: a k = 4 code
+    *as = Shape{s.d, 4, s.N * s.N, 2 * s.w, s.P};
+    *pair_n = s.N;
+  }
+  const Kind staged{0, 1, 0, 0};
+  const int kb = as->k / 4, ni = kb > 0 ? s.d / 16 / kb : 0;
+  if (as->k % 4 != 0 || ni < 1 || ni * kb * 16 != s.d || (int64_t)as->N * as->k > 16384) return staged;
+  const int lds = as->N * as->k * 4;
+  if (kb == 1 && as->w == 8) return Kind{8, 1, s.d / 64, lds};
+  if (kb == 1 && as->w == 12) return Kind{12, 1, s.d == 64 ? 2 : 3, lds};
+  if (s.d == 64 && kb == 2 && (as->w == 4 || as->w == 6)) return Kind{as->w, 2, 1, lds};
+  if (s.P < 8 || kb > 4) return staged;
+  for (int q = 0; q < 4; ++q) {  // 8 bytes inside the row that hold the quarter
+    const int bit = q * ni * as->w;
+    const int st = bit / 8 < s.P - 8 ? bit / 8 : s.P - 8;
+    if (bit - 8 * st + ni * as->w > 64) return staged;
+  }
+  return Kind{0, kb, 2, lds};
+}
+
+// Row tiles: 16 RT rows share the gathered codewords; registers hold 64 rows
+// at d = 64 and 32 at d = 128.
+static int tile_rows(int rows, int D) {
+  if (rows <= 16) return 16;
+  if (rows <= 32 || D == 128) return 32;
+  return 64;
+}
+constexpr int kMaxWgs = 512;
+
+struct Layout {
+  int tile, tiles;
+  size_t off_bounds, off_stat, off_top, total;
+};
+static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
+  Layout y{};
+  const int rows = (M > 0 ? M : 1) * G;
+  y.tile = tile_rows(rows, s.d);
+  y.tiles = (rows + y.tile - 1) / y.tile;
+  const int64_t items = n_groups * y.tiles;
+  auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  y.off_bounds = al((size_t)(items + kMaxWgs) * rec_floats(s.d, y.tile / 16) * 4);
+  y.off_stat = al(y.off_bounds + (size_t)items * 8);
+  y.off_top = al(y.off_stat + (M > 0 ? 0 : (size_t)n_groups * rows * 8));
+  y.total = al(y.off_top + kTop * 4);
+  return y;
+}
+
+template <int D, int RT, int W, int KB, int QW, bool WT>
+static hipError_t launch_rows(Args a, int table, hipStream_t st) {
+  a.lds_scratch = table;
+  size_t scratch = (size_t)16 * RT * (D + 4) * 4;  // rotated queries
+  const size_t states = WT ? 0 : (size_t)(kWaves / 2) * 64 * state_regs(D, RT) * 4;
+  const size_t tiles = QW == 0 ? (size_t)kWaves * 2 * kStep * tile_stride(D) : 0;
+  if (states > scratch) scratch = states;
+  if (tiles > scratch) scratch = tiles;
+  const size_t lds = table + scratch;
+  auto kern = rows_kernel<D, RT, W, KB, QW, WT>;
+  if (lds > 65536) {  // above the default dynamic LDS limit
+    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  // as many workgroups as run at once: two per compute unit where registers and LDS allow
+  const int64_t most = (int64_t)a.n_groups * a.tiles * ((a.T_stride + kRun - 1) / kRun);
+  int64_t wgs = RT == 1 && D == 64 && lds <= 78 * 1024 ? kMaxWgs : kMaxWgs / 2;
+  if (wgs > most) wgs = most;
+  hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kThreads), lds, st, a);
+  return hipGetLastError();
+}
+
+template <int D, int RT, bool WT>
+static hipError_t launch_kind(const Args& a, const Kind& x, hipStream_t st) {
+#define FIBQ_SV(WW, KK, QQ) \
+  if (x.w == WW && x.kb == KK && x.qw == QQ) return launch_rows<D, RT, WW, KK, QQ, WT>(a, x.lds, st);
+  if constexpr (D == 64) {
+    FIBQ_SV(8, 1, 1) FIBQ_SV(12, 1, 2) FIBQ_SV(4, 2, 1) FIBQ_SV(6, 2, 1)
+  } else {
+    FIBQ_SV(8, 1, 2) FIBQ_SV(12, 1, 3)
+  }
+  FIBQ_SV(0, 1, 2) FIBQ_SV(0, 2, 2) FIBQ_SV(0, 4, 2) FIBQ_SV(0, 1, 0)
+#undef FIBQ_SV
+  return hipErrorInvalidValue;
+}
+
+template <int D>
+static hipError_t launch_tile(const Args& a, int tile, const Kind& x, hipStream_t st) {
+  if (tile == 16) return launch_kind<D, 1, false>(a, x, st);
+  if (tile == 32) return launch_kind<D, 2, false>(a, x, st);
+  if constexpr (D == 64) return launch_kind<D, 4, false>(a, x, st);
+  return hipErrorInvalidValue;
+}
+
+template <int D>
+static int launch(const ServeAttn& v, hipStream_t st) {
+  const Layout y = make_layout(v.n_groups, v.M, v.G, v.s);
+  unsigned char* ws = static_cast<unsigned char*>(v.ws);
+  Shape as;
+  int pair_n;
+  const Kind x = kind_of(v.s, &as, &pair_n);
+  Args a{};
+  a.q = v.q;
+  a.q_dtype = v.q_dtype;
+  a.kp = v.kp;
+  a.kn = v.kn;
+  a.vp = v.vp;
+  a.vn = v.vn;
+  a.lens = v.lens;
+  a.masks = v.masks;
+  a.mask_stride = v.mask_stride;
+  a.n_groups = (int)v.n_groups;
+  a.M = v.M;
+  a.G = v.G;
+  a.rows = (v.M > 0 ? v.M : 1) * v.G;
+  a.tiles = y.tiles;
+  a.T_stride = v.T_stride;
+  a.k = as.k;
+  a.N = as.N;
+  a.w = as.w;
+  a.P = as.P;
+  a.pair_n = pair_n;
+  a.R = v.R;
+  a.C = v.C;
+  a.qscale = v.scale * 1.4426950408889634f;  // base-2 softmax
+  a.rec = reinterpret_cast<float*>(ws);
+  a.bounds = reinterpret_cast<int32_t*>(ws + y.off_bounds);
+  float* stat = v.acc ? reinterpret_cast<float*>(ws + y.off_stat) : nullptr;
+  float* top = reinterpret_cast<float*>(ws + y.off_top);
+  a.stat = stat;
+  a.top = top;
+  a.acc = v.acc;
+  hipError_t e = hipSuccess;
+  const bool some = v.T_stride > 0;
+  if (some) {
+    if (x.qw == 0) {
+      hipLaunchKernelGGL(top_kernel, dim3(kTop), dim3(256), 0, st, v.C, v.s.N * v.s.k, top);
+      if ((e = hipGetLastError()) != hipSuccess) return (int)e;
+    }
+    if ((e = launch_tile<D>(a, y.tile, x, st)) != hipSuccess) return (int)e;
+  }
+  const int64_t blocks = v.n_groups * ((a.rows + 256 / D - 1) / (256 / D));
+  hipLaunchKernelGGL(merge_kernel<D>, dim3((unsigned)blocks), dim3(256), 0, st, a.rec, a.bounds,
+                     v.lens, v.T_stride, v.M, a.rows, y.tiles, y.tile, v.R, stat, v.out);
+  if ((e = hipGetLastError()) != hipSuccess) return (int)e;
+  if (v.acc && some) return (int)launch_kind<D, 1, true>(a, x, st);
+  return 0;
 }
 
 }  // namespace sv
 
 size_t serve_attn_workspace_bytes(int64_t n_groups, int M, int G, const Shape& s) {
-  return M > 0 ? 0 : (size_t)n_groups * G * 2 * 4;
-}
-
-template <int D>
-static int launch_serve(const ServeAttn& a, hipStream_t st) {
-  const int rows = (a.M > 0 ? a.M : 1) * a.G;
-  const float qscale = a.scale * 1.4426950408889634f;  // base-2 softmax
-  float* stat = a.acc ? static_cast<float*>(a.ws) : nullptr;
-  hipLaunchKernelGGL(sv::rows_kernel<D>, dim3((unsigned)(a.n_groups * rows)), dim3(256), 0, st, a.q,
-                     a.q_dtype, a.kp, a.kn, a.vp, a.vn, a.lens, a.masks, a.mask_stride, a.M, a.G,
-                     a.T_stride, a.s, a.R, a.C, qscale, stat, a.out);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.acc || a.T_stride == 0) return (int)e;
-  hipLaunchKernelGGL(sv::weights_kernel<D>,
-                     dim3((unsigned)((a.T_stride + 255) / 256), (unsigned)a.n_groups), dim3(256),
-                     0, st, a.q, a.q_dtype, a.kp, a.kn, a.lens, a.G, a.T_stride, a.s, a.R, a.C,
-                     qscale, stat, a.acc);
-  return (int)hipGetLastError();
+  return sv::make_layout(n_groups, M, G, s).total;
 }
 
 int launch_serve_attn(const ServeAttn& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return a.s.d == 64 ? launch_serve<64>(a, st) : launch_serve<128>(a, st);
+  return a.s.d == 64 ? sv::launch<64>(a, st) : sv::launch<128>(a, st);
 }
 
 }  // namespace dev
