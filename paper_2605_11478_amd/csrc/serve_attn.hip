@@ -244,6 +244,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
   const int kbit = g16 * NI * w, vbit = (c & 3) * NI * w;
   const int kst = min(kbit >> 3, P - 4 * QD), vst = min(vbit >> 3, P - 4 * QD);
   const int ksh = kbit - 8 * kst, vsh = vbit - 8 * vst;
+  const int ko = c * P + kst, vo = (4 * g16 + (c >> 2)) * P + vst;
   auto quarter = [&](const uint8_t* at, int sh, uint32_t (&d)[QD]) {
     __builtin_memcpy(d, at, 4 * QD);
     if constexpr (QD == 1) {
@@ -259,35 +260,43 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
   auto segment = [&](int len, int rt0, int r0, int take) {
     const int tot = len + a.M;
     const int64_t base = (int64_t)g * a.T_stride;
+    // a unit inside the group is read at wave-uniform addresses plus the lane's
+    // offset; in the last one of a ragged group every token is clamped into it
+    const uint8_t* kpg = a.kp + base * P;
+    const uint8_t* vpg = a.vp + base * P;
+    const uint16_t* kng = a.kn + base;
+    const uint16_t* vng = a.vn + base;
     auto load = [&](int u) -> Unit<QD> {
       Unit<QD> x{};
       const int tb = u * kStep, tm = tot - 1;
-      const uint16_t* kng = a.kn + base;
-      const uint16_t* vng = a.vn + base;
-      const bool whole = tb + kStep <= tot;
+      if (tb + kStep <= tot) {
+        const uint8_t* kb = kpg + (int64_t)tb * P;
+        const uint8_t* vb = vpg + (int64_t)tb * P;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if constexpr (!kStaged) quarter(kb + (uint32_t)(16 * t * P + ko), ksh, x.kq[t]);
+          __builtin_memcpy(&x.nk[2 * t], kng + tb + (uint32_t)(16 * t + 4 * g16), 8);
+          if constexpr (!WT) {
+            if constexpr (!kStaged) quarter(vb + (uint32_t)(16 * t * P + vo), vsh, x.vq[t]);
+            __builtin_memcpy(&x.nv[2 * t], vng + tb + (uint32_t)(16 * t + 4 * g16), 8);
+          }
+        }
+        return x;
+      }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if constexpr (!kStaged) {
-          const int tk = whole ? tb + 16 * t + c : min(tb + 16 * t + c, tm);
-          quarter(a.kp + (base + tk) * P + kst, ksh, x.kq[t]);
-          if constexpr (!WT) {
-            const int tv0 = tb + 16 * t + 4 * g16 + (c >> 2);
-            const int tv = whole ? tv0 : min(tv0, tm);
-            quarter(a.vp + (base + tv) * P + vst, vsh, x.vq[t]);
-          }
+          quarter(kpg + (int64_t)min(tb + 16 * t + c, tm) * P + kst, ksh, x.kq[t]);
+          if constexpr (!WT)
+            quarter(vpg + (int64_t)min(tb + 16 * t + 4 * g16 + (c >> 2), tm) * P + vst, vsh, x.vq[t]);
         }
         const int ts = tb + 16 * t + 4 * g16;
-        if (whole) {
-          __builtin_memcpy(&x.nk[2 * t], kng + ts, 8);
-          if constexpr (!WT) __builtin_memcpy(&x.nv[2 * t], vng + ts, 8);
-        } else {  // (tokens behind the last one: norm 0)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = min(ts + e, tm);
-            const uint32_t in = ts + e <= tm ? 0xFFFFu : 0u;
-            x.nk[2 * t + (e >> 1)] |= (kng[at] & in) << (16 * (e & 1));
-            if constexpr (!WT) x.nv[2 * t + (e >> 1)] |= (vng[at] & in) << (16 * (e & 1));
-          }
+        for (int e = 0; e < 4; ++e) {  // (tokens behind the last one: norm 0)
+          const int at = min(ts + e, tm);
+          const uint32_t in = ts + e <= tm ? 0xFFFFu : 0u;
+          x.nk[2 * t + (e >> 1)] |= (kng[at] & in) << (16 * (e & 1));
+          if constexpr (!WT) x.nv[2 * t + (e >> 1)] |= (vng[at] & in) << (16 * (e & 1));
         }
       }
       return x;
@@ -350,6 +359,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int kap = 0; kap < KS; ++kap) {
+        bh[t][kap] = bl[t][kap] = h8{};  // (rows behind the last one)
         if (t >= live) continue;
         const float* at = qt + (16 * t + c) * QS + 4 * (g16 * Q + 2 * kap);
         uint32_t hi[4], lo[4];
@@ -376,13 +386,6 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       m[0] = a.stat[at] == -INFINITY ? 0.0f : a.stat[at];
       l[0] = c < a.rows && a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
     }
-    uint64_t mask[RT];
-    if constexpr (!WT) {
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-        mask[t] = a.M > 0 ? a.masks[g * a.mask_stride + min(row0 + 16 * t + c, a.rows - 1) / a.G] : 0;
-    }
-
     // staged codes: rows of the unit's tokens into the tile; whether any has a residual
     auto stage = [&](const uint8_t* pay, int tb) -> bool {
       bool any = false;
@@ -425,9 +428,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       return __any(any);
     };
 
-    auto compute = [&](const Unit<QD>& x, int tb) {
+    // one unit; TAIL: it holds drafted tokens or ends behind the last one
+    auto compute = [&](const Unit<QD>& x, int tb, auto tail_tag) {
+      constexpr bool TAIL = decltype(tail_tag)::value;
       bool lo_now = has_lo;  // (uniform) residual rows to add
       if constexpr (kStaged) lo_now = stage(a.kp, tb);
+      const int lo_at = kStaged ? kStep * tile_stride(D) : nrow * 8;
       // two gathered rows per lane of tile t, K-step kap, `d` bytes behind the high parts
       auto krow = [&](int t, int kap, int d) -> h8 {
         if constexpr (kStaged) {
@@ -438,26 +444,92 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
           return h8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
         }
       };
-      const int lo_at = kStaged ? kStep * tile_stride(D) : nrow * 8;
-      h8 ka[2][KS];
+      // ---- scores of all row tiles, 16 tokens at a time
+      f4 s[RT][2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < 2; ++i) {
+        h8 ka[KS];
 #pragma unroll
-        for (int kap = 0; kap < KS; ++kap) ka[t][kap] = krow(t, kap, 0);
-      float nk[8], nv[8];
+        for (int kap = 0; kap < KS; ++kap) ka[kap] = krow(i, kap, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const h2 k2 = __builtin_bit_cast(h2, x.nk[i]), v2 = __builtin_bit_cast(h2, x.nv[i]);
-        nk[2 * i] = (float)k2[0] * ks;
-        nk[2 * i + 1] = (float)k2[1] * ks;
-        nv[2 * i] = (float)v2[0];
-        nv[2 * i + 1] = (float)v2[1];
+        for (int t = 0; t < RT; ++t) s[t][i] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int kap = 0; kap < KS; ++kap) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bl[t][kap], s[t][i], 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bh[t][kap], s[t][i], 0, 0, 0);
+        }
       }
-      if constexpr (!WT) {
-        // the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
-        float top = 0.0f;
+      if (lo_now) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(nv[i]));
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int kap = 0; kap < KS; ++kap) {
+            const h8 kr = krow(i, kap, lo_at);
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+              s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr, bh[t][kap], s[t][i], 0, 0, 0);
+          }
+      }
+      float nk[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1] * ks;
+      uint32_t seen[RT];  // of this lane's tokens (tail units)
+      if constexpr (TAIL) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          uint64_t mask = 0;
+          if (!WT && a.M > 0) mask = a.masks[g * a.mask_stride + min(row0 + 16 * t + c, a.rows - 1) / a.G];
+          seen[t] = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int j = tb + 16 * (i >> 2) + 4 * g16 + (i & 3) - len;
+            if (j < 0 || (j < a.M && (mask >> (j & 63) & 1))) seen[t] |= 1u << i;
+          }
+        }
+      }
+      // scores against the running maxima (an unseen token's norm may be anything)
+      auto against = [&](int t, float ref, float (&p)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = fmaf(s[t][i >> 2][i & 3], nk[i], -ref);
+          if (TAIL) p[i] = seen[t] >> i & 1 ? p[i] : -INFINITY;
+        }
+      };
+      if constexpr (WT) {
+        float p[8];
+        against(0, m[0], p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]) * l[0];
+        // sums over the rows (lanes of a 16-lane row), each step halving the
+        // tokens that a lane keeps: bits 3, 2, 1 of c pick token i's bits 2, 1, 0
+        auto dpp = [](float v, auto ctrl) {
+          return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
+        };
+        const bool b3 = c & 8, b2 = c & 4, b1 = c & 2;
+        float x4[4], x2[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // row_ror:8 swaps lanes c and c ^ 8
+          x4[i] = (b3 ? p[i + 4] : p[i]) + dpp(b3 ? p[i] : p[i + 4], std::integral_constant<int, 0x128>{});
+#pragma unroll
+        for (int i = 0; i < 2; ++i)  // row_half_mirror: lanes c and c ^ 7
+          x2[i] = (b2 ? x4[i + 2] : x4[i]) + dpp(b2 ? x4[i] : x4[i + 2], std::integral_constant<int, 0x141>{});
+        // quad_perm [2, 3, 0, 1] and [1, 0, 3, 2]: lanes c and c ^ 2, c and c ^ 1
+        float x1 = (b1 ? x2[1] : x2[0]) + dpp(b1 ? x2[0] : x2[1], std::integral_constant<int, 0x4E>{});
+        x1 += dpp(x1, std::integral_constant<int, 0xB1>{});
+        const int at = tb + 16 * (b3 ? 1 : 0) + 4 * g16 + (b2 ? 2 : 0) + (b1 ? 1 : 0);
+        if ((c & 1) == 0 && (!TAIL || at < tot)) a.acc[base + at] += x1;
+      } else {
+        // ---- the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
+        float nv[8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          nv[i] = (float)__builtin_bit_cast(h2, x.nv[i >> 1])[i & 1];
+          top = fmaxf(top, fabsf(nv[i]));
+        }
         if (__any(top > vlim)) {
           top = 0.0f;
 #pragma unroll
@@ -478,140 +550,92 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) nv[i] *= vs;
-      }
-      const bool tail = tb + kStep > len;
-      h8 wh[RT], wl[RT];
+        // ---- a score far above its row's maximum, or (not a number or infinite)
+        //      no finite one yet: the maxima move
+        bool over = false;
+        float p[RT][8], most[RT];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        if (t >= live) continue;
-        f4 s[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          s[i] = f4{0, 0, 0, 0};
-#pragma unroll
-          for (int kap = 0; kap < KS; ++kap) {
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[i][kap], bl[t][kap], s[i], 0, 0, 0);
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[i][kap], bh[t][kap], s[i], 0, 0, 0);
-          }
+        for (int t = 0; t < RT; ++t) {
+          against(t, m[t], p[t]);
+          most[t] = fmaxf(fmaxf(fmaxf(p[t][0], p[t][1]), fmaxf(p[t][2], p[t][3])),
+                          fmaxf(fmaxf(p[t][4], p[t][5]), fmaxf(p[t][6], p[t][7])));
+          over |= !(most[t] <= kLag);
         }
-        if (lo_now) {
+        if (__any(over)) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int t = 0; t < RT; ++t) {
+            const bool first = m[t] == -INFINITY;
+            float mh = most[t];
+            if (first) {
+              mh = -INFINITY;
 #pragma unroll
-            for (int kap = 0; kap < KS; ++kap)
-              s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(krow(i, kap, lo_at), bh[t][kap], s[i], 0, 0, 0);
-        }
-        float p[8];
+              for (int i = 0; i < 8; ++i)
+                if (!TAIL || (seen[t] >> i & 1)) mh = fmaxf(mh, s[t][i >> 2][i & 3] * nk[i]);
+            }
+            mh = xmax(xmax(mh, 16), 32);
+            const float m_new = first ? mh : m[t] + fmaxf(mh, 0.0f);
+            const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
+            m[t] = m_new;
+            against(t, m_new == -INFINITY ? 0.0f : m_new, p[t]);  // (scores of -inf have weight 0)
+            l[t] *= f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = fmaf(s[i >> 2][i & 3], nk[i], -m[t]);
-        uint32_t seen = 0xFFu;  // of this lane's tokens (tail units)
-        if (tail) {
+            for (int e = 0; e < 4; ++e) {
+              const float fr = __shfl(f, 4 * g16 + e, 64);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int j = tb + 16 * (i >> 2) + 4 * g16 + (i & 3) - len;
-            bool in = j < 0;
-            if constexpr (!WT) in = in || (j < a.M && (mask[t] >> (j & 63) & 1));
-            if (!in) {
-              p[i] = -INFINITY;
-              seen &= ~(1u << i);
+              for (int mu = 0; mu < VM; ++mu) acc[t][mu][e] *= fr;
             }
           }
         }
-        if constexpr (WT) {
+        // ---- weights in two binary16 parts
+        h8 wh[RT], wl[RT];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]) * l[0];
-          // sums over the rows (lanes of a 16-lane row), each step halving the
-          // tokens that a lane keeps: bits 3, 2, 1 of c pick token i's bits 2, 1, 0
-          auto dpp = [](float v, auto ctrl) {
-            return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
-          };
-          const bool b3 = c & 8, b2 = c & 4, b1 = c & 2;
-          float x4[4], x2[2];
+        for (int t = 0; t < RT; ++t) {
+          uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)  // row_ror:8 swaps lanes c and c ^ 8
-            x4[i] = (b3 ? p[i + 4] : p[i]) + dpp(b3 ? p[i] : p[i + 4], std::integral_constant<int, 0x128>{});
+          for (int i = 0; i < 8; ++i) p[t][i] = __builtin_amdgcn_exp2f(p[t][i]);
 #pragma unroll
-          for (int i = 0; i < 2; ++i)  // row_half_mirror: lanes c and c ^ 7
-            x2[i] = (b2 ? x4[i + 2] : x4[i]) + dpp(b2 ? x4[i] : x4[i + 2], std::integral_constant<int, 0x141>{});
-          // quad_perm [2, 3, 0, 1] and [1, 0, 3, 2]: lanes c and c ^ 2, c and c ^ 1
-          float x1 = (b1 ? x2[1] : x2[0]) + dpp(b1 ? x2[0] : x2[1], std::integral_constant<int, 0x4E>{});
-          x1 += dpp(x1, std::integral_constant<int, 0xB1>{});
-          const int at = tb + 16 * (b3 ? 1 : 0) + 4 * g16 + (b2 ? 2 : 0) + (b1 ? 1 : 0);
-          if ((c & 1) == 0 && at < tot) a.acc[base + at] += x1;
-          continue;
-        }
-        float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])),
-                          fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-        // a score far above the maximum, or (not a number or infinite) no finite one yet
-        if (__any(!(top <= kLag))) {
-          const bool first = m[t] == -INFINITY;
-          float mh = top;
-          if (first) {
-            mh = -INFINITY;
+          for (int i = 0; i < 8; ++i) l[t] += p[t][i];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (seen >> i & 1) mh = fmaxf(mh, s[i >> 2][i & 3] * nk[i]);
+          for (int i = 0; i < 8; ++i) {
+            p[t][i] *= nv[i];
+            if (TAIL) p[t][i] = seen[t] >> i & 1 ? p[t][i] : 0.0f;
           }
-          mh = xmax(xmax(mh, 16), 32);
-          const float m_new = first ? mh : m[t] + fmaxf(mh, 0.0f);
-          const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
-          m[t] = m_new;
-          const float sub = m_new == -INFINITY ? 0.0f : m_new;  // (scores of -inf have weight 0)
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            p[i] = seen >> i & 1 ? fmaf(s[i >> 2][i & 3], nk[i], -sub) : -INFINITY;
-          l[t] *= f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float fr = __shfl(f, 4 * g16 + e, 64);
-#pragma unroll
-            for (int mu = 0; mu < VM; ++mu) acc[t][mu][e] *= fr;
-          }
+          for (int i = 0; i < 4; ++i) split2(p[t][2 * i], p[t][2 * i + 1], &hi[i], &lo[i]);
+          __builtin_memcpy(&wh[t], hi, 16);
+          __builtin_memcpy(&wl[t], lo, 16);
         }
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) l[t] += p[i];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] *= nv[i];
-        if (tail) {  // (an unseen token's norm may be anything)
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (!(seen >> i & 1)) p[i] = 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], &hi[i], &lo[i]);
-        __builtin_memcpy(&wh[t], hi, 16);
-        __builtin_memcpy(&wl[t], lo, 16);
-      }
-      if constexpr (!WT) {
+        // ---- values
         if constexpr (kStaged) lo_now = stage(a.vp, tb);
-#pragma unroll
-        for (int mu = 0; mu < VM; ++mu) {
+        auto vrow = [&](int mu, int d) -> h8 {
           const unsigned char *ra, *rb;
           if constexpr (kStaged) {
-            ra = tile + (4 * g16 + (c >> 2)) * tile_stride(D) + 8 * ((c & 3) * VM + mu);
+            ra = tile + (4 * g16 + (c >> 2)) * tile_stride(D) + 8 * ((c & 3) * VM + mu) + d;
             rb = ra + 16 * tile_stride(D);
           } else {
-            ra = smem + qrow<QD, W, KB>(x.vq[0], mu, w);
-            rb = smem + qrow<QD, W, KB>(x.vq[1], mu, w);
+            ra = smem + qrow<QD, W, KB>(x.vq[0], mu, w) + d;
+            rb = smem + qrow<QD, W, KB>(x.vq[1], mu, w) + d;
           }
           const h4 b0 = tr_read(ra), b1 = tr_read(rb);
-          const h8 bv = h8{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
+          return h8{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
+        };
 #pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            if (t >= live) continue;
+        for (int mu = 0; mu < VM; ++mu) {
+          const h8 bv = vrow(mu, 0);
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
             acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl[t], bv, acc[t][mu], 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
             acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], bv, acc[t][mu], 0, 0, 0);
-          }
-          if (lo_now) {
-            const h4 d0 = tr_read(ra + lo_at), d1 = tr_read(rb + lo_at);
-            const h8 dv = h8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+        }
+        if (lo_now) {
+#pragma unroll
+          for (int mu = 0; mu < VM; ++mu) {
+            const h8 dv = vrow(mu, lo_at);
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-              if (t < live)
-                acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], dv, acc[t][mu], 0, 0, 0);
+              acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], dv, acc[t][mu], 0, 0, 0);
           }
         }
       }
@@ -621,11 +645,17 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       }
     };
 
-    for (; u < u_end; u += kWaves) {
+    const int u_full = min(u_end, len / kStep);  // units of context only
+    for (; u < u_full; u += kWaves) {
       Unit<QD> nxt{};
       if (u + kWaves < u_end) nxt = load(u + kWaves);
-      compute(cur, u * kStep);
+      compute(cur, u * kStep, std::false_type{});
       cur = nxt;
+    }
+#pragma unroll 1
+    for (; u < u_end; u += kWaves) {
+      compute(cur, u * kStep, std::true_type{});
+      if (u + kWaves < u_end) cur = load(u + kWaves);
     }
 
     if constexpr (!WT) {
@@ -638,6 +668,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         for (int mu = 0; mu < VM; ++mu) acc[t][mu] *= vi;
       }
       __syncthreads();  // (staged: the tiles are done with)
+#pragma unroll 1
       for (int h = kWaves / 2; h > 0; h >>= 1) {
         float* st = scratch + (size_t)(wave - (wave >= h ? h : 0)) * 64 * state_regs(D, RT) + lane;
         if (wave >= h && wave < 2 * h) {
@@ -676,6 +707,8 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         // items and workgroups both only grow along the units, so item + workgroup
         // is a different number for every segment
         float* r = a.rec + (item + b) * rec_floats(D, RT);
+        int at = 2 * ROWS + 4 * g16 * D + 4 * (c >> 2) * VM + (c & 3);
+        asm volatile("" : "+v"(at));  // (64 addresses held through the unit loop would spill)
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           if (lane < 16) {
@@ -686,7 +719,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
           for (int mu = 0; mu < VM; ++mu)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              r[2 * ROWS + (16 * t + 4 * g16 + e) * D + 4 * ((c >> 2) * VM + mu) + (c & 3)] = acc[t][mu][e];
+              r[at + (16 * t + e) * D + 4 * mu] = acc[t][mu][e];
         }
         if (lane == 0) {
           if (r0 == 0) a.bounds[2 * item] = b;
