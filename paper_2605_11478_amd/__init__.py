@@ -1,8 +1,8 @@
 """FibQuant random-access KV-cache codec on MI355X (gfx950).
 
 Thin binding over ``libfibq.so`` (declared in ``include/fibq.h``): argument
-marshalling only, by ctypes and, for encode, decode and attention calls on
-device tensors, by the compiled module ``_binding.so``, which the first such
+marshalling only, by ctypes and, for encode, decode, attention and serving calls
+on device tensors, by the compiled module ``_binding.so``, which the first such
 call loads (host functions need neither it nor torch).  Every step of the codec
 runs in the library's HIP kernels; there is no CPU fallback, and a missing
 library or module raises.
@@ -117,8 +117,21 @@ def _bind(L):
     _binding.bind(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in
                     ("fibq_encode", "fibq_decode", "fibq_attn_decode",
                      "fibq_attn_workspace_bytes", "fibq_payload_bytes")), _check)
+    _binding.bind_serving(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in
+                            ("fibq_attn_tree", "fibq_attn_tree_workspace_bytes",
+                             "fibq_attn_decode_accum", "fibq_attn_decode_accum_workspace_bytes",
+                             "fibq_accept_draft", "fibq_evict", "fibq_evict_workspace_bytes")))
     _fast = _binding
     _bound = True
+
+
+def _compiled(t):
+    """The compiled per-call path for calls on device tensors, else None."""
+    if not getattr(t, "is_cuda", False):
+        return None
+    if not _bound:
+        _bind(lib())
+    return _fast
 
 
 def _raw_stream():
@@ -555,6 +568,12 @@ def attn_tree(q, k_payload, k_norms, v_payload, v_norms, lens, masks, k, N, R, C
     [0, T_stride - M] are NaN.  ``workspace`` as for ``attn_decode``
     (``attn_tree_workspace_bytes``).
     """
+    fast = _compiled(q)
+    if fast is not None:
+        done = fast.attn_tree(q, k_payload, k_norms, v_payload, v_norms, lens, masks, k, N, R, C,
+                              scale, workspace, out, _raw_stream(), _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
     torch = _torch()
     _want(q, "q", (torch.float32, torch.float16, torch.bfloat16), (None, None, None, None))
     n_groups, M, G, d = q.shape
@@ -588,6 +607,12 @@ def accept_draft(k_payload, k_norms, v_payload, v_norms, lens, M, path, n_acc, n
     -> new_lens = lens + n_acc (pass ``new_lens=lens`` to update it in place);
     -1 for a group with a bad length, count or path, whose rows stay.
     """
+    fast = _compiled(lens)
+    if fast is not None:
+        done = fast.accept(k_payload, k_norms, v_payload, v_norms, lens, M, path, n_acc, new_lens,
+                           _raw_stream(), _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
     torch = _torch()
     n_groups, T_stride, P = _check_cache(k_payload, k_norms, v_payload, v_norms, lens)
     _want(path, "path", (torch.int32,), (n_groups, None))
@@ -614,6 +639,13 @@ def attn_decode_accum(q, k_payload, k_norms, v_payload, v_norms, lens, acc, k, N
     q [n_groups, G, d] -> out float32 [n_groups, G, d]; a length outside
     [0, T_stride] gives NaN rows and leaves the group's acc.
     """
+    fast = _compiled(q)
+    if fast is not None:
+        done = fast.attn_accum(q, k_payload, k_norms, v_payload, v_norms, lens, acc, k, N, R, C,
+                               scale, workspace, out, _raw_stream(),
+                               _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
     torch = _torch()
     _want(q, "q", (torch.float32, torch.float16, torch.bfloat16), (None, None, None))
     n_groups, G, d = q.shape
@@ -652,6 +684,12 @@ def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=N
     behind the new length are not written.  ``out``: seven such tensors, none
     sharing memory with an input.
     """
+    fast = _compiled(lens)
+    if fast is not None and out is not None:
+        done = fast.evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent,
+                          tuple(out), workspace, _raw_stream(), _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
     torch = _torch()
     n_groups, T_stride, P = _check_cache(k_payload, k_norms, v_payload, v_norms, lens)
     _want(acc, "acc", (torch.float32,), (n_groups, T_stride))

@@ -462,7 +462,8 @@ int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t*
                uint16_t* v_norms_out, float* acc_out, int32_t* new_lens, int32_t* index,
                void* workspace, size_t workspace_bytes, void* stream) {
   if (!serve_sizes(n_groups, T_stride) || P < 1 || P > 256 || keep < 1 || keep >= (1LL << 30) ||
-      recent < 0 || recent > keep || T_out < keep || T_out >= (1LL << 30))
+      recent < 0 || recent > keep || T_out < keep || T_out >= (1LL << 30) ||
+      n_groups * keep >= (1LL << 31))
     return FIBQ_EINVAL;
   if (n_groups == 0) return FIBQ_OK;
   if (!lens || !k_payload_out || !k_norms_out || !v_payload_out || !v_norms_out || !acc_out ||
