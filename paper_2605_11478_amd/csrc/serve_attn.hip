@@ -11,15 +11,15 @@
 // binary16 does not hold adds its residual rows' products.  Statistics and sums
 // are float32.
 //
-// rows_kernel.  An item is (group, tile of 16 RT query rows); its work is cut
-// into units of 32 tokens.  The units of all items, in runs of 8 (one per
-// wavefront), are split into equal contiguous ranges, one per workgroup; the
-// lengths are on the device, so every workgroup finds its range from them.  For
-// each item that its range meets, a workgroup rotates the tile's queries, keeps
-// them in registers as operands, goes over its units, combines its wavefronts'
-// states in LDS and leaves one record (m, l, acc) in rotated space.  Per unit a
-// wavefront gathers the keys' and the values' codewords once for all RT row
-// tiles:
+// An item is (group, tile of 16 RT query rows); its work is cut into units of 32
+// tokens.  The units of all items, in runs of 8 (one per wavefront of a
+// workgroup), are split into equal contiguous ranges, one per workgroup.
+// prep_kernel  rotates every item's queries and writes them as operands; one of
+//   its blocks finds the ranges from the lengths, which are on the device.
+// rows_kernel  goes over a range.  For each item that it meets, a workgroup keeps
+//   the queries in registers, goes over the units, combines its wavefronts' states
+//   in LDS and leaves one record (m, l, acc) in rotated space.  Per unit a
+//   wavefront gathers the keys' and the values' codewords once for all row tiles:
 //   scores  S[t][r] = K_hat[t][:] . q~[r][:]  (v_mfma_f32_16x16x32_f16, A = two
 //           gathered 4-dim codeword rows per lane, B = the queries' high, then
 //           low parts): lane l holds row l % 16 and tokens 4 (l / 16) + e of
@@ -27,6 +27,10 @@
 //   values  acc[r][dims] += W[r][t] V_hat[t][dims]: those are the lane's K
 //           slots of the A operand, so the weights need no exchange; B comes
 //           from transposing LDS reads of codeword rows.
+//   Up to 8 rows ("packed") share a product between their parts: columns h and
+//   h + 8 of B are row h's high and low part, summed by one exchange in which
+//   lane h keeps the first tile's tokens and lane h + 8 the second's; rows h and
+//   h + 8 of the weights are row h's parts (the low one times 2^11).
 // merge_kernel combines an item's records by log-sum-exp and applies Pi^T.
 #include <hip/hip_runtime.h>
 
@@ -49,6 +53,12 @@ constexpr int kTop = 64;               // partial maxima of a codebook
 constexpr float kLag = 8.0f;           // a maximum moves when a score exceeds it by this (log2)
 constexpr float kCs = 4096.0f;         // scale of the codebook's binary16 rows
 
+struct Start {  // of a workgroup's range: a group, runs before it, runs in all
+  int32_t g;
+  uint32_t pad;
+  uint64_t off, count;
+};
+
 struct Args {
   const void* q;
   int q_dtype;
@@ -65,9 +75,12 @@ struct Args {
   const float* R;
   const float* C;
   float qscale;
+  h8* ops;            // the items' query operands, and their divisors
+  float* qs;
+  Start* start;       // of every workgroup
   float* rec;
   int32_t* bounds;    // first and last workgroup of every item
-  const float* top;   // kTop partial maxima of |C| (staged codes)
+  float* top;         // kTop partial maxima of |C| (staged codes)
   const float* stat;  // weights pass: m, l of every row
   float* acc;         // weights pass
   int lds_scratch;
@@ -76,6 +89,8 @@ struct Args {
 __host__ __device__ constexpr int rec_floats(int D, int RT) { return 16 * RT * (D + 2); }
 constexpr int tile_stride(int D) { return 2 * D + 16; }  // bytes of a staged row: spreads the banks
 constexpr int state_regs(int D, int RT) { return RT * (D / 16) * 4 + 2 * RT; }
+constexpr int kReg = 68;  // floats between a state's registers in LDS: spreads the banks
+constexpr int state_floats(int D, int RT) { return state_regs(D, RT) * kReg; }
 
 // runs of units of a group; none for a bad length
 __device__ __forceinline__ int runs_of(const Args& a, int g) {
@@ -100,81 +115,197 @@ __device__ __forceinline__ f4 load4(const void* q, int64_t at) {
   return f4{to_float(w[0]), to_float(w[1]), to_float(w[2]), to_float(w[3])};
 }
 
+// One block per item, then one that writes the ranges of `wgs` workgroups, then
+// (staged codes) kTop that write partial maxima of the codebook.
+//
+// The rotation runs on v_mfma_f32_16x16x4_f32 (float32 products and sums; K slot
+// kk of lane group gq is column D / 4 gq + kk).  Operands are at the power of two
+// that takes the item's largest finite entry to [2^13, 2^14), so that the low
+// parts are normal numbers.
+template <int D, int RT, bool PK>
+__global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
+  constexpr int KS = D / 32, KQ = D / 4, Q = D / 16;
+  constexpr int ROWS = 16 * RT, QS = D + 4;
+  __shared__ __align__(16) float qt[ROWS * QS];
+  __shared__ uint64_t sums[256];
+  __shared__ float red[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int items = a.n_groups * a.tiles;
+  if ((int)blockIdx.x > items) {  // a part of the codebook's largest entry
+    float t = 0.0f;
+    for (int i = (blockIdx.x - items - 1) * 256 + tid; i < a.N * a.k; i += kTop * 256)
+      t = fmaxf(t, fabsf(a.C[i]));
+    t = wave_max_dpp(t);
+    if (lane == 0) red[wave] = t;
+    __syncthreads();
+    if (tid == 0) a.top[blockIdx.x - items - 1] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    return;
+  }
+  if ((int)blockIdx.x == items) {
+    const int per = (a.n_groups + 255) / 256;
+    uint64_t mine = 0;
+    for (int i = 0; i < per; ++i) {
+      const int g = tid * per + i;
+      if (g < a.n_groups) mine += runs_of(a, g);
+    }
+    mine *= a.tiles;
+    uint64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    uint64_t all = 0, add = 0;
+    for (int i = 0; i < 4; ++i) {
+      if (i < wave) add += sums[i];
+      all += sums[i];
+    }
+    __syncthreads();
+    sums[tid] = upto + add;  // runs up to and with this thread's groups
+    __syncthreads();
+    const uint64_t each = all >> 32 ? all / wgs : (uint32_t)all / (uint32_t)wgs;
+    const uint32_t rest = (uint32_t)(all - each * wgs);
+    for (int b = tid; b < wgs; b += 256) {
+      const uint64_t from = b * each + min((uint32_t)b, rest);
+      Start s{0, 0, 0, each + ((uint32_t)b < rest)};
+      if (s.count > 0) {
+        int t = 0;  // the first thread whose groups reach beyond `from`
+#pragma unroll
+        for (int h = 128; h > 0; h >>= 1)
+          if (sums[t + h - 1] <= from) t += h;
+        uint64_t off = from - (t > 0 ? sums[t - 1] : 0);
+        int g = t * per;
+        for (;; ++g) {  // (ends: the thread's groups hold `from`)
+          const uint64_t v = (uint64_t)runs_of(a, g) * a.tiles;
+          if (off < v) break;
+          off -= v;
+        }
+        s.g = g;
+        s.off = off;
+      }
+      a.start[b] = s;
+    }
+    return;
+  }
+  const int64_t g = blockIdx.x / a.tiles;
+  const int row0 = (int)(blockIdx.x % a.tiles) * ROWS;
+  if (runs_of(a, (int)g) == 0) return;
+  const int c = lane & 15, g16 = lane >> 4;
+  const int live = (min(ROWS, a.rows - row0) + 15) / 16;
+  float top = 0.0f;
+  for (int it = wave; it < (D / 16) * live; it += 4) {
+    const int dt = it % (D / 16), t = it / (D / 16);
+    const int row = row0 + 16 * t + c;
+    f4 pa[KQ / 4], pb[KQ / 4] = {};
+#pragma unroll
+    for (int p = 0; p < KQ / 4; ++p)
+      __builtin_memcpy(&pa[p], a.R + (16 * dt + c) * D + KQ * g16 + 4 * p, 16);
+    if (row < a.rows) {
+      const int64_t at = (g * a.rows + row) * D + KQ * g16;
+#pragma unroll
+      for (int p = 0; p < KQ / 4; ++p)
+        pb[p] = a.q_dtype == FIBQ_F32   ? load4<float>(a.q, at + 4 * p)
+                : a.q_dtype == FIBQ_F16 ? load4<f16_t>(a.q, at + 4 * p)
+                                        : load4<bf16_t>(a.q, at + 4 * p);
+    }
+    f4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int p = 0; p < KQ / 4; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(pa[p][e], pb[p][e], s, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[e] *= a.qscale;
+      top = fmaxf(top, fabsf(s[e]) < INFINITY ? fabsf(s[e]) : 0.0f);
+    }
+    *reinterpret_cast<f4*>(qt + (16 * t + c) * QS + 16 * dt + 4 * g16) = s;
+  }
+  top = wave_max_dpp(top);
+  if (lane == 0) red[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  float qs = 1.0f, qi = 1.0f;
+  if (top > 0.0f) {
+    int e2 = 0;
+    frexpf(top, &e2);
+    e2 = max(e2 - 14, -100);
+    qs = ldexpf(1.0f, e2);
+    qi = ldexpf(1.0f, -e2);
+  }
+  if (tid == 0) a.qs[blockIdx.x] = qs;
+  // B operand of K-step kap: lane l holds column l % 16 (PK: row l % 8, its high
+  // part below 8, else its low part), K slots = dims 4 (l / 16 Q + 2 kap) .. + 7
+  h8* to = a.ops + (int64_t)blockIdx.x * RT * KS * (PK ? 1 : 2) * 64;
+  for (int x = tid; x < RT * KS * 64; x += 256) {
+    const int l = x & 63, kap = (x >> 6) % KS, t = (x >> 6) / KS;
+    const int r = 16 * t + (PK ? l & 7 : l & 15);
+    uint32_t hi[4] = {}, lo[4] = {};
+    if (row0 + r < a.rows) {
+      const float* at = qt + r * QS + 4 * ((l >> 4) * Q + 2 * kap);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) split2(at[2 * i] * qi, at[2 * i + 1] * qi, &hi[i], &lo[i]);
+    }
+    if constexpr (PK) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) hi[i] = (l & 8) ? lo[i] : hi[i];
+      __builtin_memcpy(&to[kap * 64 + l], hi, 16);
+    } else {
+      __builtin_memcpy(&to[(t * KS + kap) * 128 + l], hi, 16);
+      __builtin_memcpy(&to[(t * KS + kap) * 128 + 64 + l], lo, 16);
+    }
+  }
+}
+
+// Barrier for data in LDS: loads from global memory stay in flight across it
+// (the fence of __syncthreads waits for them).
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // One lane's loads of a unit: a payload quarter of the token whose K row it
 // gathers in each tile, one of the token whose V rows it addresses, and the
-// norms of its eight softmax tokens (binary16 pairs).
-template <int QW>
+// norms of its softmax tokens (binary16 pairs).
+template <int QW, int NE>
 struct Unit {
   uint32_t kq[2][QW], vq[2][QW];
-  uint32_t nk[4], nv[4];
+  uint32_t nk[NE / 2], nv[NE / 2];
 };
 
 // W > 0: compile-time index width, W = 0: at run time; KB: 4-dim rows per
-// codeword; QW: dwords of a payload quarter, 0 for staged codes (below).
-// WT: the weights pass (scores only, added to acc).
+// codeword; QW: dwords of a payload quarter, 0 for staged codes (below); PK:
+// packed rows.  WT: the weights pass (scores only, added to acc).
 //
 // Staged codes (QW = 0) are those whose codewords cannot be addressed as 4-dim
 // rows of an LDS table (k = 1, most of k = 2, quarters of a payload that share
 // a codeword, tables above 64 KB): each wavefront writes the decoded rows of
 // its unit, keys and then values, into a tile of its own and reads the operands
 // from there.
-template <int D, int RT, int W, int KB, int QW, bool WT>
+template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
 __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_kernel(const Args a) {
   constexpr int NB = D / 4, Q = NB / 4;  // 4-dim rows, of them per quarter
-  constexpr int KS = D / 32, VM = D / 16, KQ = D / 4;
-  constexpr int ROWS = 16 * RT, QS = D + 4;  // (floats between rows of the rotated queries)
+  constexpr int KS = D / 32, VM = D / 16;
+  constexpr int ROWS = 16 * RT;
+  constexpr int NE = PK ? 4 : 8;         // softmax tokens of a lane
   constexpr bool kStaged = QW == 0;
   constexpr int QD = kStaged ? 1 : QW;
+  static_assert(!PK || RT == 1, "packed rows are one tile");
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ uint64_t wsum[kWaves];
-  __shared__ uint64_t start[2];
   __shared__ float red[kWaves];
   __shared__ int redi[kWaves];
+  __shared__ float fac[4][ROWS];  // the states' factors in a record, and the rows' m, l
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g16 = lane >> 4, c = lane & 15;
+  const int g16 = lane >> 4, c = lane & 15, hr = PK ? c & 7 : c;
   const int w = W > 0 ? W : a.w;
   const int P = a.P;
-
-  // ---- this workgroup's range of runs
-  const int per = (a.n_groups + kThreads - 1) / kThreads;
-  uint64_t mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int g = tid * per + i;
-    if (g < a.n_groups) mine += runs_of(a, g);
-  }
-  mine *= a.tiles;
-  uint64_t upto = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up(upto, o, 64);
-    if (lane >= o) upto += y;
-  }
-  if (lane == 63) wsum[wave] = upto;
-  __syncthreads();
-  uint64_t all = 0, before = upto - mine;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < wave) before += wsum[i];
-    all += wsum[i];
-  }
-  const uint32_t nwg = gridDim.x, b = blockIdx.x;
-  const uint64_t each = all >> 32 ? all / nwg : (uint32_t)all / nwg;
-  const uint32_t rest = (uint32_t)(all - each * nwg);
-  const uint64_t from = b * each + min(b, rest);
-  uint64_t left = each + (b < rest);
+  const uint32_t b = blockIdx.x;
+  const Start from = a.start[b];
+  uint64_t left = from.count, off = from.off;
+  int g = from.g;
   if (left == 0) return;
-  if (from >= before && from < before + mine) {
-    uint64_t off = from - before;
-    int g = tid * per;
-    for (;; ++g) {
-      const uint64_t v = (uint64_t)runs_of(a, g) * a.tiles;
-      if (off < v) break;
-      off -= v;
-    }
-    start[0] = g;
-    start[1] = off;
-  }
 
   // ---- the codebook's binary16 rows times cs (pairs: of the pair codebook) and
   //      their residuals.  Entries of unit vectors' blocks are at most 1; at
@@ -192,48 +323,37 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
     ci = ldexpf(1.0f, -e2);
     return true;
   };
-  if constexpr (kStaged) {
-    pick_scale(wave_max_dpp(a.top[lane]));
-    __syncthreads();
-  } else {
-#pragma unroll 1
-    for (bool again = false;; again = true) {
-      bool lo_any = false;
-      float top = 0.0f;
-      for (int i = tid; i < nrow; i += kThreads) {
-        float cv[4];
-        if (a.pair_n > 0) {
-          __builtin_memcpy(cv, a.C + 2 * (i % a.pair_n), 8);
-          __builtin_memcpy(cv + 2, a.C + 2 * (i / a.pair_n), 8);
-        } else {
-          __builtin_memcpy(cv, a.C + (size_t)i * 4, 16);
-        }
-        h4 hi, lo;
+  auto table = [&]() {
+    bool lo_any = false;
+    float top = 0.0f;
+    for (int i = tid; i < nrow; i += kThreads) {
+      float cv[4];
+      if (a.pair_n > 0) {
+        __builtin_memcpy(cv, a.C + 2 * (i % a.pair_n), 8);
+        __builtin_memcpy(cv + 2, a.C + 2 * (i / a.pair_n), 8);
+      } else {
+        __builtin_memcpy(cv, a.C + (size_t)i * 4, 16);
+      }
+      h4 hi, lo;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          hi[e] = (_Float16)(cv[e] * cs);
-          lo[e] = (_Float16)fmaf(cv[e], cs, -(float)hi[e]);
-          lo_any |= (float)lo[e] != 0.0f;
-          top = fmaxf(top, fabsf(cv[e]));
-        }
-        reinterpret_cast<h4*>(smem)[i] = hi;
-        reinterpret_cast<h4*>(smem)[nrow + i] = lo;
+      for (int e = 0; e < 4; ++e) {
+        hi[e] = (_Float16)(cv[e] * cs);
+        lo[e] = (_Float16)fmaf(cv[e], cs, -(float)hi[e]);
+        lo_any |= (float)lo[e] != 0.0f;
+        top = fmaxf(top, fabsf(cv[e]));
       }
-      top = wave_max_dpp(top);
-      lo_any = __any(lo_any);
-      if (lane == 0) {
-        red[wave] = top;
-        redi[wave] = lo_any;
-      }
-      __syncthreads();
-      has_lo = __any(lane < kWaves && redi[lane & (kWaves - 1)] != 0);
-      top = wave_max_dpp(red[lane & (kWaves - 1)]);
-      if (again || !pick_scale(top)) break;
-      __syncthreads();  // (red is written again)
+      reinterpret_cast<h4*>(smem)[i] = hi;
+      reinterpret_cast<h4*>(smem)[nrow + i] = lo;
     }
-  }
-  int g = (int)start[0];
-  uint64_t off = start[1];
+    top = wave_max_dpp(top);
+    lo_any = __any(lo_any);
+    if (lane == 0) {
+      red[wave] = top;
+      redi[wave] = lo_any;
+    }
+  };
+  if constexpr (kStaged) pick_scale(wave_max_dpp(a.top[lane]));
+  else table();
 
   float* scratch = reinterpret_cast<float*>(smem + a.lds_scratch);
   // (staged: a tile of high parts, then of residuals, for each wavefront)
@@ -255,19 +375,22 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       d[1] = (uint32_t)(u >> 32);
     }
   };
+  // token i of the lane's softmax tokens, in the unit
+  const int tok0 = 4 * g16 + (PK ? 2 * (c & 8) : 0);
+  auto token = [&](int i) { return tok0 + 16 * (i >> 2) + (i & 3); };
 
   // ---- one item, runs r0 .. r0 + take - 1
-  auto segment = [&](int len, int rt0, int r0, int take) {
+  auto segment = [&](int len, int rt0, int r0, int take, bool first) {
     const int tot = len + a.M;
-    const int64_t base = (int64_t)g * a.T_stride;
+    const int64_t base = (int64_t)g * a.T_stride, item = (int64_t)g * a.tiles + rt0;
     // a unit inside the group is read at wave-uniform addresses plus the lane's
     // offset; in the last one of a ragged group every token is clamped into it
     const uint8_t* kpg = a.kp + base * P;
     const uint8_t* vpg = a.vp + base * P;
     const uint16_t* kng = a.kn + base;
     const uint16_t* vng = a.vn + base;
-    auto load = [&](int u) -> Unit<QD> {
-      Unit<QD> x{};
+    auto load = [&](int u) -> Unit<QD, NE> {
+      Unit<QD, NE> x{};
       const int tb = u * kStep, tm = tot - 1;
       if (tb + kStep <= tot) {
         const uint8_t* kb = kpg + (int64_t)tb * P;
@@ -275,100 +398,59 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           if constexpr (!kStaged) quarter(kb + (uint32_t)(16 * t * P + ko), ksh, x.kq[t]);
-          __builtin_memcpy(&x.nk[2 * t], kng + tb + (uint32_t)(16 * t + 4 * g16), 8);
-          if constexpr (!WT) {
-            if constexpr (!kStaged) quarter(vb + (uint32_t)(16 * t * P + vo), vsh, x.vq[t]);
-            __builtin_memcpy(&x.nv[2 * t], vng + tb + (uint32_t)(16 * t + 4 * g16), 8);
-          }
+          if constexpr (!kStaged && !WT) quarter(vb + (uint32_t)(16 * t * P + vo), vsh, x.vq[t]);
+        }
+#pragma unroll
+        for (int i = 0; i < NE; i += 4) {
+          __builtin_memcpy(&x.nk[i / 2], kng + tb + (uint32_t)(tok0 + 4 * i), 8);
+          if constexpr (!WT) __builtin_memcpy(&x.nv[i / 2], vng + tb + (uint32_t)(tok0 + 4 * i), 8);
         }
         return x;
       }
+      if constexpr (!kStaged) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if constexpr (!kStaged) {
+        for (int t = 0; t < 2; ++t) {
           quarter(kpg + (int64_t)min(tb + 16 * t + c, tm) * P + kst, ksh, x.kq[t]);
           if constexpr (!WT)
             quarter(vpg + (int64_t)min(tb + 16 * t + 4 * g16 + (c >> 2), tm) * P + vst, vsh, x.vq[t]);
         }
-        const int ts = tb + 16 * t + 4 * g16;
+      }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {  // (tokens behind the last one: norm 0)
-          const int at = min(ts + e, tm);
-          const uint32_t in = ts + e <= tm ? 0xFFFFu : 0u;
-          x.nk[2 * t + (e >> 1)] |= (kng[at] & in) << (16 * (e & 1));
-          if constexpr (!WT) x.nv[2 * t + (e >> 1)] |= (vng[at] & in) << (16 * (e & 1));
-        }
+      for (int i = 0; i < NE; ++i) {  // (tokens behind the last one: norm 0)
+        const int at = min(tb + token(i), tm);
+        const uint32_t in = tb + token(i) <= tm ? 0xFFFFu : 0u;
+        x.nk[i >> 1] |= (kng[at] & in) << (16 * (i & 1));
+        if constexpr (!WT) x.nv[i >> 1] |= (vng[at] & in) << (16 * (i & 1));
       }
       return x;
     };
     const int u_end = min((r0 + take) * kWaves, (tot + kStep - 1) / kStep);
     int u = r0 * kWaves + wave;
-    Unit<QD> cur{};
-    if (u < u_end) cur = load(u);  // goes out before the queries are built
+    Unit<QD, NE> cur{};
+    if (u < u_end) cur = load(u);
 
-    // ---- the tile's queries: rotated on v_mfma_f32_16x16x4_f32 (float32 products
-    //      and sums; K slot kk of lane group gq is column KQ gq + kk), then as
-    //      operands at the power of two that takes the largest finite entry to
-    //      [2^13, 2^14), so that the low parts are normal numbers
-    const int row0 = rt0 * ROWS, live = (min(ROWS, a.rows - row0) + 15) / 16;
-    float* qt = scratch;
-    __syncthreads();  // (the scratch is free)
-    float top = 0.0f;
-    for (int it = wave; it < (D / 16) * live; it += kWaves) {
-      const int dt = it % (D / 16), t = it / (D / 16);
-      const int row = row0 + 16 * t + c;
-      f4 pa[KQ / 4], pb[KQ / 4] = {};
-#pragma unroll
-      for (int p = 0; p < KQ / 4; ++p)
-        __builtin_memcpy(&pa[p], a.R + (16 * dt + c) * D + KQ * g16 + 4 * p, 16);
-      if (row < a.rows) {
-        const int64_t at = ((int64_t)g * a.rows + row) * D + KQ * g16;
-#pragma unroll
-        for (int p = 0; p < KQ / 4; ++p)
-          pb[p] = a.q_dtype == FIBQ_F32   ? load4<float>(a.q, at + 4 * p)
-                  : a.q_dtype == FIBQ_F16 ? load4<f16_t>(a.q, at + 4 * p)
-                                          : load4<bf16_t>(a.q, at + 4 * p);
-      }
-      f4 s = {0, 0, 0, 0};
-#pragma unroll
-      for (int p = 0; p < KQ / 4; ++p)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(pa[p][e], pb[p][e], s, 0, 0, 0);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[e] *= a.qscale;
-        top = fmaxf(top, fabsf(s[e]) < INFINITY ? fabsf(s[e]) : 0.0f);
-      }
-      *reinterpret_cast<f4*>(qt + (16 * t + c) * QS + 16 * dt + 4 * g16) = s;
-    }
-    top = wave_max_dpp(top);
-    if (lane == 0) red[wave] = top;
-    __syncthreads();
-    top = wave_max_dpp(red[lane & (kWaves - 1)]);
-    float qs = 1.0f, qi = 1.0f;
-    if (top > 0.0f) {
-      int e2 = 0;
-      frexpf(top, &e2);
-      e2 = max(e2 - 14, -100);
-      qs = ldexpf(1.0f, e2);
-      qi = ldexpf(1.0f, -e2);
-    }
-    h8 bh[RT][KS], bl[RT][KS];
+    // ---- the tile's queries
+    const int row0 = rt0 * ROWS;
+    h8 bh[RT][KS], bl[PK ? 1 : RT][PK ? 1 : KS];
+    const h8* op = a.ops + item * (RT * KS * (PK ? 1 : 2) * 64) + lane;
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int kap = 0; kap < KS; ++kap) {
-        bh[t][kap] = bl[t][kap] = h8{};  // (rows behind the last one)
-        if (t >= live) continue;
-        const float* at = qt + (16 * t + c) * QS + 4 * (g16 * Q + 2 * kap);
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split2(at[2 * i] * qi, at[2 * i + 1] * qi, &hi[i], &lo[i]);
-        __builtin_memcpy(&bh[t][kap], hi, 16);
-        __builtin_memcpy(&bl[t][kap], lo, 16);
+        bh[t][kap] = op[(t * KS + kap) * (PK ? 64 : 128)];
+        if constexpr (!PK) bl[t][kap] = op[(t * KS + kap) * 128 + 64];
       }
-    if constexpr (kStaged) __syncthreads();  // (tiles overwrite qt)
+    const float qs = a.qs[item];
+    if (!kStaged && first) {  // the table is whole; is its scale right?
+      lds_barrier();
+      const float top = wave_max_dpp(red[lane & (kWaves - 1)]);
+      if (pick_scale(top)) {
+        lds_barrier();  // (red is written again)
+        table();
+        lds_barrier();
+      }
+      has_lo = __any(lane < kWaves && redi[lane & (kWaves - 1)] != 0);
+    }
     const float ks = qs * ci;  // scores: products times nu_K times this, in log2 units
 
     f4 acc[RT][VM];
@@ -382,10 +464,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       for (int mu = 0; mu < VM; ++mu) acc[t][mu] = f4{0, 0, 0, 0};
     }
     if constexpr (WT) {  // this row's statistics
-      const int64_t at = ((int64_t)g * a.rows + min(c, a.rows - 1)) * 2;
+      const int64_t at = ((int64_t)g * a.rows + min(hr, a.rows - 1)) * 2;
       m[0] = a.stat[at] == -INFINITY ? 0.0f : a.stat[at];
-      l[0] = c < a.rows && a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
+      l[0] = hr < a.rows && a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
     }
+
     // staged codes: rows of the unit's tokens into the tile; whether any has a residual
     auto stage = [&](const uint8_t* pay, int tb) -> bool {
       bool any = false;
@@ -429,7 +512,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
     };
 
     // one unit; TAIL: it holds drafted tokens or ends behind the last one
-    auto compute = [&](const Unit<QD>& x, int tb, auto tail_tag) {
+    auto compute = [&](const Unit<QD, NE>& x, int tb, auto tail_tag) {
       constexpr bool TAIL = decltype(tail_tag)::value;
       bool lo_now = has_lo;  // (uniform) residual rows to add
       if constexpr (kStaged) lo_now = stage(a.kp, tb);
@@ -455,9 +538,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         for (int t = 0; t < RT; ++t) s[t][i] = f4{0, 0, 0, 0};
 #pragma unroll
         for (int kap = 0; kap < KS; ++kap) {
+          if constexpr (!PK) {
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bl[t][kap], s[t][i], 0, 0, 0);
+            for (int t = 0; t < RT; ++t)
+              s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bl[t][kap], s[t][i], 0, 0, 0);
+          }
 #pragma unroll
           for (int t = 0; t < RT; ++t)
             s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bh[t][kap], s[t][i], 0, 0, 0);
@@ -474,36 +559,47 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
               s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr, bh[t][kap], s[t][i], 0, 0, 0);
           }
       }
-      float nk[8];
+      auto ror8 = [](float v) {  // lanes c and c ^ 8 of a 16-lane row
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
+      };
+      if constexpr (PK) {  // high + low parts; lane h: tile 0, lane h + 8: tile 1
 #pragma unroll
-      for (int i = 0; i < 8; ++i) nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1] * ks;
+        for (int e = 0; e < 4; ++e) {
+          const float own = (c & 8) ? s[0][1][e] : s[0][0][e];
+          const float other = (c & 8) ? s[0][0][e] : s[0][1][e];
+          s[0][0][e] = own + ror8(other);
+        }
+      }
+      float nk[NE];
+#pragma unroll
+      for (int i = 0; i < NE; ++i) nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1] * ks;
       uint32_t seen[RT];  // of this lane's tokens (tail units)
       if constexpr (TAIL) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           uint64_t mask = 0;
-          if (!WT && a.M > 0) mask = a.masks[g * a.mask_stride + min(row0 + 16 * t + c, a.rows - 1) / a.G];
+          if (!WT && a.M > 0) mask = a.masks[g * a.mask_stride + min(row0 + 16 * t + hr, a.rows - 1) / a.G];
           seen[t] = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int j = tb + 16 * (i >> 2) + 4 * g16 + (i & 3) - len;
+          for (int i = 0; i < NE; ++i) {
+            const int j = tb + token(i) - len;
             if (j < 0 || (j < a.M && (mask >> (j & 63) & 1))) seen[t] |= 1u << i;
           }
         }
       }
       // scores against the running maxima (an unseen token's norm may be anything)
-      auto against = [&](int t, float ref, float (&p)[8]) {
+      auto against = [&](int t, float ref, float (&p)[NE]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < NE; ++i) {
           p[i] = fmaf(s[t][i >> 2][i & 3], nk[i], -ref);
           if (TAIL) p[i] = seen[t] >> i & 1 ? p[i] : -INFINITY;
         }
       };
       if constexpr (WT) {
-        float p[8];
+        float p[NE];
         against(0, m[0], p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]) * l[0];
+        for (int i = 0; i < NE; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]) * l[0];
         // sums over the rows (lanes of a 16-lane row), each step halving the
         // tokens that a lane keeps: bits 3, 2, 1 of c pick token i's bits 2, 1, 0
         auto dpp = [](float v, auto ctrl) {
@@ -512,8 +608,10 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         const bool b3 = c & 8, b2 = c & 4, b1 = c & 2;
         float x4[4], x2[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)  // row_ror:8 swaps lanes c and c ^ 8
-          x4[i] = (b3 ? p[i + 4] : p[i]) + dpp(b3 ? p[i] : p[i + 4], std::integral_constant<int, 0x128>{});
+        for (int i = 0; i < 4; ++i) {  // row_ror:8 swaps lanes c and c ^ 8 (packed: those are two tiles)
+          if constexpr (PK) x4[i] = p[i];
+          else x4[i] = (b3 ? p[i + 4] : p[i]) + ror8(b3 ? p[i] : p[i + 4]);
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i)  // row_half_mirror: lanes c and c ^ 7
           x2[i] = (b2 ? x4[i + 2] : x4[i]) + dpp(b2 ? x4[i] : x4[i + 2], std::integral_constant<int, 0x141>{});
@@ -524,18 +622,19 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         if ((c & 1) == 0 && (!TAIL || at < tot)) a.acc[base + at] += x1;
       } else {
         // ---- the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
-        float nv[8], top = 0.0f;
+        float nv[NE], top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < NE; ++i) {
           nv[i] = (float)__builtin_bit_cast(h2, x.nv[i >> 1])[i & 1];
           top = fmaxf(top, fabsf(nv[i]));
         }
         if (__any(top > vlim)) {
           top = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < NE; ++i)
             top = fmaxf(top, fabsf(nv[i]) < INFINITY ? fabsf(nv[i]) : 0.0f);
           top = xmax(xmax(top, 16), 32);
+          if constexpr (PK) top = xmax(top, 8);
           if (top > vlim) {  // (uniform)
             int e2 = 0;
             frexpf(top, &e2);
@@ -549,16 +648,17 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) nv[i] *= vs;
+        for (int i = 0; i < NE; ++i) nv[i] *= vs;
         // ---- a score far above its row's maximum, or (not a number or infinite)
         //      no finite one yet: the maxima move
         bool over = false;
-        float p[RT][8], most[RT];
+        float p[RT][NE], most[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           against(t, m[t], p[t]);
-          most[t] = fmaxf(fmaxf(fmaxf(p[t][0], p[t][1]), fmaxf(p[t][2], p[t][3])),
-                          fmaxf(fmaxf(p[t][4], p[t][5]), fmaxf(p[t][6], p[t][7])));
+          most[t] = fmaxf(fmaxf(p[t][0], p[t][1]), fmaxf(p[t][2], p[t][3]));
+          if constexpr (!PK)
+            most[t] = fmaxf(most[t], fmaxf(fmaxf(p[t][4], p[t][5]), fmaxf(p[t][6], p[t][7])));
           over |= !(most[t] <= kLag);
         }
         if (__any(over)) {
@@ -569,10 +669,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
             if (first) {
               mh = -INFINITY;
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
+              for (int i = 0; i < NE; ++i)
                 if (!TAIL || (seen[t] >> i & 1)) mh = fmaxf(mh, s[t][i >> 2][i & 3] * nk[i]);
             }
             mh = xmax(xmax(mh, 16), 32);
+            if constexpr (PK) mh = xmax(mh, 8);
             const float m_new = first ? mh : m[t] + fmaxf(mh, 0.0f);
             const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
             m[t] = m_new;
@@ -580,7 +681,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
             l[t] *= f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float fr = __shfl(f, 4 * g16 + e, 64);
+              const float fr = __shfl(f, (4 * g16 + e) & (PK ? 7 : 15), 64);
 #pragma unroll
               for (int mu = 0; mu < VM; ++mu) acc[t][mu][e] *= fr;
             }
@@ -592,18 +693,34 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         for (int t = 0; t < RT; ++t) {
           uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) p[t][i] = __builtin_amdgcn_exp2f(p[t][i]);
+          for (int i = 0; i < NE; ++i) p[t][i] = __builtin_amdgcn_exp2f(p[t][i]);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) l[t] += p[t][i];
+          for (int i = 0; i < NE; ++i) l[t] += p[t][i];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < NE; ++i) {
             p[t][i] *= nv[i];
             if (TAIL) p[t][i] = seen[t] >> i & 1 ? p[t][i] : 0.0f;
           }
+          if constexpr (PK) {
+            // lanes h and h + 8 trade: row h takes both tiles' high parts, row
+            // h + 8 their low parts times 2^11
 #pragma unroll
-          for (int i = 0; i < 4; ++i) split2(p[t][2 * i], p[t][2 * i + 1], &hi[i], &lo[i]);
+            for (int i = 0; i < 2; ++i) {
+              uint32_t uh = __builtin_bit_cast(uint32_t, h2{(_Float16)p[0][2 * i], (_Float16)p[0][2 * i + 1]});
+              asm("" : "+v"(uh));  // (the rest is taken from these bits)
+              const h2 h = __builtin_bit_cast(h2, uh);
+              const uint32_t ul = __builtin_bit_cast(uint32_t, h2{(_Float16)((p[0][2 * i] - (float)h[0]) * 2048.0f),
+                                                                  (_Float16)((p[0][2 * i + 1] - (float)h[1]) * 2048.0f)});
+              const uint32_t got = __float_as_uint(ror8(__uint_as_float((c & 8) ? uh : ul)));
+              hi[i] = (c & 8) ? got : uh;
+              hi[2 + i] = (c & 8) ? ul : got;
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) split2(p[t][2 * i], p[t][2 * i + 1], &hi[i], &lo[i]);
+            __builtin_memcpy(&wl[t], lo, 16);
+          }
           __builtin_memcpy(&wh[t], hi, 16);
-          __builtin_memcpy(&wl[t], lo, 16);
         }
         // ---- values
         if constexpr (kStaged) lo_now = stage(a.vp, tb);
@@ -622,9 +739,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
 #pragma unroll
         for (int mu = 0; mu < VM; ++mu) {
           const h8 bv = vrow(mu, 0);
+          if constexpr (!PK) {
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-            acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl[t], bv, acc[t][mu], 0, 0, 0);
+            for (int t = 0; t < RT; ++t)
+              acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl[t], bv, acc[t][mu], 0, 0, 0);
+          }
 #pragma unroll
           for (int t = 0; t < RT; ++t)
             acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], bv, acc[t][mu], 0, 0, 0);
@@ -647,7 +766,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
 
     const int u_full = min(u_end, len / kStep);  // units of context only
     for (; u < u_full; u += kWaves) {
-      Unit<QD> nxt{};
+      Unit<QD, NE> nxt{};
       if (u + kWaves < u_end) nxt = load(u + kWaves);
       compute(cur, u * kStep, std::false_type{});
       cur = nxt;
@@ -659,92 +778,115 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
     }
 
     if constexpr (!WT) {
-      // ---- the wavefronts' states, halves at a time, into wavefront 0's
+      // ---- the wavefronts' states: the upper four are taken into the lower
+      //      four's registers, whose states all threads then combine into the record
       const float vi = ci / vs;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         l[t] = xsum(xsum(l[t], 16), 32);
+        if constexpr (PK) l[t] = xsum(l[t], 8);
 #pragma unroll
-        for (int mu = 0; mu < VM; ++mu) acc[t][mu] *= vi;
-      }
-      __syncthreads();  // (staged: the tiles are done with)
-#pragma unroll 1
-      for (int h = kWaves / 2; h > 0; h >>= 1) {
-        float* st = scratch + (size_t)(wave - (wave >= h ? h : 0)) * 64 * state_regs(D, RT) + lane;
-        if (wave >= h && wave < 2 * h) {
+        for (int mu = 0; mu < VM; ++mu) {
+          if constexpr (PK) {  // rows h and h + 8 sit in lanes l and l ^ 32
 #pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            st[(2 * t) * 64] = m[t];
-            st[(2 * t + 1) * 64] = l[t];
-#pragma unroll
-            for (int mu = 0; mu < VM; ++mu)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) st[(2 * RT + (t * VM + mu) * 4 + e) * 64] = acc[t][mu][e];
+            for (int e = 0; e < 4; ++e)
+              acc[t][mu][e] = fmaf(__shfl_xor(acc[t][mu][e], 32, 64), 0x1p-11f, acc[t][mu][e]);
           }
+          acc[t][mu] *= vi;
         }
-        __syncthreads();
-        if (wave < h) {
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            const float mo = st[(2 * t) * 64], lo = st[(2 * t + 1) * 64];
-            const float mx = fmaxf(m[t], mo), sub = mx == -INFINITY ? 0.0f : mx;
-            const float f = __builtin_amdgcn_exp2f(m[t] - sub), fo = __builtin_amdgcn_exp2f(mo - sub);
-            m[t] = mx;
-            l[t] = l[t] * f + lo * fo;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float fr = __shfl(f, 4 * g16 + e, 64), fro = __shfl(fo, 4 * g16 + e, 64);
-#pragma unroll
-              for (int mu = 0; mu < VM; ++mu)
-                acc[t][mu][e] = acc[t][mu][e] * fr + st[(2 * RT + (t * VM + mu) * 4 + e) * 64] * fro;
-            }
-          }
-        }
-        __syncthreads();
       }
-      const int64_t item = (int64_t)g * a.tiles + rt0;
-      if (wave == 0) {
-        // items and workgroups both only grow along the units, so item + workgroup
-        // is a different number for every segment
-        float* r = a.rec + (item + b) * rec_floats(D, RT);
-        int at = 2 * ROWS + 4 * g16 * D + 4 * (c >> 2) * VM + (c & 3);
-        asm volatile("" : "+v"(at));  // (64 addresses held through the unit loop would spill)
+      float* slot = scratch + (wave & 3) * state_floats(D, RT) + lane;
+      auto put = [&]() {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          if (lane < 16) {
-            r[16 * t + lane] = m[t];
-            r[ROWS + 16 * t + lane] = l[t];
-          }
+          slot[(2 * t) * kReg] = m[t];
+          slot[(2 * t + 1) * kReg] = l[t];
 #pragma unroll
           for (int mu = 0; mu < VM; ++mu)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              r[at + (16 * t + e) * D + 4 * mu] = acc[t][mu][e];
+            for (int e = 0; e < 4; ++e) slot[(2 * RT + (t * VM + mu) * 4 + e) * kReg] = acc[t][mu][e];
         }
-        if (lane == 0) {
-          if (r0 == 0) a.bounds[2 * item] = b;
-          if (r0 + take == (tot + kRun - 1) / kRun) a.bounds[2 * item + 1] = b;
+      };
+      lds_barrier();  // (the scratch is free)
+      if (wave >= 4) put();
+      lds_barrier();
+      if (wave < 4) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const float mo = slot[(2 * t) * kReg], lo = slot[(2 * t + 1) * kReg];
+          const float mx = fmaxf(m[t], mo), sub = mx == -INFINITY ? 0.0f : mx;
+          const float f = __builtin_amdgcn_exp2f(m[t] - sub), fo = __builtin_amdgcn_exp2f(mo - sub);
+          m[t] = mx;
+          l[t] = l[t] * f + lo * fo;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float fr = __shfl(f, 4 * g16 + e, 64), fro = __shfl(fo, 4 * g16 + e, 64);
+#pragma unroll
+            for (int mu = 0; mu < VM; ++mu)
+              acc[t][mu][e] = acc[t][mu][e] * fr + slot[(2 * RT + (t * VM + mu) * 4 + e) * kReg] * fro;
+          }
         }
+        put();
+      }
+      lds_barrier();
+      // items and workgroups both only grow along the units, so item + workgroup
+      // is a different number for every segment
+      float* r = a.rec + (item + b) * rec_floats(D, RT);
+      if (tid < ROWS) {
+        const float* st = scratch + 2 * (tid >> 4) * kReg + (tid & 15);
+        float mw[4], lw = 0.0f, mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          mw[i] = st[i * state_floats(D, RT)];
+          mx = fmaxf(mx, mw[i]);
+        }
+        const float sub = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = __builtin_amdgcn_exp2f(mw[i] - sub);
+          fac[i][tid] = f;
+          lw = fmaf(st[i * state_floats(D, RT) + kReg], f, lw);
+        }
+        r[tid] = mx;
+        r[ROWS + tid] = lw;
+      }
+      if (tid == 0) {
+        if (r0 == 0) a.bounds[2 * item] = b;
+        if (r0 + take == (tot + kRun - 1) / kRun) a.bounds[2 * item + 1] = b;
+      }
+      lds_barrier();
+#pragma unroll
+      for (int x = tid; x < (PK ? 8 : ROWS) * D; x += kThreads) {
+        // row 16 t + 4 g + e, dim 4 ((c / 4) VM + mu) + c % 4: register (t, mu, e) of lane 16 g + c
+        const int row = x / D, dim = x % D;
+        const int reg = 2 * RT + ((row >> 4) * VM + (dim >> 2) % VM) * 4 + (row & 3);
+        const float* st = scratch + reg * kReg + 16 * ((row >> 2) & 3) + 4 * (dim / (4 * VM)) + (dim & 3);
+        float v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v = fmaf(st[i * state_floats(D, RT)], fac[i][row], v);
+        r[2 * ROWS + x] = v;
       }
     }
   };
 
-  while (left > 0) {
-    // the next group that holds units (64 at a time)
-    for (;;) {
-      const int at = g + lane;
-      const uint64_t some = __ballot(at < a.n_groups && runs_of(a, min(at, a.n_groups - 1)) > 0);
-      if (some) {
-        g += __builtin_ctzll(some);
-        break;
+  for (bool first = true; left > 0; first = false) {
+    if (off == 0 && !first) {  // the next group that holds units (64 at a time)
+      for (;;) {
+        const int at = g + lane;
+        const uint64_t some = __ballot(at < a.n_groups && runs_of(a, min(at, a.n_groups - 1)) > 0);
+        if (some) {
+          g += __builtin_ctzll(some);
+          break;
+        }
+        g += 64;
+        if (g >= a.n_groups) return;  // (not reached: units are left)
       }
-      g += 64;
-      if (g >= a.n_groups) return;  // (not reached: units are left)
     }
     const int len = a.lens[g], runs = runs_of(a, g);
-    const int rt0 = (int)(off / runs), r0 = (int)(off - (uint64_t)rt0 * runs);
+    const int rt0 = a.tiles == 1 ? 0 : (int)((uint32_t)off / (uint32_t)runs);
+    const int r0 = (int)(off - (uint64_t)rt0 * runs);
     const int take = (int)(left < (uint64_t)(runs - r0) ? left : (uint64_t)(runs - r0));
-    segment(len, rt0, r0, take);
+    segment(len, rt0, r0, take, first);
     left -= take;
     off += take;
     if (off == (uint64_t)runs * a.tiles) {
@@ -752,18 +894,6 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       ++g;
     }
   }
-}
-
-// Partial maxima of |C| for staged codes, whose workgroups do not read all of it.
-__global__ __launch_bounds__(256) void top_kernel(const float* __restrict__ C, int n,
-                                                  float* __restrict__ top) {
-  __shared__ float red[4];
-  float t = 0.0f;
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += kTop * 256) t = fmaxf(t, fabsf(C[i]));
-  t = wave_max_dpp(t);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
-  __syncthreads();
-  if (threadIdx.x == 0) top[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
 // Block: 256 / D rows of a group, a thread per (row, dim).  Log-sum-exp over the
@@ -861,49 +991,50 @@ static int tile_rows(int rows, int D) {
 constexpr int kMaxWgs = 512;
 
 struct Layout {
-  int tile, tiles;
-  size_t off_bounds, off_stat, off_top, total;
+  bool packed;
+  int tile, tiles;  // rows of a tile, tiles of a group
+  size_t off_qs, off_start, off_top, off_bounds, off_stat, off_rec, total;
 };
 static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
   Layout y{};
   const int rows = (M > 0 ? M : 1) * G;
+  y.packed = rows <= 8;
   y.tile = tile_rows(rows, s.d);
   y.tiles = (rows + y.tile - 1) / y.tile;
-  const int64_t items = n_groups * y.tiles;
+  const size_t items = (size_t)n_groups * y.tiles;
   auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  y.off_bounds = al((size_t)(items + kMaxWgs) * rec_floats(s.d, y.tile / 16) * 4);
-  y.off_stat = al(y.off_bounds + (size_t)items * 8);
-  y.off_top = al(y.off_stat + (M > 0 ? 0 : (size_t)n_groups * rows * 8));
-  y.total = al(y.off_top + kTop * 4);
+  y.off_qs = al(items * (y.tile / 16) * (s.d / 32) * (y.packed ? 1 : 2) * 1024);
+  y.off_start = al(y.off_qs + items * 4);
+  y.off_top = al(y.off_start + kMaxWgs * sizeof(Start));
+  y.off_bounds = al(y.off_top + kTop * 4);
+  y.off_stat = al(y.off_bounds + items * 8);
+  y.off_rec = al(y.off_stat + (M > 0 ? 0 : (size_t)n_groups * rows * 8));
+  y.total = al(y.off_rec + (items + kMaxWgs) * rec_floats(s.d, y.tile / 16) * 4);
   return y;
 }
 
-template <int D, int RT, int W, int KB, int QW, bool WT>
-static hipError_t launch_rows(Args a, int table, hipStream_t st) {
+// The main launch of a code; *wgs: as many workgroups as run at once, two per
+// compute unit where registers and LDS allow, or one per run if those are fewer.
+template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
+static hipError_t launch_rows(Args a, int table, int wgs, hipStream_t st) {
   a.lds_scratch = table;
-  size_t scratch = (size_t)16 * RT * (D + 4) * 4;  // rotated queries
-  const size_t states = WT ? 0 : (size_t)(kWaves / 2) * 64 * state_regs(D, RT) * 4;
+  size_t scratch = WT ? 0 : (size_t)4 * state_floats(D, RT) * 4;
   const size_t tiles = QW == 0 ? (size_t)kWaves * 2 * kStep * tile_stride(D) : 0;
-  if (states > scratch) scratch = states;
   if (tiles > scratch) scratch = tiles;
   const size_t lds = table + scratch;
-  auto kern = rows_kernel<D, RT, W, KB, QW, WT>;
-  if (lds > 65536) {  // above the default dynamic LDS limit
+  auto kern = rows_kernel<D, RT, W, KB, QW, PK, WT>;
+  if (lds > 65536 - 4096) {  // above the default LDS limit, with the static part
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  // as many workgroups as run at once: two per compute unit where registers and LDS allow
-  const int64_t most = (int64_t)a.n_groups * a.tiles * ((a.T_stride + kRun - 1) / kRun);
-  int64_t wgs = RT == 1 && D == 64 && lds <= 78 * 1024 ? kMaxWgs : kMaxWgs / 2;
-  if (wgs > most) wgs = most;
   hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(kThreads), lds, st, a);
   return hipGetLastError();
 }
 
-template <int D, int RT, bool WT>
-static hipError_t launch_kind(const Args& a, const Kind& x, hipStream_t st) {
+template <int D, int RT, bool PK, bool WT>
+static hipError_t launch_kind(const Args& a, const Kind& x, int wgs, hipStream_t st) {
 #define FIBQ_SV(WW, KK, QQ) \
-  if (x.w == WW && x.kb == KK && x.qw == QQ) return launch_rows<D, RT, WW, KK, QQ, WT>(a, x.lds, st);
+  if (x.w == WW && x.kb == KK && x.qw == QQ) return launch_rows<D, RT, WW, KK, QQ, PK, WT>(a, x.lds, wgs, st);
   if constexpr (D == 64) {
     FIBQ_SV(8, 1, 1) FIBQ_SV(12, 1, 2) FIBQ_SV(4, 2, 1) FIBQ_SV(6, 2, 1)
   } else {
@@ -914,12 +1045,28 @@ static hipError_t launch_kind(const Args& a, const Kind& x, hipStream_t st) {
   return hipErrorInvalidValue;
 }
 
-template <int D>
-static hipError_t launch_tile(const Args& a, int tile, const Kind& x, hipStream_t st) {
-  if (tile == 16) return launch_kind<D, 1, false>(a, x, st);
-  if (tile == 32) return launch_kind<D, 2, false>(a, x, st);
-  if constexpr (D == 64) return launch_kind<D, 4, false>(a, x, st);
-  return hipErrorInvalidValue;
+// prep, main, merge, and the weights pass
+template <int D, int RT, bool PK>
+static int launch_tile(const ServeAttn& v, const Args& a, const Layout& y, const Kind& x, hipStream_t st) {
+  const int64_t items = v.n_groups * y.tiles;
+  const int64_t most = items * ((v.T_stride + kRun - 1) / kRun);
+  int64_t wgs = RT == 1 && D == 64 && x.qw > 0 && x.lds <= 32768 ? kMaxWgs : kMaxWgs / 2;
+  if (wgs > most) wgs = most;
+  hipError_t e = hipSuccess;
+  if (wgs > 0) {
+    hipLaunchKernelGGL((prep_kernel<D, RT, PK>), dim3((unsigned)(items + 1 + (x.qw == 0 ? kTop : 0))),
+                       dim3(256), 0, st, a, (int)wgs);
+    if ((e = hipGetLastError()) != hipSuccess) return (int)e;
+    if ((e = launch_kind<D, RT, PK, false>(a, x, (int)wgs, st)) != hipSuccess) return (int)e;
+  }
+  const int64_t blocks = v.n_groups * ((a.rows + 256 / D - 1) / (256 / D));
+  hipLaunchKernelGGL(merge_kernel<D>, dim3((unsigned)blocks), dim3(256), 0, st, a.rec, a.bounds,
+                     v.lens, v.T_stride, v.M, a.rows, y.tiles, y.tile, v.R,
+                     const_cast<float*>(a.stat), v.out);
+  if ((e = hipGetLastError()) != hipSuccess) return (int)e;
+  if constexpr (RT == 1)
+    if (v.acc && wgs > 0) return (int)launch_kind<D, 1, PK, true>(a, x, (int)wgs, st);
+  return 0;
 }
 
 template <int D>
@@ -953,28 +1100,19 @@ static int launch(const ServeAttn& v, hipStream_t st) {
   a.R = v.R;
   a.C = v.C;
   a.qscale = v.scale * 1.4426950408889634f;  // base-2 softmax
-  a.rec = reinterpret_cast<float*>(ws);
+  a.ops = reinterpret_cast<h8*>(ws);
+  a.qs = reinterpret_cast<float*>(ws + y.off_qs);
+  a.start = reinterpret_cast<Start*>(ws + y.off_start);
+  a.top = reinterpret_cast<float*>(ws + y.off_top);
   a.bounds = reinterpret_cast<int32_t*>(ws + y.off_bounds);
-  float* stat = v.acc ? reinterpret_cast<float*>(ws + y.off_stat) : nullptr;
-  float* top = reinterpret_cast<float*>(ws + y.off_top);
-  a.stat = stat;
-  a.top = top;
+  a.stat = v.acc ? reinterpret_cast<float*>(ws + y.off_stat) : nullptr;
+  a.rec = reinterpret_cast<float*>(ws + y.off_rec);
   a.acc = v.acc;
-  hipError_t e = hipSuccess;
-  const bool some = v.T_stride > 0;
-  if (some) {
-    if (x.qw == 0) {
-      hipLaunchKernelGGL(top_kernel, dim3(kTop), dim3(256), 0, st, v.C, v.s.N * v.s.k, top);
-      if ((e = hipGetLastError()) != hipSuccess) return (int)e;
-    }
-    if ((e = launch_tile<D>(a, y.tile, x, st)) != hipSuccess) return (int)e;
-  }
-  const int64_t blocks = v.n_groups * ((a.rows + 256 / D - 1) / (256 / D));
-  hipLaunchKernelGGL(merge_kernel<D>, dim3((unsigned)blocks), dim3(256), 0, st, a.rec, a.bounds,
-                     v.lens, v.T_stride, v.M, a.rows, y.tiles, y.tile, v.R, stat, v.out);
-  if ((e = hipGetLastError()) != hipSuccess) return (int)e;
-  if (v.acc && some) return (int)launch_kind<D, 1, true>(a, x, st);
-  return 0;
+  if (y.packed) return launch_tile<D, 1, true>(v, a, y, x, st);
+  if (y.tile == 16) return launch_tile<D, 1, false>(v, a, y, x, st);
+  if (y.tile == 32) return launch_tile<D, 2, false>(v, a, y, x, st);
+  if constexpr (D == 64) return launch_tile<D, 4, false>(v, a, y, x, st);
+  return (int)hipErrorInvalidValue;
 }
 
 }  // namespace sv
