@@ -83,7 +83,7 @@ struct Args {
   float* top;         // kTop partial maxima of |C| (staged codes)
   const float* stat;  // weights pass: m, l of every row
   float* acc;         // weights pass
-  int lds_scratch;
+  int lds_ops, lds_scratch;  // LDS bytes before the queries' low parts, the scratch
 };
 
 __host__ __device__ constexpr int rec_floats(int D, int RT) { return 16 * RT * (D + 2); }
@@ -91,6 +91,9 @@ constexpr int tile_stride(int D) { return 2 * D + 16; }  // bytes of a staged ro
 constexpr int state_regs(int D, int RT) { return RT * (D / 16) * 4 + 2 * RT; }
 constexpr int kReg = 68;  // floats between a state's registers in LDS: spreads the banks
 constexpr int state_floats(int D, int RT) { return state_regs(D, RT) * kReg; }
+// the queries' low parts: in registers for one row tile, else in LDS (they are 32
+// of 256 registers at four tiles, where the unit loop spilled without)
+constexpr int ops_bytes(int D, int RT) { return RT > 1 ? RT * (D / 32) * 1024 : 0; }
 
 // runs of units of a group; none for a bad length
 __device__ __forceinline__ int runs_of(const Args& a, int g) {
@@ -123,26 +126,33 @@ __device__ __forceinline__ f4 load4(const void* q, int64_t at) {
 // that takes the item's largest finite entry to [2^13, 2^14), so that the low
 // parts are normal numbers.
 template <int D, int RT, bool PK>
-__global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
+__global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args a, int wgs) {
   constexpr int KS = D / 32, KQ = D / 4, Q = D / 16;
   constexpr int ROWS = 16 * RT, QS = D + 4;
   __shared__ __align__(16) float qt[ROWS * QS];
-  __shared__ uint64_t sums[256];
-  __shared__ float red[4];
+  constexpr int kT = 256 * (RT > 1 ? 2 : 1);
+  __shared__ uint64_t sums[kT];
+  __shared__ float red[kT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int items = a.n_groups * a.tiles;
+  auto wave_max_of = [](const float* r) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kT / 64; ++i) t = fmaxf(t, r[i]);
+    return t;
+  };
   if ((int)blockIdx.x > items) {  // a part of the codebook's largest entry
     float t = 0.0f;
-    for (int i = (blockIdx.x - items - 1) * 256 + tid; i < a.N * a.k; i += kTop * 256)
+    for (int i = (blockIdx.x - items - 1) * kT + tid; i < a.N * a.k; i += kTop * kT)
       t = fmaxf(t, fabsf(a.C[i]));
     t = wave_max_dpp(t);
     if (lane == 0) red[wave] = t;
     __syncthreads();
-    if (tid == 0) a.top[blockIdx.x - items - 1] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    if (tid == 0) a.top[blockIdx.x - items - 1] = wave_max_of(red);
     return;
   }
   if ((int)blockIdx.x == items) {
-    const int per = (a.n_groups + 255) / 256;
+    const int per = (a.n_groups + kT - 1) / kT;
     uint64_t mine = 0;
     for (int i = 0; i < per; ++i) {
       const int g = tid * per + i;
@@ -158,7 +168,7 @@ __global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     uint64_t all = 0, add = 0;
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kT / 64; ++i) {
       if (i < wave) add += sums[i];
       all += sums[i];
     }
@@ -167,13 +177,13 @@ __global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
     __syncthreads();
     const uint64_t each = all >> 32 ? all / wgs : (uint32_t)all / (uint32_t)wgs;
     const uint32_t rest = (uint32_t)(all - each * wgs);
-    for (int b = tid; b < wgs; b += 256) {
+    for (int b = tid; b < wgs; b += kT) {
       const uint64_t from = b * each + min((uint32_t)b, rest);
       Start s{0, 0, 0, each + ((uint32_t)b < rest)};
       if (s.count > 0) {
         int t = 0;  // the first thread whose groups reach beyond `from`
 #pragma unroll
-        for (int h = 128; h > 0; h >>= 1)
+        for (int h = kT / 2; h > 0; h >>= 1)
           if (sums[t + h - 1] <= from) t += h;
         uint64_t off = from - (t > 0 ? sums[t - 1] : 0);
         int g = t * per;
@@ -195,7 +205,7 @@ __global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
   const int c = lane & 15, g16 = lane >> 4;
   const int live = (min(ROWS, a.rows - row0) + 15) / 16;
   float top = 0.0f;
-  for (int it = wave; it < (D / 16) * live; it += 4) {
+  for (int it = wave; it < (D / 16) * live; it += kT / 64) {
     const int dt = it % (D / 16), t = it / (D / 16);
     const int row = row0 + 16 * t + c;
     f4 pa[KQ / 4], pb[KQ / 4] = {};
@@ -204,11 +214,13 @@ __global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
       __builtin_memcpy(&pa[p], a.R + (16 * dt + c) * D + KQ * g16 + 4 * p, 16);
     if (row < a.rows) {
       const int64_t at = (g * a.rows + row) * D + KQ * g16;
+      auto all = [&](auto load) {
 #pragma unroll
-      for (int p = 0; p < KQ / 4; ++p)
-        pb[p] = a.q_dtype == FIBQ_F32   ? load4<float>(a.q, at + 4 * p)
-                : a.q_dtype == FIBQ_F16 ? load4<f16_t>(a.q, at + 4 * p)
-                                        : load4<bf16_t>(a.q, at + 4 * p);
+        for (int p = 0; p < KQ / 4; ++p) pb[p] = load(at + 4 * p);
+      };
+      if (a.q_dtype == FIBQ_F32) all([&](int64_t i) { return load4<float>(a.q, i); });
+      else if (a.q_dtype == FIBQ_F16) all([&](int64_t i) { return load4<f16_t>(a.q, i); });
+      else all([&](int64_t i) { return load4<bf16_t>(a.q, i); });
     }
     f4 s = {0, 0, 0, 0};
 #pragma unroll
@@ -226,7 +238,7 @@ __global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
   top = wave_max_dpp(top);
   if (lane == 0) red[wave] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  top = wave_max_of(red);
   float qs = 1.0f, qi = 1.0f;
   if (top > 0.0f) {
     int e2 = 0;
@@ -239,7 +251,7 @@ __global__ __launch_bounds__(256) void prep_kernel(const Args a, int wgs) {
   // B operand of K-step kap: lane l holds column l % 16 (PK: row l % 8, its high
   // part below 8, else its low part), K slots = dims 4 (l / 16 Q + 2 kap) .. + 7
   h8* to = a.ops + (int64_t)blockIdx.x * RT * KS * (PK ? 1 : 2) * 64;
-  for (int x = tid; x < RT * KS * 64; x += 256) {
+  for (int x = tid; x < RT * KS * 64; x += kT) {
     const int l = x & 63, kap = (x >> 6) % KS, t = (x >> 6) / KS;
     const int r = 16 * t + (PK ? l & 7 : l & 15);
     uint32_t hi[4] = {}, lo[4] = {};
@@ -284,7 +296,7 @@ struct Unit {
 // its unit, keys and then values, into a tile of its own and reads the operands
 // from there.
 template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
-__global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_kernel(const Args a) {
+__global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_kernel(const Args a) {
   constexpr int NB = D / 4, Q = NB / 4;  // 4-dim rows, of them per quarter
   constexpr int KS = D / 32, VM = D / 16;
   constexpr int ROWS = 16 * RT;
@@ -326,24 +338,38 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
   auto table = [&]() {
     bool lo_any = false;
     float top = 0.0f;
-    for (int i = tid; i < nrow; i += kThreads) {
-      float cv[4];
+    auto row = [&](int i, f4* v) {
       if (a.pair_n > 0) {
-        __builtin_memcpy(cv, a.C + 2 * (i % a.pair_n), 8);
-        __builtin_memcpy(cv + 2, a.C + 2 * (i / a.pair_n), 8);
+        __builtin_memcpy(v, a.C + 2 * (i & (a.pair_n - 1)), 8);
+        __builtin_memcpy(reinterpret_cast<float*>(v) + 2, a.C + 2 * (i / a.pair_n), 8);
       } else {
-        __builtin_memcpy(cv, a.C + (size_t)i * 4, 16);
+        __builtin_memcpy(v, a.C + (size_t)i * 4, 16);
       }
+    };
+    auto put = [&](int i, const f4& v) {
       h4 hi, lo;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        hi[e] = (_Float16)(cv[e] * cs);
-        lo[e] = (_Float16)fmaf(cv[e], cs, -(float)hi[e]);
+        hi[e] = (_Float16)(v[e] * cs);
+        lo[e] = (_Float16)fmaf(v[e], cs, -(float)hi[e]);
         lo_any |= (float)lo[e] != 0.0f;
-        top = fmaxf(top, fabsf(cv[e]));
+        top = fmaxf(top, fabsf(v[e]));
       }
       reinterpret_cast<h4*>(smem)[i] = hi;
       reinterpret_cast<h4*>(smem)[nrow + i] = lo;
+    };
+    int i = tid;
+    for (; i + 3 * kThreads < nrow; i += 4 * kThreads) {  // four loads at once
+      f4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) row(i + j * kThreads, &v[j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) put(i + j * kThreads, v[j]);
+    }
+    for (; i < nrow; i += kThreads) {
+      f4 v;
+      row(i, &v);
+      put(i, v);
     }
     top = wave_max_dpp(top);
     lo_any = __any(lo_any);
@@ -431,16 +457,22 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
 
     // ---- the tile's queries
     const int row0 = rt0 * ROWS;
-    h8 bh[RT][KS], bl[PK ? 1 : RT][PK ? 1 : KS];
+    h8 bh[RT][KS], bl[KS];  // (low parts: RT = 1 only)
     const h8* op = a.ops + item * (RT * KS * (PK ? 1 : 2) * 64) + lane;
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int kap = 0; kap < KS; ++kap) {
         bh[t][kap] = op[(t * KS + kap) * (PK ? 64 : 128)];
-        if constexpr (!PK) bl[t][kap] = op[(t * KS + kap) * 128 + 64];
+        if constexpr (RT == 1 && !PK) bl[kap] = op[kap * 128 + 64];
       }
     const float qs = a.qs[item];
+    if constexpr (RT > 1) {
+      h8* to = reinterpret_cast<h8*>(smem + a.lds_ops);
+      for (int x = tid; x < RT * KS * 64; x += kThreads)
+        to[x] = (a.ops + item * (RT * KS * 128))[(x >> 6) * 128 + 64 + (x & 63)];
+      lds_barrier();
+    }
     if (!kStaged && first) {  // the table is whole; is its scale right?
       lds_barrier();
       const float top = wave_max_dpp(red[lane & (kWaves - 1)]);
@@ -511,49 +543,68 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       return __any(any);
     };
 
-    // one unit; TAIL: it holds drafted tokens or ends behind the last one
-    auto compute = [&](const Unit<QD, NE>& x, int tb, auto tail_tag) {
-      constexpr bool TAIL = decltype(tail_tag)::value;
+    auto compute = [&](const Unit<QD, NE>& x, int tb) {
       bool lo_now = has_lo;  // (uniform) residual rows to add
       if constexpr (kStaged) lo_now = stage(a.kp, tb);
       const int lo_at = kStaged ? kStep * tile_stride(D) : nrow * 8;
       // two gathered rows per lane of tile t, K-step kap, `d` bytes behind the high parts
-      auto krow = [&](int t, int kap, int d) -> h8 {
+      auto krow = [&](const uint32_t (&kq)[2][QD], int t, int kap, int d) -> h8 {
         if constexpr (kStaged) {
           return *reinterpret_cast<const h8*>(tile + (16 * t + c) * tile_stride(D) + 8 * (g16 * Q + 2 * kap) + d);
         } else {
-          const h4 a0 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(x.kq[t], 2 * kap, w) + d);
-          const h4 a1 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(x.kq[t], 2 * kap + 1, w) + d);
+          const h4 a0 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(kq[t], 2 * kap, w) + d);
+          const h4 a1 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(kq[t], 2 * kap + 1, w) + d);
           return h8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
         }
       };
       // ---- scores of all row tiles, 16 tokens at a time
       f4 s[RT][2];
+      h8 ka[2][KS];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        h8 ka[KS];
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int kap = 0; kap < KS; ++kap) ka[kap] = krow(i, kap, 0);
+        for (int kap = 0; kap < KS; ++kap) ka[i][kap] = krow(x.kq, i, kap, 0);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) s[t][i] = f4{0, 0, 0, 0};
+      for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
+      int opl = a.lds_ops + 16 * lane;
+      asm volatile("" : "+v"(opl));  // (else these reads move out of the unit loop, into registers)
 #pragma unroll
-        for (int kap = 0; kap < KS; ++kap) {
-          if constexpr (!PK) {
+      for (int kap = 0; kap < KS; ++kap) {
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-              s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bl[t][kap], s[t][i], 0, 0, 0);
-          }
+        for (int t = 0; t < RT; ++t) {
+          if constexpr (PK) break;
+          h8 lo;
+          if constexpr (RT > 1) lo = *reinterpret_cast<const h8*>(smem + opl + (t * KS + kap) * 1024);
+          else lo = bl[kap];
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[kap], bh[t][kap], s[t][i], 0, 0, 0);
+          for (int i = 0; i < 2; ++i)
+            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[i][kap], lo, s[t][i], 0, 0, 0);
         }
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[i][kap], bh[t][kap], s[t][i], 0, 0, 0);
       }
+      // a copy whose row addresses are computed anew (kept from the high parts'
+      // reads for this rare path they would cost 16 registers)
+      auto again = [&](const uint32_t (&q)[2][QD], uint32_t (&y)[2][QD]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < QD; ++i) {
+            y[t][i] = q[t][i];
+            asm volatile("" : "+v"(y[t][i]));
+          }
+      };
       if (lo_now) {
+        uint32_t kq[2][QD];
+        again(x.kq, kq);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int kap = 0; kap < KS; ++kap) {
-            const h8 kr = krow(i, kap, lo_at);
+            const h8 kr = krow(kq, i, kap, lo_at);
 #pragma unroll
             for (int t = 0; t < RT; ++t)
               s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr, bh[t][kap], s[t][i], 0, 0, 0);
@@ -573,27 +624,44 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       float nk[NE];
 #pragma unroll
       for (int i = 0; i < NE; ++i) nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1] * ks;
-      uint32_t seen[RT];  // of this lane's tokens (tail units)
-      if constexpr (TAIL) {
+      float nv[NE];
+#pragma unroll
+      for (int i = 0; i < NE; ++i)
+        nv[i] = WT ? 0.0f : (float)__builtin_bit_cast(h2, x.nv[i >> 1])[i & 1];
+      // A unit that holds drafted tokens or ends behind the last one: unseen
+      // scores become -inf.  Norms may be anything there: one that is not a
+      // positive number is multiplied into the seen scores (a value norm that is
+      // no number makes them NaN), and leaves the unseen ones alone.  A token that
+      // no row of the tile sees gets value norm 0, so that it has no part in the
+      // scale of the weights either.
+      if (tb + kStep > len) {
+        uint32_t seen = 0;  // by this lane's rows
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           uint64_t mask = 0;
           if (!WT && a.M > 0) mask = a.masks[g * a.mask_stride + min(row0 + 16 * t + hr, a.rows - 1) / a.G];
-          seen[t] = 0;
 #pragma unroll
           for (int i = 0; i < NE; ++i) {
             const int j = tb + token(i) - len;
-            if (j < 0 || (j < a.M && (mask >> (j & 63) & 1))) seen[t] |= 1u << i;
+            float v = s[t][i >> 2][i & 3];
+            if (!(nk[i] > 0.0f && nk[i] < INFINITY)) v *= nk[i];
+            if (!(fabsf(nv[i]) < INFINITY)) v = NAN;
+            const bool in = j < 0 || (j < a.M && (mask >> (j & 63) & 1));
+            s[t][i >> 2][i & 3] = in ? v : -INFINITY;
+            seen |= (uint32_t)in << i;
           }
         }
-      }
-      // scores against the running maxima (an unseen token's norm may be anything)
-      auto against = [&](int t, float ref, float (&p)[NE]) {
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-          p[i] = fmaf(s[t][i >> 2][i & 3], nk[i], -ref);
-          if (TAIL) p[i] = seen[t] >> i & 1 ? p[i] : -INFINITY;
+          // (the lanes that hold this token's scores)
+          const uint64_t any = __ballot(seen >> i & 1) >> (lane & (PK ? 56 : 48)) & (PK ? 0xFF : 0xFFFF);
+          nk[i] = nk[i] > 0.0f && nk[i] < INFINITY ? nk[i] : 1.0f;
+          nv[i] = any != 0 && fabsf(nv[i]) < INFINITY ? nv[i] : 0.0f;
         }
+      }
+      auto against = [&](int t, float ref, float (&p)[NE]) {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) p[i] = fmaf(s[t][i >> 2][i & 3], nk[i], -ref);
       };
       if constexpr (WT) {
         float p[NE];
@@ -619,15 +687,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         float x1 = (b1 ? x2[1] : x2[0]) + dpp(b1 ? x2[0] : x2[1], std::integral_constant<int, 0x4E>{});
         x1 += dpp(x1, std::integral_constant<int, 0xB1>{});
         const int at = tb + 16 * (b3 ? 1 : 0) + 4 * g16 + (b2 ? 2 : 0) + (b1 ? 1 : 0);
-        if ((c & 1) == 0 && (!TAIL || at < tot)) a.acc[base + at] += x1;
+        if ((c & 1) == 0 && at < tot) a.acc[base + at] += x1;
       } else {
         // ---- the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
-        float nv[NE], top = 0.0f;
+        float top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NE; ++i) {
-          nv[i] = (float)__builtin_bit_cast(h2, x.nv[i >> 1])[i & 1];
-          top = fmaxf(top, fabsf(nv[i]));
-        }
+        for (int i = 0; i < NE; ++i) top = fmaxf(top, fabsf(nv[i]));
         if (__any(top > vlim)) {
           top = 0.0f;
 #pragma unroll
@@ -670,7 +735,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
               mh = -INFINITY;
 #pragma unroll
               for (int i = 0; i < NE; ++i)
-                if (!TAIL || (seen[t] >> i & 1)) mh = fmaxf(mh, s[t][i >> 2][i & 3] * nk[i]);
+                mh = fmaxf(mh, s[t][i >> 2][i & 3] * nk[i]);
             }
             mh = xmax(xmax(mh, 16), 32);
             if constexpr (PK) mh = xmax(mh, 8);
@@ -697,10 +762,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
 #pragma unroll
           for (int i = 0; i < NE; ++i) l[t] += p[t][i];
 #pragma unroll
-          for (int i = 0; i < NE; ++i) {
-            p[t][i] *= nv[i];
-            if (TAIL) p[t][i] = seen[t] >> i & 1 ? p[t][i] : 0.0f;
-          }
+          for (int i = 0; i < NE; ++i) p[t][i] *= nv[i];
           if constexpr (PK) {
             // lanes h and h + 8 trade: row h takes both tiles' high parts, row
             // h + 8 their low parts times 2^11
@@ -724,21 +786,21 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         }
         // ---- values
         if constexpr (kStaged) lo_now = stage(a.vp, tb);
-        auto vrow = [&](int mu, int d) -> h8 {
+        auto vrow = [&](const uint32_t (&vq)[2][QD], int mu, int d) -> h8 {
           const unsigned char *ra, *rb;
           if constexpr (kStaged) {
             ra = tile + (4 * g16 + (c >> 2)) * tile_stride(D) + 8 * ((c & 3) * VM + mu) + d;
             rb = ra + 16 * tile_stride(D);
           } else {
-            ra = smem + qrow<QD, W, KB>(x.vq[0], mu, w) + d;
-            rb = smem + qrow<QD, W, KB>(x.vq[1], mu, w) + d;
+            ra = smem + qrow<QD, W, KB>(vq[0], mu, w) + d;
+            rb = smem + qrow<QD, W, KB>(vq[1], mu, w) + d;
           }
           const h4 b0 = tr_read(ra), b1 = tr_read(rb);
           return h8{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
         };
 #pragma unroll
         for (int mu = 0; mu < VM; ++mu) {
-          const h8 bv = vrow(mu, 0);
+          const h8 bv = vrow(x.vq, mu, 0);
           if constexpr (!PK) {
 #pragma unroll
             for (int t = 0; t < RT; ++t)
@@ -749,9 +811,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
             acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], bv, acc[t][mu], 0, 0, 0);
         }
         if (lo_now) {
+          uint32_t vq[2][QD];
+          again(x.vq, vq);
 #pragma unroll
           for (int mu = 0; mu < VM; ++mu) {
-            const h8 dv = vrow(mu, lo_at);
+            const h8 dv = vrow(vq, mu, lo_at);
 #pragma unroll
             for (int t = 0; t < RT; ++t)
               acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], dv, acc[t][mu], 0, 0, 0);
@@ -764,17 +828,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
       }
     };
 
-    const int u_full = min(u_end, len / kStep);  // units of context only
-    for (; u < u_full; u += kWaves) {
+    for (; u < u_end; u += kWaves) {
       Unit<QD, NE> nxt{};
       if (u + kWaves < u_end) nxt = load(u + kWaves);
-      compute(cur, u * kStep, std::false_type{});
+      compute(cur, u * kStep);
       cur = nxt;
-    }
-#pragma unroll 1
-    for (; u < u_end; u += kWaves) {
-      compute(cur, u * kStep, std::true_type{});
-      if (u + kWaves < u_end) cur = load(u + kWaves);
     }
 
     if constexpr (!WT) {
@@ -855,7 +913,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
         if (r0 + take == (tot + kRun - 1) / kRun) a.bounds[2 * item + 1] = b;
       }
       lds_barrier();
-#pragma unroll
+#pragma unroll 1  // (code is fetched once per workgroup, at about 0.7 us per KB)
       for (int x = tid; x < (PK ? 8 : ROWS) * D; x += kThreads) {
         // row 16 t + 4 g + e, dim 4 ((c / 4) VM + mu) + c % 4: register (t, mu, e) of lane 16 g + c
         const int row = x / D, dim = x % D;
@@ -897,20 +955,25 @@ __global__ __launch_bounds__(kThreads, RT == 1 && D == 64 ? 4 : 2) void rows_ker
 }
 
 // Block: 256 / D rows of a group, a thread per (row, dim).  Log-sum-exp over the
-// row's records, o = Pi^T (acc / l); stat (nullable) receives m and l.
+// row's records, then o = Pi^T (acc / l) with Pi's rows in stripes over the
+// threads, loaded before the records; stat (nullable) receives m and l.
 template <int D>
 __global__ __launch_bounds__(256) void merge_kernel(
     const float* __restrict__ rec, const int32_t* __restrict__ bounds,
     const int32_t* __restrict__ lens, int64_t T_stride, int M, int rows, int tiles, int tile_rows,
     const float* __restrict__ R, float* __restrict__ stat, float* __restrict__ out) {
-  constexpr int HB = 256 / D;
+  constexpr int HB = 256 / D, RI = D / HB;  // stripes = rows of the block
   __shared__ float ar[HB][D];
+  __shared__ float part[HB][HB][D];
   const int blocks = (rows + HB - 1) / HB;
   const int64_t g = blockIdx.x / blocks;
   const int hr = threadIdx.x / D, dim = threadIdx.x % D;
   const int row = (int)(blockIdx.x % blocks) * HB + hr;
   const int len = lens[g];
   const bool bad = len < 0 || len > T_stride - M;
+  float pi[RI];
+#pragma unroll
+  for (int i = 0; i < RI; ++i) pi[i] = R[(hr * RI + i) * D + dim];
   float m = -INFINITY, l = 0.0f, s = 0.0f;
   if (!bad && len + M > 0 && row < rows) {
     const int64_t item = g * tiles + row / tile_rows;
@@ -942,10 +1005,18 @@ __global__ __launch_bounds__(256) void merge_kernel(
   }
   ar[hr][dim] = l == 0.0f ? 0.0f : s / l;
   __syncthreads();
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {  // this stripe's part of row h
+    float o = 0.0f;
+#pragma unroll
+    for (int i = 0; i < RI; ++i) o = fmaf(pi[i], ar[h][hr * RI + i], o);
+    part[hr][h][dim] = o;
+  }
+  __syncthreads();
   if (row >= rows) return;
   float o = 0.0f;
-#pragma unroll 16
-  for (int i = 0; i < D; ++i) o = fmaf(R[i * D + dim], ar[hr][i], o);
+#pragma unroll
+  for (int x = 0; x < HB; ++x) o += part[x][hr][dim];
   out[(g * rows + row) * D + dim] = bad ? NAN : o;
   if (stat && dim < 2) stat[(g * rows + row) * 2 + dim] = dim == 0 ? m : l;
 }
@@ -1017,11 +1088,12 @@ static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
 // compute unit where registers and LDS allow, or one per run if those are fewer.
 template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
 static hipError_t launch_rows(Args a, int table, int wgs, hipStream_t st) {
-  a.lds_scratch = table;
+  a.lds_ops = table;
+  a.lds_scratch = table + ops_bytes(D, RT);
   size_t scratch = WT ? 0 : (size_t)4 * state_floats(D, RT) * 4;
   const size_t tiles = QW == 0 ? (size_t)kWaves * 2 * kStep * tile_stride(D) : 0;
   if (tiles > scratch) scratch = tiles;
-  const size_t lds = table + scratch;
+  const size_t lds = a.lds_scratch + scratch;
   auto kern = rows_kernel<D, RT, W, KB, QW, PK, WT>;
   if (lds > 65536 - 4096) {  // above the default LDS limit, with the static part
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -1050,12 +1122,12 @@ template <int D, int RT, bool PK>
 static int launch_tile(const ServeAttn& v, const Args& a, const Layout& y, const Kind& x, hipStream_t st) {
   const int64_t items = v.n_groups * y.tiles;
   const int64_t most = items * ((v.T_stride + kRun - 1) / kRun);
-  int64_t wgs = RT == 1 && D == 64 && x.qw > 0 && x.lds <= 32768 ? kMaxWgs : kMaxWgs / 2;
+  int64_t wgs = PK && D == 64 && x.qw > 0 && x.lds <= 32768 ? kMaxWgs : kMaxWgs / 2;
   if (wgs > most) wgs = most;
   hipError_t e = hipSuccess;
   if (wgs > 0) {
     hipLaunchKernelGGL((prep_kernel<D, RT, PK>), dim3((unsigned)(items + 1 + (x.qw == 0 ? kTop : 0))),
-                       dim3(256), 0, st, a, (int)wgs);
+                       dim3(256 * (RT > 1 ? 2 : 1)), 0, st, a, (int)wgs);
     if ((e = hipGetLastError()) != hipSuccess) return (int)e;
     if ((e = launch_kind<D, RT, PK, false>(a, x, (int)wgs, st)) != hipSuccess) return (int)e;
   }
