@@ -391,14 +391,20 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
   const int kst = min(kbit >> 3, P - 4 * QD), vst = min(vbit >> 3, P - 4 * QD);
   const int ksh = kbit - 8 * kst, vsh = vbit - 8 * vst;
   const int ko = c * P + kst, vo = (4 * g16 + (c >> 2)) * P + vst;
-  auto quarter = [&](const uint8_t* at, int sh, uint32_t (&d)[QD]) {
-    __builtin_memcpy(d, at, 4 * QD);
-    if constexpr (QD == 1) {
-      d[0] >>= sh;
-    } else if constexpr (QD == 2) {
-      const uint64_t u = ((uint64_t)d[0] | ((uint64_t)d[1] << 32)) >> sh;
-      d[0] = (uint32_t)u;
-      d[1] = (uint32_t)(u >> 32);
+  // (shifted where it is used: a shift at the load would wait for it)
+  auto shifted = [&](const uint32_t (&q)[2][QD], int sh, uint32_t (&d)[2][QD]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if constexpr (QD == 1) {
+        d[t][0] = q[t][0] >> sh;
+      } else if constexpr (QD == 2) {
+        const uint64_t u = ((uint64_t)q[t][0] | ((uint64_t)q[t][1] << 32)) >> sh;
+        d[t][0] = (uint32_t)u;
+        d[t][1] = (uint32_t)(u >> 32);
+      } else {
+#pragma unroll
+        for (int i = 0; i < QD; ++i) d[t][i] = q[t][i];
+      }
     }
   };
   // token i of the lane's softmax tokens, in the unit
@@ -423,8 +429,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         const uint8_t* vb = vpg + (int64_t)tb * P;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if constexpr (!kStaged) quarter(kb + (uint32_t)(16 * t * P + ko), ksh, x.kq[t]);
-          if constexpr (!kStaged && !WT) quarter(vb + (uint32_t)(16 * t * P + vo), vsh, x.vq[t]);
+          if constexpr (!kStaged) __builtin_memcpy(x.kq[t], kb + (uint32_t)(16 * t * P + ko), 4 * QD);
+          if constexpr (!kStaged && !WT) __builtin_memcpy(x.vq[t], vb + (uint32_t)(16 * t * P + vo), 4 * QD);
         }
 #pragma unroll
         for (int i = 0; i < NE; i += 4) {
@@ -436,9 +442,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
       if constexpr (!kStaged) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          quarter(kpg + (int64_t)min(tb + 16 * t + c, tm) * P + kst, ksh, x.kq[t]);
+          __builtin_memcpy(x.kq[t], kpg + (int64_t)min(tb + 16 * t + c, tm) * P + kst, 4 * QD);
           if constexpr (!WT)
-            quarter(vpg + (int64_t)min(tb + 16 * t + 4 * g16 + (c >> 2), tm) * P + vst, vsh, x.vq[t]);
+            __builtin_memcpy(x.vq[t], vpg + (int64_t)min(tb + 16 * t + 4 * g16 + (c >> 2), tm) * P + vst, 4 * QD);
         }
       }
 #pragma unroll
@@ -546,14 +552,17 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
     auto compute = [&](const Unit<QD, NE>& x, int tb) {
       bool lo_now = has_lo;  // (uniform) residual rows to add
       if constexpr (kStaged) lo_now = stage(a.kp, tb);
+      uint32_t kq[2][QD], vq[2][QD];
+      shifted(x.kq, ksh, kq);
+      shifted(x.vq, vsh, vq);
       const int lo_at = kStaged ? kStep * tile_stride(D) : nrow * 8;
       // two gathered rows per lane of tile t, K-step kap, `d` bytes behind the high parts
-      auto krow = [&](const uint32_t (&kq)[2][QD], int t, int kap, int d) -> h8 {
+      auto krow = [&](const uint32_t (&q)[2][QD], int t, int kap, int d) -> h8 {
         if constexpr (kStaged) {
           return *reinterpret_cast<const h8*>(tile + (16 * t + c) * tile_stride(D) + 8 * (g16 * Q + 2 * kap) + d);
         } else {
-          const h4 a0 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(kq[t], 2 * kap, w) + d);
-          const h4 a1 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(kq[t], 2 * kap + 1, w) + d);
+          const h4 a0 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(q[t], 2 * kap, w) + d);
+          const h4 a1 = *reinterpret_cast<const h4*>(smem + qrow<QD, W, KB>(q[t], 2 * kap + 1, w) + d);
           return h8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
         }
       };
@@ -563,7 +572,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int kap = 0; kap < KS; ++kap) ka[i][kap] = krow(x.kq, i, kap, 0);
+        for (int kap = 0; kap < KS; ++kap) ka[i][kap] = krow(kq, i, kap, 0);
 #pragma unroll
       for (int t = 0; t < RT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
       int opl = a.lds_ops + 16 * lane;
@@ -598,13 +607,13 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           }
       };
       if (lo_now) {
-        uint32_t kq[2][QD];
-        again(x.kq, kq);
+        uint32_t kl[2][QD];
+        again(kq, kl);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int kap = 0; kap < KS; ++kap) {
-            const h8 kr = krow(kq, i, kap, lo_at);
+            const h8 kr = krow(kl, i, kap, lo_at);
 #pragma unroll
             for (int t = 0; t < RT; ++t)
               s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr, bh[t][kap], s[t][i], 0, 0, 0);
@@ -786,21 +795,21 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         }
         // ---- values
         if constexpr (kStaged) lo_now = stage(a.vp, tb);
-        auto vrow = [&](const uint32_t (&vq)[2][QD], int mu, int d) -> h8 {
+        auto vrow = [&](const uint32_t (&q)[2][QD], int mu, int d) -> h8 {
           const unsigned char *ra, *rb;
           if constexpr (kStaged) {
             ra = tile + (4 * g16 + (c >> 2)) * tile_stride(D) + 8 * ((c & 3) * VM + mu) + d;
             rb = ra + 16 * tile_stride(D);
           } else {
-            ra = smem + qrow<QD, W, KB>(vq[0], mu, w) + d;
-            rb = smem + qrow<QD, W, KB>(vq[1], mu, w) + d;
+            ra = smem + qrow<QD, W, KB>(q[0], mu, w) + d;
+            rb = smem + qrow<QD, W, KB>(q[1], mu, w) + d;
           }
           const h4 b0 = tr_read(ra), b1 = tr_read(rb);
           return h8{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
         };
 #pragma unroll
         for (int mu = 0; mu < VM; ++mu) {
-          const h8 bv = vrow(x.vq, mu, 0);
+          const h8 bv = vrow(vq, mu, 0);
           if constexpr (!PK) {
 #pragma unroll
             for (int t = 0; t < RT; ++t)
@@ -811,11 +820,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
             acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], bv, acc[t][mu], 0, 0, 0);
         }
         if (lo_now) {
-          uint32_t vq[2][QD];
-          again(x.vq, vq);
+          uint32_t vl[2][QD];
+          again(vq, vl);
 #pragma unroll
           for (int mu = 0; mu < VM; ++mu) {
-            const h8 dv = vrow(vq, mu, lo_at);
+            const h8 dv = vrow(vl, mu, lo_at);
 #pragma unroll
             for (int t = 0; t < RT; ++t)
               acc[t][mu] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[t], dv, acc[t][mu], 0, 0, 0);
