@@ -30,7 +30,7 @@
 //   Up to 8 rows ("packed") share a product between their parts: columns h and
 //   h + 8 of B are row h's high and low part, summed by one exchange in which
 //   lane h keeps the first tile's tokens and lane h + 8 the second's; rows h and
-//   h + 8 of the weights are row h's parts (the low one times 2^11).
+//   h + 8 of the weights are row h's parts.
 // merge_kernel combines an item's records by log-sum-exp and applies Pi^T.
 #include <hip/hip_runtime.h>
 
@@ -83,7 +83,7 @@ struct Args {
   float* top;         // kTop partial maxima of |C| (staged codes)
   const float* stat;  // weights pass: m, l of every row
   float* acc;         // weights pass
-  int lds_ops, lds_scratch;  // LDS bytes before the queries' low parts, the scratch
+  int lds_small, lds_ops, lds_scratch;  // LDS bytes before the small arrays, the queries' low parts, the scratch
 };
 
 __host__ __device__ constexpr int rec_floats(int D, int RT) { return 16 * RT * (D + 2); }
@@ -284,6 +284,7 @@ template <int QW, int NE>
 struct Unit {
   uint32_t kq[2][QW], vq[2][QW];
   uint32_t nk[NE / 2], nv[NE / 2];
+  float acc;  // weights pass: the accumulator that the lane adds to
 };
 
 // W > 0: compile-time index width, W = 0: at run time; KB: 4-dim rows per
@@ -304,10 +305,12 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
   constexpr bool kStaged = QW == 0;
   constexpr int QD = kStaged ? 1 : QW;
   static_assert(!PK || RT == 1, "packed rows are one tile");
+  // All LDS is dynamic, the table first: at address 0 its rows' offsets are their
+  // addresses (one instruction less per gathered row).
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float red[kWaves];
-  __shared__ int redi[kWaves];
-  __shared__ float fac[4][ROWS];  // the states' factors in a record, and the rows' m, l
+  float* red = reinterpret_cast<float*>(smem + a.lds_small);  // [kWaves]
+  int* redi = reinterpret_cast<int*>(red + kWaves);            // [kWaves]
+  float* fac = red + 2 * kWaves;                               // [4][ROWS]: the states' factors in a record
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g16 = lane >> 4, c = lane & 15, hr = PK ? c & 7 : c;
@@ -410,6 +413,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
   // token i of the lane's softmax tokens, in the unit
   const int tok0 = 4 * g16 + (PK ? 2 * (c & 8) : 0);
   auto token = [&](int i) { return tok0 + 16 * (i >> 2) + (i & 3); };
+  // weights pass: the token whose sum ends in this lane (bits 3, 2, 1 of c)
+  const int acc_tok = 2 * (c & 8) + 4 * g16 + (c & 4) / 2 + (c & 2) / 2;
 
   // ---- one item, runs r0 .. r0 + take - 1
   auto segment = [&](int len, int rt0, int r0, int take, bool first) {
@@ -427,18 +432,26 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
       if (tb + kStep <= tot) {
         const uint8_t* kb = kpg + (int64_t)tb * P;
         const uint8_t* vb = vpg + (int64_t)tb * P;
+        const uint8_t* knb = reinterpret_cast<const uint8_t*>(kng + tb);
+        const uint8_t* vnb = reinterpret_cast<const uint8_t*>(vng + tb);
+        // (the offsets stay 32 bits wide and in this block, so that they are the
+        // loads' own offset operands)
+        uint32_t ok = ko, ov = vo, on = 2 * tok0;
+        asm volatile("" : "+v"(ok), "+v"(ov), "+v"(on));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if constexpr (!kStaged) __builtin_memcpy(x.kq[t], kb + (uint32_t)(16 * t * P + ko), 4 * QD);
-          if constexpr (!kStaged && !WT) __builtin_memcpy(x.vq[t], vb + (uint32_t)(16 * t * P + vo), 4 * QD);
+          if constexpr (!kStaged) __builtin_memcpy(x.kq[t], kb + 16 * t * P + ok, 4 * QD);
+          if constexpr (!kStaged && !WT) __builtin_memcpy(x.vq[t], vb + 16 * t * P + ov, 4 * QD);
         }
 #pragma unroll
         for (int i = 0; i < NE; i += 4) {
-          __builtin_memcpy(&x.nk[i / 2], kng + tb + (uint32_t)(tok0 + 4 * i), 8);
-          if constexpr (!WT) __builtin_memcpy(&x.nv[i / 2], vng + tb + (uint32_t)(tok0 + 4 * i), 8);
+          __builtin_memcpy(&x.nk[i / 2], knb + 8 * i + on, 8);
+          if constexpr (!WT) __builtin_memcpy(&x.nv[i / 2], vnb + 8 * i + on, 8);
         }
+        if constexpr (WT) x.acc = a.acc[base + tb + acc_tok];
         return x;
       }
+      if constexpr (WT) x.acc = a.acc[base + min(tb + acc_tok, tm)];
       if constexpr (!kStaged) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -494,6 +507,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
     f4 acc[RT][VM];
     float m[RT], l[RT];
     float vlim = 0.0f, vs = 1.0f;  // bound of the value norms so far, their scale
+    uint16_t vbits = 0;            // the largest binary16 below the bound, as bits
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       m[t] = -INFINITY;
@@ -695,15 +709,17 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         // quad_perm [2, 3, 0, 1] and [1, 0, 3, 2]: lanes c and c ^ 2, c and c ^ 1
         float x1 = (b1 ? x2[1] : x2[0]) + dpp(b1 ? x2[0] : x2[1], std::integral_constant<int, 0x4E>{});
         x1 += dpp(x1, std::integral_constant<int, 0xB1>{});
-        const int at = tb + 16 * (b3 ? 1 : 0) + 4 * g16 + (b2 ? 2 : 0) + (b1 ? 1 : 0);
-        if ((c & 1) == 0 && at < tot) a.acc[base + at] += x1;
+        const int at = tb + acc_tok;
+        if ((c & 1) == 0 && at < tot) a.acc[base + at] = x.acc + x1;
       } else {
         // ---- the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
-        float top = 0.0f;
+        typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+        u2 most_v = __builtin_bit_cast(u2, x.nv[0]);
 #pragma unroll
-        for (int i = 0; i < NE; ++i) top = fmaxf(top, fabsf(nv[i]));
-        if (__any(top > vlim)) {
-          top = 0.0f;
+        for (int i = 1; i < NE / 2; ++i) most_v = __builtin_elementwise_max(most_v, __builtin_bit_cast(u2, x.nv[i]));
+        // (norms as binary16 bits: one that is no positive number compares above all)
+        if (__any(__builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(most_v, u2(vbits))) != 0)) {
+          float top = 0.0f;
 #pragma unroll
           for (int i = 0; i < NE; ++i)
             top = fmaxf(top, fabsf(nv[i]) < INFINITY ? fabsf(nv[i]) : 0.0f);
@@ -714,6 +730,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
             frexpf(top, &e2);
             const float now = ldexpf(1.0f, 7 - e2), f = now / vs;
             vlim = ldexpf(1.0f, e2);
+            vbits = (uint16_t)(__builtin_bit_cast(uint16_t, (_Float16)vlim) - 1);
             vs = now;
 #pragma unroll
             for (int t = 0; t < RT; ++t)
@@ -774,14 +791,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           for (int i = 0; i < NE; ++i) p[t][i] *= nv[i];
           if constexpr (PK) {
             // lanes h and h + 8 trade: row h takes both tiles' high parts, row
-            // h + 8 their low parts times 2^11
+            // h + 8 their low parts
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              uint32_t uh = __builtin_bit_cast(uint32_t, h2{(_Float16)p[0][2 * i], (_Float16)p[0][2 * i + 1]});
-              asm("" : "+v"(uh));  // (the rest is taken from these bits)
-              const h2 h = __builtin_bit_cast(h2, uh);
-              const uint32_t ul = __builtin_bit_cast(uint32_t, h2{(_Float16)((p[0][2 * i] - (float)h[0]) * 2048.0f),
-                                                                  (_Float16)((p[0][2 * i + 1] - (float)h[1]) * 2048.0f)});
+              uint32_t uh, ul;
+              split2(p[0][2 * i], p[0][2 * i + 1], &uh, &ul);
               const uint32_t got = __float_as_uint(ror8(__uint_as_float((c & 8) ? uh : ul)));
               hi[i] = (c & 8) ? got : uh;
               hi[2 + i] = (c & 8) ? ul : got;
@@ -837,7 +851,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
       }
     };
 
-    for (; u < u_end; u += kWaves) {
+    for (; u < u_end; u += kWaves) {  // (the next unit's loads are in flight meanwhile)
       Unit<QD, NE> nxt{};
       if (u + kWaves < u_end) nxt = load(u + kWaves);
       compute(cur, u * kStep);
@@ -857,7 +871,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           if constexpr (PK) {  // rows h and h + 8 sit in lanes l and l ^ 32
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              acc[t][mu][e] = fmaf(__shfl_xor(acc[t][mu][e], 32, 64), 0x1p-11f, acc[t][mu][e]);
+              acc[t][mu][e] += __shfl_xor(acc[t][mu][e], 32, 64);
           }
           acc[t][mu] *= vi;
         }
@@ -911,7 +925,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float f = __builtin_amdgcn_exp2f(mw[i] - sub);
-          fac[i][tid] = f;
+          fac[i * ROWS + tid] = f;
           lw = fmaf(st[i * state_floats(D, RT) + kReg], f, lw);
         }
         r[tid] = mx;
@@ -930,7 +944,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         const float* st = scratch + reg * kReg + 16 * ((row >> 2) & 3) + 4 * (dim / (4 * VM)) + (dim & 3);
         float v = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v = fmaf(st[i * state_floats(D, RT)], fac[i][row], v);
+        for (int i = 0; i < 4; ++i) v = fmaf(st[i * state_floats(D, RT)], fac[i * ROWS + row], v);
         r[2 * ROWS + x] = v;
       }
     }
@@ -1097,14 +1111,15 @@ static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
 // compute unit where registers and LDS allow, or one per run if those are fewer.
 template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
 static hipError_t launch_rows(Args a, int table, int wgs, hipStream_t st) {
-  a.lds_ops = table;
-  a.lds_scratch = table + ops_bytes(D, RT);
+  a.lds_small = table;
+  a.lds_ops = table + (2 * kWaves + 4 * 16 * RT) * 4;
+  a.lds_scratch = a.lds_ops + ops_bytes(D, RT);
   size_t scratch = WT ? 0 : (size_t)4 * state_floats(D, RT) * 4;
   const size_t tiles = QW == 0 ? (size_t)kWaves * 2 * kStep * tile_stride(D) : 0;
   if (tiles > scratch) scratch = tiles;
   const size_t lds = a.lds_scratch + scratch;
   auto kern = rows_kernel<D, RT, W, KB, QW, PK, WT>;
-  if (lds > 65536 - 4096) {  // above the default LDS limit, with the static part
+  if (lds > 65536) {  // above the default dynamic LDS limit
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
