@@ -506,8 +506,13 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
 
     f4 acc[RT][VM];
     float m[RT], l[RT];
-    float vlim = 0.0f, vs = 1.0f;  // bound of the value norms so far, their scale
-    uint16_t vbits = 0;            // the largest binary16 below the bound, as bits
+    // The reference m of a row: weights are 2^(score - m).  It is the running
+    // maximum less `head`, which keeps weight times value norm within binary16:
+    // norms so far are below 2^(7 - head), so the maximum's weight 2^head times a
+    // norm is at most 2^7, and a score may exceed the maximum by 2^kLag before the
+    // reference moves.
+    float vlim = 0.0f, head = 0.0f;  // bound of the value norms so far
+    uint16_t vbits = 0;              // the largest binary16 below the bound, as bits
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       m[t] = -INFINITY;
@@ -644,9 +649,15 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           s[0][0][e] = own + ror8(other);
         }
       }
+      // (one tile scales its scores, and the norms stay binary16 operands; more
+      // tiles share the scaled norms)
       float nk[NE];
 #pragma unroll
-      for (int i = 0; i < NE; ++i) nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1] * ks;
+      for (int i = 0; i < NE; ++i) {
+        nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1];
+        if constexpr (RT > 1) nk[i] *= ks;
+        else s[0][i >> 2][i & 3] *= ks;
+      }
       float nv[NE];
 #pragma unroll
       for (int i = 0; i < NE; ++i)
@@ -712,7 +723,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         const int at = tb + acc_tok;
         if ((c & 1) == 0 && at < tot) a.acc[base + at] = x.acc + x1;
       } else {
-        // ---- the scale of the weights: p nu vs <= 2^(kLag + 7) for the norms so far
+        // ---- larger value norms than so far: the references move
         typedef uint16_t u2 __attribute__((ext_vector_type(2)));
         u2 most_v = __builtin_bit_cast(u2, x.nv[0]);
 #pragma unroll
@@ -728,18 +739,19 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           if (top > vlim) {  // (uniform)
             int e2 = 0;
             frexpf(top, &e2);
-            const float now = ldexpf(1.0f, 7 - e2), f = now / vs;
+            const float d = (float)(7 - e2) - head, f = __builtin_amdgcn_exp2f(d);
             vlim = ldexpf(1.0f, e2);
             vbits = (uint16_t)(__builtin_bit_cast(uint16_t, (_Float16)vlim) - 1);
-            vs = now;
+            head = (float)(7 - e2);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
+            for (int t = 0; t < RT; ++t) {
+              m[t] -= d;  // (-inf stays)
+              l[t] *= f;
 #pragma unroll
               for (int mu = 0; mu < VM; ++mu) acc[t][mu] *= f;
+            }
           }
         }
-#pragma unroll
-        for (int i = 0; i < NE; ++i) nv[i] *= vs;
         // ---- a score far above its row's maximum, or (not a number or infinite)
         //      no finite one yet: the maxima move
         bool over = false;
@@ -750,7 +762,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           most[t] = fmaxf(fmaxf(p[t][0], p[t][1]), fmaxf(p[t][2], p[t][3]));
           if constexpr (!PK)
             most[t] = fmaxf(most[t], fmaxf(fmaxf(p[t][4], p[t][5]), fmaxf(p[t][6], p[t][7])));
-          over |= !(most[t] <= kLag);
+          over |= !(most[t] <= head + kLag);
         }
         if (__any(over)) {
 #pragma unroll
@@ -765,7 +777,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
             }
             mh = xmax(xmax(mh, 16), 32);
             if constexpr (PK) mh = xmax(mh, 8);
-            const float m_new = first ? mh : m[t] + fmaxf(mh, 0.0f);
+            const float m_new = first ? mh - head : m[t] + fmaxf(mh - head, 0.0f);
             const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
             m[t] = m_new;
             against(t, m_new == -INFINITY ? 0.0f : m_new, p[t]);  // (scores of -inf have weight 0)
@@ -861,7 +873,6 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
     if constexpr (!WT) {
       // ---- the wavefronts' states: the upper four are taken into the lower
       //      four's registers, whose states all threads then combine into the record
-      const float vi = ci / vs;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         l[t] = xsum(xsum(l[t], 16), 32);
@@ -873,7 +884,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
             for (int e = 0; e < 4; ++e)
               acc[t][mu][e] += __shfl_xor(acc[t][mu][e], 32, 64);
           }
-          acc[t][mu] *= vi;
+          acc[t][mu] *= ci;
         }
       }
       float* slot = scratch + (wave & 3) * state_floats(D, RT) + lane;
