@@ -67,18 +67,18 @@ __device__ __forceinline__ uint32_t key_of(float a) {
 // Selection of the kept rows.  The key of the last kept one is found digit by
 // digit (11, 11 and 10 bits) from histograms; its equals are taken from the
 // lowest index on, so a row's place is the number of larger keys and of taken
-// equals before it.  One workgroup per group does all of it in one launch; few
-// long groups are cut into slices, a workgroup each, whose histograms meet in
-// the workspace between launches.  What bounds it: the LDS atomics of the
-// histograms (attention weights share few exponents, so a digit's bins are kept
-// in kCopies copies by lane) and the scans of the last pass; the accumulators
-// are read four times, three of them from L2.
+// equals before it.  Up to 32768 tokens, one workgroup per group reads them once,
+// keeps the keys in registers and does all of it in one launch; longer groups are
+// cut into slices, a workgroup each, whose histograms meet in the workspace
+// between four launches.  What bounds it: the LDS atomics of the histograms
+// (attention weights share few exponents, so the bins are kept in kCopies copies
+// by lane) and the passes' barriers.
 constexpr int kSel = 1024;      // threads
 constexpr int kBins = 2048;
 constexpr int kCopies = 4;
-constexpr int kEach = 8;        // consecutive tokens of a thread in the last pass
-constexpr int kSlice = 16384;   // tokens of a slice, at least
+constexpr int kSlice = 8192;    // tokens of a slice, at least
 constexpr int kSlices = 64;     // slices of a group, at most
+constexpr int kMaxKeys = 32;    // keys of a thread
 
 struct Sel {
   const float* acc;
@@ -87,8 +87,10 @@ struct Sel {
   int keep, recent;
   int32_t* new_lens;
   int32_t* index;
-  int slices, slice_len;  // (one launch: 1 and T_stride)
-  int32_t* hist;          // [digit][group][slice][kBins]
+  int slices, slice_len;
+  int32_t* hist;   // [digit][group][slice][kBins]
+  int32_t* found;  // [digit][group][2]: the digits so far, the keys still needed
+  int32_t* ahead;  // [group][slice]: larger keys of a slice, by the first two digits
   int n_groups;
 };
 __device__ __forceinline__ int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
@@ -96,26 +98,26 @@ __device__ __forceinline__ uint32_t digit_of(uint32_t u, int d) {
   return (u >> digit_shift(d)) & (d == 2 ? 1023u : 2047u);
 }
 
-// exclusive sums over the block of v; *total the whole sum
-__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* tmp, uint32_t* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t x = v;
+// sums over the wavefront of v up to and with this lane
+__device__ __forceinline__ uint32_t wave_upto(uint32_t v) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
+    const uint32_t y = __shfl_up(v, o, 64);
+    if (lane >= o) v += y;
   }
-  if (lane == 63) tmp[wave] = x;
+  return v;
+}
+// exclusive sums over the block of v
+__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* tmp) {
+  const int wave = threadIdx.x >> 6;
+  const uint32_t x = wave_upto(v);
+  if ((threadIdx.x & 63) == 63) tmp[wave] = x;
   __syncthreads();
-  uint32_t before = 0, all = 0;
+  uint32_t before = 0;
 #pragma unroll
-  for (int i = 0; i < kSel / 64; ++i) {
-    const uint32_t y = tmp[i];
-    before += i < wave ? y : 0;
-    all += y;
-  }
+  for (int i = 0; i < kSel / 64; ++i) before += i < wave ? tmp[i] : 0;
   __syncthreads();
-  *total = all;
   return before + x - v;
 }
 
@@ -125,27 +127,21 @@ struct Found {
   int need;      // how many keys with these digits are kept
 };
 
-// counts of digit d over tokens [t0, t1) whose higher digits are f.top's, into
-// bins [kBins][kCopies] of LDS
-__device__ void count_digit(const float* a, int t0, int t1, int d, const Found& f, int* bins) {
+__device__ __forceinline__ void clear_bins(int* bins) {
   for (int i = threadIdx.x; i < kBins * kCopies; i += kSel) bins[i] = 0;
   __syncthreads();
+}
+// counts key u's digit d if its higher digits are f.top's
+__device__ __forceinline__ void count_key(uint32_t u, int d, const Found& f, int* bins) {
   const int sh = digit_shift(d) + (d == 2 ? 10 : 11);
-  auto add = [&](float v) {
-    const uint32_t u = key_of(v);
-    if (d == 0 || (u >> sh) == (f.top >> sh))
-      atomicAdd(&bins[digit_of(u, d) * kCopies + (threadIdx.x & (kCopies - 1))], 1);
-  };
-  int t = t0 + threadIdx.x;
-  for (; t + 3 * kSel < t1; t += 4 * kSel) {  // four loads at once
-    float v[4];
+  if (d == 0 || (u >> sh) == (f.top >> sh))
+    atomicAdd(&bins[digit_of(u, d) * kCopies + (threadIdx.x & (kCopies - 1))], 1);
+}
+__device__ __forceinline__ int bin_count(const int* bins, int b) {
+  int n = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[t + i * kSel];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) add(v[i]);
-  }
-  for (; t < t1; t += kSel) add(a[t]);
-  __syncthreads();
+  for (int i = 0; i < kCopies; ++i) n += bins[b * kCopies + i];
+  return n;
 }
 
 // the digit at which the counts from the largest bin down reach f.need;
@@ -154,8 +150,7 @@ template <typename COUNT>
 __device__ void find_digit(int d, COUNT count, uint32_t* tmp, int* found, Found* f) {
   const int b1 = kBins - 1 - 2 * (int)threadIdx.x, b0 = b1 - 1;  // this thread's bins
   const int c1 = count(b1), c0 = count(b0);
-  uint32_t all;
-  const int before = (int)block_before((uint32_t)(c1 + c0), tmp, &all);
+  const int before = (int)block_before((uint32_t)(c1 + c0), tmp);
   if (before < f->need && f->need <= before + c1 + c0) {
     const bool upper = f->need <= before + c1;
     found[0] = upper ? b1 : b0;
@@ -165,35 +160,6 @@ __device__ void find_digit(int d, COUNT count, uint32_t* tmp, int* found, Found*
   f->top |= (uint32_t)found[0] << digit_shift(d);
   f->need = found[1];
   __syncthreads();
-}
-
-// places of the kept tokens of [t0, t1): `larger` and `equal` keys before t0
-__device__ void emit(const float* a, int t0, int t1, int old, bool any, const Found& f, int larger,
-                     int equal, uint32_t* tmp, int32_t* out) {
-  for (int c0 = t0; c0 < t1; c0 += kSel * kEach) {
-    const int t = c0 + threadIdx.x * kEach;
-    uint32_t gt = 0, eq = 0;  // bit i: token t + i
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const bool is_old = any && t + i < old;
-      const uint32_t u = is_old && t + i < t1 ? key_of(a[t + i]) : 0;
-      const bool in = t + i < t1;
-      if (in && (t + i >= old || (is_old && u > f.top))) gt |= 1u << i;
-      if (in && is_old && u == f.top) eq |= 1u << i;
-    }
-    uint32_t all;  // (at most kSel kEach = 2^13 of each)
-    const uint32_t before = block_before(__popc(gt) | (uint32_t)__popc(eq) << 16, tmp, &all);
-    int g = larger + (int)(before & 0xFFFFu), e = equal + (int)(before >> 16);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const bool is_gt = gt >> i & 1, is_eq = eq >> i & 1;
-      if (is_gt || (is_eq && e < f.need)) out[g + min(e, f.need)] = t + i;
-      g += is_gt;
-      e += is_eq;
-    }
-    larger += (int)(all & 0xFFFFu);
-    equal += (int)(all >> 16);
-  }
 }
 
 // The simple outcomes: a bad length, or everything kept.  True if done.
@@ -209,86 +175,189 @@ __device__ bool whole_group(const Sel& p, int g, int len, int32_t* out, bool fir
   return bad || len <= p.keep;
 }
 
+// Keys of tokens t0 .. t0 + 1024 E - 1 in registers: u[4 j + i] is token
+// t0 + 4096 j + 4 tid + i, valid below `old`.
+template <int E>
+__device__ __forceinline__ void load_keys(const float* a, int t0, int old, uint32_t (&u)[E]) {
+#pragma unroll
+  for (int j = 0; j < E / 4; ++j) {
+    const int t = t0 + 4096 * j + 4 * (int)threadIdx.x;
+    float v[4] = {};
+    if (t + 4 <= old) {
+      __builtin_memcpy(v, a + t, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t + i < old) v[i] = a[t + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[4 * j + i] = key_of(v[i]);
+  }
+}
+
+// Places of the kept ones of those tokens (below `len`), with `larger` and
+// `equal` keys before t0.  any: some of the first `old` are kept.
+template <int E>
+__device__ void emit(const uint32_t (&u)[E], int t0, int len, int old, bool any, const Found& f,
+                     int larger, int equal, uint32_t (*sums)[kSel / 64], int32_t* out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t before[E / 4];  // of a 4096-token piece: larger keys | equal keys << 16
+#pragma unroll
+  for (int j = 0; j < E / 4; ++j) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4096 * j + 4 * (int)threadIdx.x + i;
+      const bool is_old = any && t < old;
+      n += (t < len && (t >= old || (is_old && u[4 * j + i] > f.top))) ? 1u : 0u;
+      n += (is_old && u[4 * j + i] == f.top) ? 1u << 16 : 0u;
+    }
+    const uint32_t upto = wave_upto(n);
+    if (lane == 63) sums[j][wave] = upto;
+    before[j] = upto - n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < E / 4; ++j) {
+    uint32_t all = 0, mine = before[j];
+#pragma unroll
+    for (int i = 0; i < kSel / 64; ++i) {
+      const uint32_t y = sums[j][i];
+      mine += i < wave ? y : 0;
+      all += y;
+    }
+    int g = larger + (int)(mine & 0xFFFFu), e = equal + (int)(mine >> 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4096 * j + 4 * (int)threadIdx.x + i;
+      const bool is_old = any && t < old;
+      const bool gt = t < len && (t >= old || (is_old && u[4 * j + i] > f.top));
+      const bool eq = is_old && u[4 * j + i] == f.top;
+      if (gt || (eq && e < f.need)) out[g + min(e, f.need)] = t;
+      g += gt;
+      e += eq;
+    }
+    larger += (int)(all & 0xFFFFu);
+    equal += (int)(all >> 16);
+  }
+}
+
+template <int E>
 __global__ __launch_bounds__(kSel) void select_kernel(const Sel p) {
   __shared__ int bins[kBins * kCopies];
-  __shared__ uint32_t tmp[kSel / 64];
+  __shared__ uint32_t sums[E / 4][kSel / 64];
   __shared__ int found[2];
   const int g = blockIdx.x, len = p.lens[g];
   int32_t* out = p.index + (int64_t)g * p.keep;
   if (whole_group(p, g, len, out, true)) return;
-  const float* a = p.acc + g * p.T_stride;
   const int old = len - p.recent;
   const bool any = p.keep > p.recent;  // some of the first `old` are kept
   Found f{0, p.keep - p.recent};
+  uint32_t u[E];
+  load_keys<E>(p.acc + g * p.T_stride, 0, any ? old : 0, u);
   if (any) {
 #pragma unroll 1
     for (int d = 0; d < 3; ++d) {
-      count_digit(a, 0, old, d, f, bins);
-      find_digit(d, [&](int b) {
-        int n = 0;
-        for (int i = 0; i < kCopies; ++i) n += bins[b * kCopies + i];
-        return n;
-      }, tmp, found, &f);
+      clear_bins(bins);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (4096 * (i / 4) + 4 * (int)threadIdx.x + (i & 3) < old) count_key(u[i], d, f, bins);
+      __syncthreads();
+      find_digit(d, [&](int b) { return bin_count(bins, b); }, sums[0], found, &f);
     }
   }
-  emit(a, 0, len, old, any, f, 0, 0, tmp, out);
+  emit<E>(u, 0, len, old, any, f, 0, 0, sums, out);
 }
 
-// Sliced: pass d < 3 counts digit d of a slice, pass 3 writes the places.  Every
-// pass finds the digits before it again from all slices' counts.
+// Sliced: pass d < 3 counts digit d of a slice, pass 3 writes the places; a pass
+// first finds the digit that the pass before counted.
 __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
   __shared__ int bins[kBins * kCopies];
-  __shared__ uint32_t tmp[kSel / 64];
+  __shared__ uint32_t sums[1][kSel / 64];
   __shared__ int found[2];
-  __shared__ int sums[2];
-  const int g = blockIdx.x / p.slices, s = blockIdx.x % p.slices, len = p.lens[g];
+  __shared__ int total[2];
+  const int g = blockIdx.x / p.slices, s = blockIdx.x % p.slices, len = p.lens[g], tid = threadIdx.x;
   int32_t* out = p.index + (int64_t)g * p.keep;
   if (whole_group(p, g, len, out, pass == 0 && s == 0)) return;
   const float* a = p.acc + g * p.T_stride;
   const int old = len - p.recent;
   const bool any = p.keep > p.recent;
   Found f{0, p.keep - p.recent};
-  auto counts = [&](int d) { return p.hist + ((int64_t)(d * p.n_groups + g) * p.slices) * kBins; };
-  if (any) {
-    for (int d = 0; d < pass && d < 3; ++d) {
-      const int32_t* h = counts(d);
-      find_digit(d, [&](int b) {
-        int n = 0;
-        for (int i = 0; i < p.slices; ++i) n += h[(int64_t)i * kBins + b];
-        return n;
-      }, tmp, found, &f);
+  auto counts = [&](int d, int slice) {
+    return p.hist + (((int64_t)d * p.n_groups + g) * p.slices + slice) * kBins;
+  };
+  auto state = [&](int d) { return p.found + ((int64_t)d * p.n_groups + g) * 2; };
+  if (tid < 2) total[tid] = 0;
+  if (any && pass > 0) {
+    const int d = pass - 1;
+    if (d > 0) f = Found{(uint32_t)state(d - 1)[0], state(d - 1)[1]};
+    find_digit(d, [&](int b) {
+      int n = 0;
+#pragma unroll 8
+      for (int i = 0; i < p.slices; ++i) n += counts(d, i)[b];
+      return n;
+    }, sums[0], found, &f);
+    if (d < 2) {
+      // every slice's workgroup finds the same; slice 0's hands it on
+      if (s == 0 && tid == 0) {
+        state(d)[0] = (int32_t)f.top;
+        state(d)[1] = f.need;
+      }
+      int n = 0;  // this slice's keys above the digit
+      for (int b = tid; b < kBins; b += kSel)
+        if (b > (int)digit_of(f.top, d)) n += counts(d, s)[b];
+      if (n) atomicAdd(&total[0], n);
+      __syncthreads();
+      if (tid == 0) {
+        int32_t* at = p.ahead + (int64_t)g * p.slices + s;
+        *at = total[0] + (d > 0 ? *at : 0);
+      }
     }
   }
-  const int64_t from = (int64_t)s * p.slice_len, to = from + p.slice_len;
+  const int from = (int)min((int64_t)s * p.slice_len, (int64_t)len);
+  const int to = (int)min((int64_t)(s + 1) * p.slice_len, (int64_t)len);
   if (pass < 3) {
     if (!any) return;
-    count_digit(a, (int)min(from, (int64_t)old), (int)min(to, (int64_t)old), pass, f, bins);
-    int32_t* h = p.hist + ((int64_t)(pass * p.n_groups + g) * p.slices + s) * kBins;
-    for (int b = threadIdx.x; b < kBins; b += kSel) {
-      int n = 0;
-      for (int i = 0; i < kCopies; ++i) n += bins[b * kCopies + i];
-      h[b] = n;
+    clear_bins(bins);
+    const int end = min(to, old);
+    for (int t0 = from; t0 < end; t0 += 8 * kSel) {
+      uint32_t u[8];
+      load_keys<8>(a, t0, end, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (t0 + 4096 * (i / 4) + 4 * tid + (i & 3) < end) count_key(u[i], pass, f, bins);
     }
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kSel) counts(pass, s)[b] = bin_count(bins, b);
     return;
   }
   // larger and equal keys of the slices before this one
-  if (threadIdx.x < 2) sums[threadIdx.x] = 0;
-  __syncthreads();
   if (any) {
+    const int b2 = (int)digit_of(f.top, 2);
     int larger = 0;
-    for (int d = 0; d < 3; ++d) {
-      const int32_t* h = counts(d);
-      const int b0 = (int)digit_of(f.top, d);
-      for (int i = threadIdx.x; i < s * kBins; i += kSel)
-        if (i % kBins > b0) larger += h[i];
+    for (int i = tid; i < s * 1024; i += kSel)
+      if ((i & 1023) > b2) larger += counts(2, i >> 10)[i & 1023];
+    if (tid < s) {
+      larger += p.ahead[(int64_t)g * p.slices + tid];
+      atomicAdd(&total[1], counts(2, tid)[b2]);
     }
-    if (larger) atomicAdd(&sums[0], larger);
-    if ((int)threadIdx.x < s) atomicAdd(&sums[1], counts(2)[(int64_t)threadIdx.x * kBins + digit_of(f.top, 2)]);
+    if (larger) atomicAdd(&total[0], larger);
   }
   __syncthreads();
   // (recent tokens of earlier slices count as larger)
-  const int larger = sums[0] + (int)max((int64_t)0, min(from, (int64_t)len) - old);
-  emit(a, (int)min(from, (int64_t)len), (int)min(to, (int64_t)len), old, any, f, larger, sums[1], tmp, out);
+  int larger = total[0] + max(0, from - old), equal = total[1];
+  for (int t0 = from; t0 < to; t0 += 4 * kSel) {
+    uint32_t u[4];
+    load_keys<4>(a, t0, any ? min(old, to) : 0, u);
+    emit<4>(u, t0, to, old, any, f, larger, equal, sums, out);
+    // what this piece held
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < kSel / 64; ++i) all += sums[0][i];
+    larger += (int)(all & 0xFFFFu);
+    equal += (int)(all >> 16);
+    __syncthreads();
+  }
 }
 
 // Copies the kept rows, V bytes of a payload row at a time (the largest that
@@ -345,17 +414,16 @@ int launch_accept(uint8_t* kp, uint16_t* kn, uint8_t* vp, uint16_t* vn, const in
   return (int)hipGetLastError();
 }
 
-// Slices pay when the groups alone leave the chip idle and a group's passes are
-// longer than the launches that slicing adds: TODO
-static int slices_of(int64_t n_groups, int64_t T_stride) {
-  if (T_stride <= 2 * sc::kSlice || n_groups > 128) return 1;
+// One launch up to kMaxKeys keys per thread; slices beyond.
+static int slices_of(int64_t T_stride) {
+  if (T_stride <= (int64_t)sc::kSel * sc::kMaxKeys) return 1;
   const int64_t s = (T_stride + sc::kSlice - 1) / sc::kSlice;
   return (int)(s < sc::kSlices ? s : sc::kSlices);
 }
 
 size_t evict_workspace_bytes(int64_t n_groups, int64_t T_stride) {
-  const int s = slices_of(n_groups, T_stride);
-  return s == 1 ? 0 : (size_t)3 * n_groups * s * sc::kBins * 4;
+  const int s = slices_of(T_stride);
+  return s == 1 ? 0 : (size_t)n_groups * ((size_t)3 * s * sc::kBins + 6 + s) * 4;
 }
 
 int launch_evict(const uint8_t* kp, const uint16_t* kn, const uint8_t* vp, const uint16_t* vn,
@@ -364,12 +432,20 @@ int launch_evict(const uint8_t* kp, const uint16_t* kn, const uint8_t* vp, const
                  uint16_t* vno, float* acco, int32_t* new_lens, int32_t* index, void* ws,
                  void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int slices = slices_of(n_groups, T_stride);
-  const sc::Sel p{acc, lens, T_stride, keep, recent, new_lens, index, slices,
-                  (int)((T_stride + slices - 1) / slices), static_cast<int32_t*>(ws), (int)n_groups};
+  const int slices = slices_of(T_stride);
+  // (whole pieces of load_keys, so that slices start at even places of them)
+  const int slice_len = (int)(((T_stride + slices - 1) / slices + 4095) / 4096 * 4096);
+  int32_t* hist = static_cast<int32_t*>(ws);
+  const int64_t n_hist = (int64_t)3 * n_groups * slices * sc::kBins;
+  const sc::Sel p{acc, lens, T_stride, keep, recent, new_lens, index, slices, slice_len, hist,
+                  hist + n_hist, hist + n_hist + 6 * n_groups, (int)n_groups};
   hipError_t e = hipSuccess;
   if (slices == 1) {
-    hipLaunchKernelGGL(sc::select_kernel, dim3((unsigned)n_groups), dim3(sc::kSel), 0, st, p);
+    auto kern = T_stride <= 4 * sc::kSel    ? sc::select_kernel<4>
+                : T_stride <= 8 * sc::kSel  ? sc::select_kernel<8>
+                : T_stride <= 16 * sc::kSel ? sc::select_kernel<16>
+                                            : sc::select_kernel<sc::kMaxKeys>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)n_groups), dim3(sc::kSel), 0, st, p);
     if ((e = hipGetLastError()) != hipSuccess) return (int)e;
   } else {
     for (int pass = 0; pass < 4; ++pass) {
