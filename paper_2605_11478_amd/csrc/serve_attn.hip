@@ -89,8 +89,10 @@ struct Args {
 __host__ __device__ constexpr int rec_floats(int D, int RT) { return 16 * RT * (D + 2); }
 constexpr int tile_stride(int D) { return 2 * D + 16; }  // bytes of a staged row: spreads the banks
 constexpr int state_regs(int D, int RT) { return RT * (D / 16) * 4 + 2 * RT; }
-constexpr int kReg = 68;  // floats between a state's registers in LDS: spreads the banks
-constexpr int state_floats(int D, int RT) { return state_regs(D, RT) * kReg; }
+// floats between a state's registers in LDS: spreads the banks.  Packed rows end in
+// half the lanes, which lets two workgroups with 64 KB tables share a compute unit.
+constexpr int reg_floats(bool PK) { return PK ? 36 : 68; }
+constexpr int state_floats(int D, int RT, bool PK) { return state_regs(D, RT) * reg_floats(PK); }
 // the queries' low parts: in registers for one row tile, else in LDS (they are 32
 // of 256 registers at four tiles, where the unit loop spilled without)
 constexpr int ops_bytes(int D, int RT) { return RT > 1 ? RT * (D / 32) * 1024 : 0; }
@@ -887,16 +889,17 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
           acc[t][mu] *= ci;
         }
       }
-      float* slot = scratch + (wave & 3) * state_floats(D, RT) + lane;
+      float* slot = scratch + (wave & 3) * state_floats(D, RT, PK) + (PK ? lane & 31 : lane);
       auto put = [&]() {
+        if (PK && lane >= 32) return;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          slot[(2 * t) * kReg] = m[t];
-          slot[(2 * t + 1) * kReg] = l[t];
+          slot[(2 * t) * reg_floats(PK)] = m[t];
+          slot[(2 * t + 1) * reg_floats(PK)] = l[t];
 #pragma unroll
           for (int mu = 0; mu < VM; ++mu)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) slot[(2 * RT + (t * VM + mu) * 4 + e) * kReg] = acc[t][mu][e];
+            for (int e = 0; e < 4; ++e) slot[(2 * RT + (t * VM + mu) * 4 + e) * reg_floats(PK)] = acc[t][mu][e];
         }
       };
       lds_barrier();  // (the scratch is free)
@@ -905,7 +908,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
       if (wave < 4) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          const float mo = slot[(2 * t) * kReg], lo = slot[(2 * t + 1) * kReg];
+          const float mo = slot[(2 * t) * reg_floats(PK)], lo = slot[(2 * t + 1) * reg_floats(PK)];
           const float mx = fmaxf(m[t], mo), sub = mx == -INFINITY ? 0.0f : mx;
           const float f = __builtin_amdgcn_exp2f(m[t] - sub), fo = __builtin_amdgcn_exp2f(mo - sub);
           m[t] = mx;
@@ -915,7 +918,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
             const float fr = __shfl(f, 4 * g16 + e, 64), fro = __shfl(fo, 4 * g16 + e, 64);
 #pragma unroll
             for (int mu = 0; mu < VM; ++mu)
-              acc[t][mu][e] = acc[t][mu][e] * fr + slot[(2 * RT + (t * VM + mu) * 4 + e) * kReg] * fro;
+              acc[t][mu][e] = acc[t][mu][e] * fr + slot[(2 * RT + (t * VM + mu) * 4 + e) * reg_floats(PK)] * fro;
           }
         }
         put();
@@ -925,11 +928,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
       // is a different number for every segment
       float* r = a.rec + (item + b) * rec_floats(D, RT);
       if (tid < ROWS) {
-        const float* st = scratch + 2 * (tid >> 4) * kReg + (tid & 15);
+        const float* st = scratch + 2 * (tid >> 4) * reg_floats(PK) + (tid & 15);
         float mw[4], lw = 0.0f, mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          mw[i] = st[i * state_floats(D, RT)];
+          mw[i] = st[i * state_floats(D, RT, PK)];
           mx = fmaxf(mx, mw[i]);
         }
         const float sub = mx == -INFINITY ? 0.0f : mx;
@@ -937,7 +940,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         for (int i = 0; i < 4; ++i) {
           const float f = __builtin_amdgcn_exp2f(mw[i] - sub);
           fac[i * ROWS + tid] = f;
-          lw = fmaf(st[i * state_floats(D, RT) + kReg], f, lw);
+          lw = fmaf(st[i * state_floats(D, RT, PK) + reg_floats(PK)], f, lw);
         }
         r[tid] = mx;
         r[ROWS + tid] = lw;
@@ -952,10 +955,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
         // row 16 t + 4 g + e, dim 4 ((c / 4) VM + mu) + c % 4: register (t, mu, e) of lane 16 g + c
         const int row = x / D, dim = x % D;
         const int reg = 2 * RT + ((row >> 4) * VM + (dim >> 2) % VM) * 4 + (row & 3);
-        const float* st = scratch + reg * kReg + 16 * ((row >> 2) & 3) + 4 * (dim / (4 * VM)) + (dim & 3);
+        const float* st = scratch + reg * reg_floats(PK) + 16 * ((row >> 2) & 3) + 4 * (dim / (4 * VM)) + (dim & 3);
         float v = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v = fmaf(st[i * state_floats(D, RT)], fac[i * ROWS + row], v);
+        for (int i = 0; i < 4; ++i) v = fmaf(st[i * state_floats(D, RT, PK)], fac[i * ROWS + row], v);
         r[2 * ROWS + x] = v;
       }
     }
@@ -1118,14 +1121,12 @@ static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
   return y;
 }
 
-// The main launch of a code; *wgs: as many workgroups as run at once, two per
-// compute unit where registers and LDS allow, or one per run if those are fewer.
 template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
 static hipError_t launch_rows(Args a, int table, int wgs, hipStream_t st) {
   a.lds_small = table;
   a.lds_ops = table + (2 * kWaves + 4 * 16 * RT) * 4;
   a.lds_scratch = a.lds_ops + ops_bytes(D, RT);
-  size_t scratch = WT ? 0 : (size_t)4 * state_floats(D, RT) * 4;
+  size_t scratch = WT ? 0 : (size_t)4 * state_floats(D, RT, PK) * 4;
   const size_t tiles = QW == 0 ? (size_t)kWaves * 2 * kStep * tile_stride(D) : 0;
   if (tiles > scratch) scratch = tiles;
   const size_t lds = a.lds_scratch + scratch;
@@ -1156,8 +1157,10 @@ static hipError_t launch_kind(const Args& a, const Kind& x, int wgs, hipStream_t
 template <int D, int RT, bool PK>
 static int launch_tile(const ServeAttn& v, const Args& a, const Layout& y, const Kind& x, hipStream_t st) {
   const int64_t items = v.n_groups * y.tiles;
+  // as many workgroups as run at once, two per compute unit where registers and
+  // LDS allow, or one per run if those are fewer
   const int64_t most = items * ((v.T_stride + kRun - 1) / kRun);
-  int64_t wgs = PK && D == 64 && x.qw > 0 && x.lds <= 32768 ? kMaxWgs : kMaxWgs / 2;
+  int64_t wgs = PK && D == 64 && x.qw > 0 ? kMaxWgs : kMaxWgs / 2;
   if (wgs > most) wgs = most;
   hipError_t e = hipSuccess;
   if (wgs > 0) {
