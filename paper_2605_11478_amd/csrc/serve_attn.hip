@@ -299,7 +299,7 @@ struct Unit {
 // its unit, keys and then values, into a tile of its own and reads the operands
 // from there.
 template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
-__global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_kernel(const Args a) {
+__global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) void rows_kernel(const Args a) {
   constexpr int NB = D / 4, Q = NB / 4;  // 4-dim rows, of them per quarter
   constexpr int KS = D / 32, VM = D / 16;
   constexpr int ROWS = 16 * RT;
@@ -532,38 +532,56 @@ __global__ __launch_bounds__(kThreads, D == 64 && (PK || WT) ? 4 : 2) void rows_
     auto stage = [&](const uint8_t* pay, int tb) -> bool {
       bool any = false;
       const int nt = min(kStep, tot - tb);
-      for (int x = lane; x < kStep * NB; x += 64) {
-        const int tok = x / NB, p = x % NB;
-        const uint8_t* row = pay + (base + tb + min(tok, nt - 1)) * P;
-        const int n = a.k >= 4 ? 1 : 4 / a.k;  // codewords of the piece
-        const int bit = (a.k >= 4 ? 4 * p / a.k : p * n) * w;
-        uint64_t bits = 0;
-        if (P >= 8) {
-          const int st = min(bit >> 3, P - 8);
-          __builtin_memcpy(&bits, row + st, 8);
-          bits >>= bit - 8 * st;
-        } else {
-          for (int i = 0; i < P; ++i) bits |= (uint64_t)row[i] << (8 * i);
-          bits >>= bit;
+      const int n = a.k >= 4 ? 1 : 4 / a.k;  // codewords of a 4-dim piece
+      const uint32_t ones = (1u << w) - 1;
+      // pieces in batches whose loads are all in flight at once: payloads, then rows
+      constexpr int kBatch = RT == 1 ? 8 : 4;
+#pragma unroll 1
+      for (int x0 = lane; x0 < kStep * NB; x0 += 64 * kBatch) {
+        uint64_t bits[kBatch];
+        float cv[kBatch][4];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int x = x0 + 64 * i, p = x % NB;
+          const uint8_t* row = pay + (base + tb + min(x / NB, nt - 1)) * P;
+          const int bit = (a.k >= 4 ? 4 * p / a.k : p * n) * w;
+          const int at = bit >> 3;
+          if (P >= 8) {  // (a piece's codewords and the shift take at most 63 bits)
+            const int st = min(at, P - 8);
+            __builtin_memcpy(&bits[i], row + st, 8);
+            bits[i] >>= bit - 8 * st;
+          } else {       // (at most 21 bits: rows of up to 7 bytes)
+            bits[i] = (row[at] | (uint32_t)row[min(at + 1, P - 1)] << 8 |
+                       (uint32_t)row[min(at + 2, P - 1)] << 16) >> (bit & 7);
+          }
         }
-        const uint64_t ones = (1ull << w) - 1;
-        float cv[4];
         if (a.k >= 4) {
-          __builtin_memcpy(cv, a.C + (size_t)(bits & ones) * a.k + 4 * p % a.k, 16);
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i)
+            __builtin_memcpy(cv[i], a.C + (size_t)((uint32_t)bits[i] & ones) * a.k + 4 * ((x0 + 64 * i) % NB) % a.k, 16);
         } else if (a.k == 2) {
-          __builtin_memcpy(cv, a.C + 2 * (size_t)(bits & ones), 8);
-          __builtin_memcpy(cv + 2, a.C + 2 * (size_t)(bits >> w & ones), 8);
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            __builtin_memcpy(cv[i], a.C + 2 * ((uint32_t)bits[i] & ones), 8);
+            __builtin_memcpy(cv[i] + 2, a.C + 2 * ((uint32_t)(bits[i] >> w) & ones), 8);
+          }
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) cv[e] = a.C[bits >> (e * w) & ones];
+          for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cv[i][e] = a.C[(uint32_t)(bits[i] >> (e * w)) & ones];
         }
-        uint32_t hi[2], lo[2];
-        split2(cv[0] * cs, cv[1] * cs, &hi[0], &lo[0]);
-        split2(cv[2] * cs, cv[3] * cs, &hi[1], &lo[1]);
-        any |= ((lo[0] | lo[1]) & 0x7FFF7FFFu) != 0;
-        unsigned char* to = tile + tok * tile_stride(D) + 8 * p;
-        __builtin_memcpy(to, hi, 8);
-        __builtin_memcpy(to + kStep * tile_stride(D), lo, 8);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int x = x0 + 64 * i;
+          uint32_t hi[2], lo[2];
+          split2(cv[i][0] * cs, cv[i][1] * cs, &hi[0], &lo[0]);
+          split2(cv[i][2] * cs, cv[i][3] * cs, &hi[1], &lo[1]);
+          any |= ((lo[0] | lo[1]) & 0x7FFF7FFFu) != 0;
+          unsigned char* to = tile + x / NB * tile_stride(D) + 8 * (x % NB);
+          __builtin_memcpy(to, hi, 8);
+          __builtin_memcpy(to + kStep * tile_stride(D), lo, 8);
+        }
       }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
