@@ -67,6 +67,7 @@ struct Args {
   const uint8_t* vp;
   const uint16_t* vn;
   const int32_t* lens;
+  int32_t* now;       // the lengths as the ranges were made from (-1: bad), for the other launches
   const uint64_t* masks;
   int64_t mask_stride;
   int n_groups, M, G, rows, tiles;  // rows of a group, row tiles of a group
@@ -97,11 +98,12 @@ constexpr int state_floats(int D, int RT, bool PK) { return state_regs(D, RT) * 
 // of 256 registers at four tiles, where the unit loop spilled without)
 constexpr int ops_bytes(int D, int RT) { return RT > 1 ? RT * (D / 32) * 1024 : 0; }
 
-// runs of units of a group; none for a bad length
-__device__ __forceinline__ int runs_of(const Args& a, int g) {
-  const int len = a.lens[g];
-  if (len < 0 || len > a.T_stride - a.M) return 0;
-  return (len + a.M + kRun - 1) / kRun;
+// runs of units of a group of this length (-1: bad, none)
+__device__ __forceinline__ int runs_of(const Args& a, int len) {
+  return len < 0 ? 0 : (len + a.M + kRun - 1) / kRun;
+}
+__device__ __forceinline__ int checked(const Args& a, int len) {
+  return len < 0 || len > a.T_stride - a.M ? -1 : len;
 }
 
 // two values as binary16 pairs: high parts, and the rest taken from their bits
@@ -158,7 +160,11 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
     uint64_t mine = 0;
     for (int i = 0; i < per; ++i) {
       const int g = tid * per + i;
-      if (g < a.n_groups) mine += runs_of(a, g);
+      if (g < a.n_groups) {
+        const int len = checked(a, a.lens[g]);
+        a.now[g] = len;
+        mine += runs_of(a, len);
+      }
     }
     mine *= a.tiles;
     uint64_t upto = mine;
@@ -190,7 +196,7 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
         uint64_t off = from - (t > 0 ? sums[t - 1] : 0);
         int g = t * per;
         for (;; ++g) {  // (ends: the thread's groups hold `from`)
-          const uint64_t v = (uint64_t)runs_of(a, g) * a.tiles;
+          const uint64_t v = (uint64_t)runs_of(a, a.now[g]) * a.tiles;
           if (off < v) break;
           off -= v;
         }
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
   }
   const int64_t g = blockIdx.x / a.tiles;
   const int row0 = (int)(blockIdx.x % a.tiles) * ROWS;
-  if (runs_of(a, (int)g) == 0) return;
+  if (runs_of(a, checked(a, a.lens[g])) == 0) return;
   const int c = lane & 15, g16 = lane >> 4;
   const int live = (min(ROWS, a.rows - row0) + 15) / 16;
   float top = 0.0f;
@@ -986,7 +992,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
     if (off == 0 && !first) {  // the next group that holds units (64 at a time)
       for (;;) {
         const int at = g + lane;
-        const uint64_t some = __ballot(at < a.n_groups && runs_of(a, min(at, a.n_groups - 1)) > 0);
+        const uint64_t some = __ballot(at < a.n_groups && runs_of(a, a.now[min(at, a.n_groups - 1)]) > 0);
         if (some) {
           g += __builtin_ctzll(some);
           break;
@@ -995,7 +1001,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
         if (g >= a.n_groups) return;  // (not reached: units are left)
       }
     }
-    const int len = a.lens[g], runs = runs_of(a, g);
+    const int len = a.now[g], runs = runs_of(a, len);
     const int rt0 = a.tiles == 1 ? 0 : (int)((uint32_t)off / (uint32_t)runs);
     const int r0 = (int)(off - (uint64_t)rt0 * runs);
     const int take = (int)(left < (uint64_t)(runs - r0) ? left : (uint64_t)(runs - r0));
@@ -1015,7 +1021,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
 template <int D>
 __global__ __launch_bounds__(256) void merge_kernel(
     const float* __restrict__ rec, const int32_t* __restrict__ bounds,
-    const int32_t* __restrict__ lens, int64_t T_stride, int M, int rows, int tiles, int tile_rows,
+    const int32_t* __restrict__ now, int M, int rows, int tiles, int tile_rows,
     const float* __restrict__ R, float* __restrict__ stat, float* __restrict__ out) {
   constexpr int HB = 256 / D, RI = D / HB;  // stripes = rows of the block
   __shared__ float ar[HB][D];
@@ -1024,8 +1030,8 @@ __global__ __launch_bounds__(256) void merge_kernel(
   const int64_t g = blockIdx.x / blocks;
   const int hr = threadIdx.x / D, dim = threadIdx.x % D;
   const int row = (int)(blockIdx.x % blocks) * HB + hr;
-  const int len = lens[g];
-  const bool bad = len < 0 || len > T_stride - M;
+  const int len = now[g];
+  const bool bad = len < 0;
   float pi[RI];
 #pragma unroll
   for (int i = 0; i < RI; ++i) pi[i] = R[(hr * RI + i) * D + dim];
@@ -1119,7 +1125,7 @@ constexpr int kMaxWgs = 512;
 struct Layout {
   bool packed;
   int tile, tiles;  // rows of a tile, tiles of a group
-  size_t off_qs, off_start, off_top, off_bounds, off_stat, off_rec, total;
+  size_t off_qs, off_now, off_start, off_top, off_bounds, off_stat, off_rec, total;
 };
 static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
   Layout y{};
@@ -1130,7 +1136,8 @@ static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
   const size_t items = (size_t)n_groups * y.tiles;
   auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
   y.off_qs = al(items * (y.tile / 16) * (s.d / 32) * (y.packed ? 1 : 2) * 1024);
-  y.off_start = al(y.off_qs + items * 4);
+  y.off_now = al(y.off_qs + items * 4);
+  y.off_start = al(y.off_now + (size_t)n_groups * 4);
   y.off_top = al(y.off_start + kMaxWgs * sizeof(Start));
   y.off_bounds = al(y.off_top + kTop * 4);
   y.off_stat = al(y.off_bounds + items * 8);
@@ -1166,7 +1173,8 @@ static hipError_t launch_kind(const Args& a, const Kind& x, int wgs, hipStream_t
   } else {
     FIBQ_SV(8, 1, 2) FIBQ_SV(12, 1, 3)
   }
-  FIBQ_SV(0, 1, 2) FIBQ_SV(0, 2, 2) FIBQ_SV(0, 4, 2) FIBQ_SV(0, 1, 0)
+  if constexpr (D == 128) { FIBQ_SV(0, 4, 2) }  // (k = 16 at d = 64 has rows of less than 8 bytes)
+  FIBQ_SV(0, 1, 2) FIBQ_SV(0, 2, 2) FIBQ_SV(0, 1, 0)
 #undef FIBQ_SV
   return hipErrorInvalidValue;
 }
@@ -1180,16 +1188,15 @@ static int launch_tile(const ServeAttn& v, const Args& a, const Layout& y, const
   const int64_t most = items * ((v.T_stride + kRun - 1) / kRun);
   int64_t wgs = PK && D == 64 && x.qw > 0 ? kMaxWgs : kMaxWgs / 2;
   if (wgs > most) wgs = most;
-  hipError_t e = hipSuccess;
-  if (wgs > 0) {
-    hipLaunchKernelGGL((prep_kernel<D, RT, PK>), dim3((unsigned)(items + 1 + (x.qw == 0 ? kTop : 0))),
-                       dim3(256 * (RT > 1 ? 2 : 1)), 0, st, a, (int)wgs);
-    if ((e = hipGetLastError()) != hipSuccess) return (int)e;
-    if ((e = launch_kind<D, RT, PK, false>(a, x, (int)wgs, st)) != hipSuccess) return (int)e;
-  }
+  // (also without any row in the cache: the merge goes by the lengths that prep leaves)
+  hipLaunchKernelGGL((prep_kernel<D, RT, PK>), dim3((unsigned)(items + 1 + (x.qw == 0 ? kTop : 0))),
+                     dim3(256 * (RT > 1 ? 2 : 1)), 0, st, a, (int)(wgs > 0 ? wgs : 1));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return (int)e;
+  if (wgs > 0 && (e = launch_kind<D, RT, PK, false>(a, x, (int)wgs, st)) != hipSuccess) return (int)e;
   const int64_t blocks = v.n_groups * ((a.rows + 256 / D - 1) / (256 / D));
   hipLaunchKernelGGL(merge_kernel<D>, dim3((unsigned)blocks), dim3(256), 0, st, a.rec, a.bounds,
-                     v.lens, v.T_stride, v.M, a.rows, y.tiles, y.tile, v.R,
+                     a.now, v.M, a.rows, y.tiles, y.tile, v.R,
                      const_cast<float*>(a.stat), v.out);
   if ((e = hipGetLastError()) != hipSuccess) return (int)e;
   if constexpr (RT == 1)
@@ -1230,6 +1237,7 @@ static int launch(const ServeAttn& v, hipStream_t st) {
   a.qscale = v.scale * 1.4426950408889634f;  // base-2 softmax
   a.ops = reinterpret_cast<h8*>(ws);
   a.qs = reinterpret_cast<float*>(ws + y.off_qs);
+  a.now = reinterpret_cast<int32_t*>(ws + y.off_now);
   a.start = reinterpret_cast<Start*>(ws + y.off_start);
   a.top = reinterpret_cast<float*>(ws + y.off_top);
   a.bounds = reinterpret_cast<int32_t*>(ws + y.off_bounds);

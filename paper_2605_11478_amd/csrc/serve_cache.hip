@@ -23,7 +23,13 @@ __global__ __launch_bounds__(256) void accept_kernel(
   __shared__ int src[64];
   const int64_t g = blockIdx.x;
   const int tid = threadIdx.x;
-  const int len = lens[g], n = n_acc[g];
+  __shared__ int read[2];  // (one reading for all threads)
+  if (tid == 0) {
+    read[0] = lens[g];
+    read[1] = n_acc[g];
+  }
+  __syncthreads();
+  const int len = read[0], n = read[1];
   bool bad = len < 0 || len > T_stride - M || n < 0 || n > min(A, M);
   if (!bad && tid < n) {
     src[tid] = path[g * A + tid];
@@ -199,7 +205,7 @@ __device__ __forceinline__ void load_keys(const float* a, int t0, int old, uint3
 // `equal` keys before t0.  any: some of the first `old` are kept.
 template <int E>
 __device__ void emit(const uint32_t (&u)[E], int t0, int len, int old, bool any, const Found& f,
-                     int larger, int equal, uint32_t (*sums)[kSel / 64], int32_t* out) {
+                     int larger, int equal, uint32_t (*sums)[kSel / 64], int32_t* out, int keep) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t before[E / 4];  // of a 4096-token piece: larger keys | equal keys << 16
 #pragma unroll
@@ -233,7 +239,10 @@ __device__ void emit(const uint32_t (&u)[E], int t0, int len, int old, bool any,
       const bool is_old = any && t < old;
       const bool gt = t < len && (t >= old || (is_old && u[4 * j + i] > f.top));
       const bool eq = is_old && u[4 * j + i] == f.top;
-      if (gt || (eq && e < f.need)) out[g + min(e, f.need)] = t;
+      // (the bound holds by the counts; it is checked, since sliced passes read
+      // accumulators that another stream might be writing)
+      const int at = g + min(e, f.need);
+      if ((gt || (eq && e < f.need)) && (uint32_t)at < (uint32_t)keep) out[at] = t;
       g += gt;
       e += eq;
     }
@@ -247,7 +256,11 @@ __global__ __launch_bounds__(kSel) void select_kernel(const Sel p) {
   __shared__ int bins[kBins * kCopies];
   __shared__ uint32_t sums[E / 4][kSel / 64];
   __shared__ int found[2];
-  const int g = blockIdx.x, len = p.lens[g];
+  __shared__ int read;  // (one reading for all threads)
+  const int g = blockIdx.x;
+  if (threadIdx.x == 0) read = p.lens[g];
+  __syncthreads();
+  const int len = read;
   int32_t* out = p.index + (int64_t)g * p.keep;
   if (whole_group(p, g, len, out, true)) return;
   const int old = len - p.recent;
@@ -266,7 +279,7 @@ __global__ __launch_bounds__(kSel) void select_kernel(const Sel p) {
       find_digit(d, [&](int b) { return bin_count(bins, b); }, sums[0], found, &f);
     }
   }
-  emit<E>(u, 0, len, old, any, f, 0, 0, sums, out);
+  emit<E>(u, 0, len, old, any, f, 0, 0, sums, out, p.keep);
 }
 
 // Sliced: pass d < 3 counts digit d of a slice, pass 3 writes the places; a pass
@@ -276,7 +289,12 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
   __shared__ uint32_t sums[1][kSel / 64];
   __shared__ int found[2];
   __shared__ int total[2];
-  const int g = blockIdx.x / p.slices, s = blockIdx.x % p.slices, len = p.lens[g], tid = threadIdx.x;
+  __shared__ int read;  // (one reading for all threads)
+  const int g = blockIdx.x / p.slices, s = blockIdx.x % p.slices, tid = threadIdx.x;
+  if (tid == 0) read = p.lens[g];
+  if (tid < 2) found[tid] = 0;
+  __syncthreads();
+  const int len = read;
   int32_t* out = p.index + (int64_t)g * p.keep;
   if (whole_group(p, g, len, out, pass == 0 && s == 0)) return;
   const float* a = p.acc + g * p.T_stride;
@@ -349,7 +367,7 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
   for (int t0 = from; t0 < to; t0 += 4 * kSel) {
     uint32_t u[4];
     load_keys<4>(a, t0, any ? min(old, to) : 0, u);
-    emit<4>(u, t0, to, old, any, f, larger, equal, sums, out);
+    emit<4>(u, t0, to, old, any, f, larger, equal, sums, out, p.keep);
     // what this piece held
     uint32_t all = 0;
 #pragma unroll

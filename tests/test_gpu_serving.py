@@ -24,7 +24,8 @@ pytestmark = pytest.mark.gpu
 CODES = [(64, 4, 256), (64, 8, 16), (64, 2, 64), (64, 2, 16), (64, 8, 64), (64, 1, 16), (64, 1, 2),
          (64, 2, 256), (64, 2, 8), (64, 4, 2), (64, 4, 512), (64, 8, 1024), (64, 16, 4096),
          (64, 32, 1024), (64, 64, 256), (64, 4, 16384), (128, 4, 4096), (128, 4, 256),
-         (128, 8, 256), (128, 16, 64), (128, 1, 16), (128, 2, 64), (128, 16, 16384)]
+         (128, 8, 256), (128, 16, 64), (128, 1, 16), (128, 2, 64), (128, 16, 16384), (128, 2, 16),
+         (128, 16, 256), (128, 4, 64), (64, 4, 64), (64, 8, 2048), (64, 16, 4), (64, 32, 2)]
 
 
 def codebook(d, k, N, seed=7, exact=True):
@@ -204,8 +205,52 @@ def test_tree_ranges(device, k, N, size, norm, scale):
     check_tree(c, q, q64, run_tree(c, q, lens, masks, scale=s), lens, masks, np.float64(np.float32(s)))
 
 
-@pytest.mark.parametrize("d,k,N", [(64, 4, 256), (64, 2, 64), (64, 1, 16)], ids=str)
-def test_tree_value_norms_that_grow(device, d, k, N):
+@pytest.mark.parametrize("M,G", [(1, 5), (3, 4), (5, 5), (19, 7)], ids=str)
+@pytest.mark.parametrize("d,k,N", [(64, 4, 256), (64, 8, 16), (64, 2, 64), (64, 1, 16), (128, 4, 256), (128, 4, 4096),
+                                   (128, 1, 4)], ids=str)
+def test_codebooks_that_binary16_does_not_hold(device, d, k, N, M, G):
+    """The residual rows' products, for every number of query rows, in the outputs and the weights."""
+    rng = np.random.default_rng(21)
+    lens = [130, 31]
+    c = Cache(d, k, N, 2, 160, device, C=codebook(d, k, N, exact=False))
+    q, q64 = queries(rng, (2, M, G, d), torch.float32, device)
+    masks = random_masks(rng, M)
+    check_tree(c, q, q64, run_tree(c, q, lens, masks), lens, masks)
+    before = torch.rand(2, 160, device=device)
+    acc = before.clone()
+    check_accum(c, q64[:, 0], run_accum(c, q[:, 0].contiguous(), lens, acc), before, acc, lens)
+
+
+@pytest.mark.parametrize("M,G", [(2, 2), (4, 4), (6, 4), (10, 8)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_tree_norms_that_are_no_numbers_where_they_are_seen(device, d, M, G):
+    """A drafted token with an infinite or NaN value norm makes the rows that see it no
+    numbers, and leaves those that do not; so does a key norm.  Another group is untouched."""
+    rng = np.random.default_rng(22)
+    lens = [61, 61]
+    c = Cache(d, 4, 256, 2, 80, device)
+    q, q64 = queries(rng, (2, M, G, d), torch.float32, device)
+    masks = np.array([1 << i for i in range(M)], dtype=np.int64)
+    a = run_tree(c, q, lens, masks)
+    for x, bits in ((3, 0x7C00), (3, 0x7E00), (1, 0x7E00)):
+        keep = c.dev[x].clone()
+        c.dev[x][1, 61 + 1] = bits
+        b = run_tree(c, q, lens, masks)
+        assert not bool(b[1, 1].isfinite().any())
+        others = [i for i in range(M) if i != 1]
+        close(b[1, others].double().cpu().numpy().reshape(-1, d), q64[1, others].reshape(-1, d),
+              c.decoded(1, 61 + M, 0), c.decoded(1, 61 + M, 1),
+              np.repeat(osv.seen_by_tree(61, masks, M)[others], G, 0))
+        assert torch.equal(a[0], b[0])
+        c.dev[x][1, 30] = bits  # in the context: every row of the group sees it
+        b = run_tree(c, q, lens, masks)
+        assert not bool(b[1].isfinite().any()) and torch.equal(a[0], b[0])
+        c.dev[x].copy_(keep)
+
+
+@pytest.mark.parametrize("M,G", [(2, 2), (4, 4), (6, 4), (10, 8)], ids=str)
+@pytest.mark.parametrize("d,k,N", [(64, 4, 256), (64, 2, 64), (64, 1, 16), (128, 4, 256)], ids=str)
+def test_tree_value_norms_that_grow(device, d, k, N, M, G):
     """Value norms that rise by powers of ten along the cache, and a zero row among them."""
     rng = np.random.default_rng(10)
     c = Cache(d, k, N, 1, 700, device)
@@ -213,8 +258,8 @@ def test_tree_value_norms_that_grow(device, d, k, N):
     h[350] = 0
     c.np[3][0] = occ.fp16_bits(h)
     c.dev[3].copy_(torch.from_numpy(c.np[3].view(np.int16)))
-    q, q64 = queries(rng, (1, 2, 2, d), torch.float32, device)
-    masks = random_masks(rng, 2)
+    q, q64 = queries(rng, (1, M, G, d), torch.float32, device)
+    masks = random_masks(rng, M)
     for length in (690, 300, 40):
         check_tree(c, q, q64, run_tree(c, q, [length], masks), [length], masks)
 
@@ -440,6 +485,22 @@ def test_evict_long(device, T, keep, recent, law):
     check_evict(c, acc, lens, keep, recent, got, keep)
 
 
+@pytest.mark.parametrize("keep,recent", [(1, 0), (1, 1), (7000, 7000), (7000, 0), (45000, 100)], ids=str)
+def test_evict_sliced_lengths(device, keep, recent):
+    """A cache of many rows whose groups are empty, short, bad, or end inside a slice."""
+    rng = np.random.default_rng(23)
+    T = 50000
+    lens = [0, 1, keep, min(keep + 1, T), 8192, 8193, 40960, T, -1, T + 1]
+    c = Cache(64, 64, 2, len(lens), T, device)
+    acc = accumulators(rng, (len(lens), T))
+    acc[:, 8190:8195] = 1e9  # equals across a slice's end
+    out = evict_out(c, keep, keep, device)
+    before = [o.clone() for o in out]
+    got = fq.evict(*c.dev, torch.from_numpy(acc).to(device),
+                   torch.tensor(lens, dtype=torch.int32, device=device), keep, recent, out=out)
+    check_evict(c, acc, lens, keep, recent, got, keep, before)
+
+
 def test_evict_refuses_overlap(device):
     c = Cache(64, 8, 16, 1, 64, device)
     acc = torch.zeros(1, 64, device=device)
@@ -641,3 +702,40 @@ def test_tensors_of_another_stream_and_kept_workspace(device):
     torch.cuda.current_stream().wait_stream(side)
     check_tree(c, q, q64, a, [290, 3], masks)
     check_tree(c, q, q64, b, [100, 296], masks)
+
+
+def test_cache_without_rows(device):
+    """T_stride = 0: a length of 0 is an empty group, any other is bad."""
+    e = lambda dt, *s: torch.empty(s, dtype=dt, device=device)
+    cache = (e(torch.uint8, 2, 0, 4), e(torch.int16, 2, 0), e(torch.uint8, 2, 0, 4), e(torch.int16, 2, 0))
+    R, C = torch.eye(64, device=device), torch.rand(16, 8, device=device)
+    lens = torch.tensor([0, 1], dtype=torch.int32, device=device)
+    q = torch.randn(2, 3, 64, device=device)
+    o = fq.attn_decode_accum(q, *cache, lens, e(torch.float32, 2, 0), 8, 16, R, C)
+    assert torch.count_nonzero(o[0]) == 0 and bool(o[1].isnan().all())
+    o = fq.attn_tree(q[:, None], *cache, lens, torch.ones(1, dtype=torch.int64, device=device), 8, 16, R, C)
+    assert bool(o.isnan().all())
+    assert fq.evict(*cache, e(torch.float32, 2, 0), lens, 4, 1)[5].tolist() == [0, -1]
+
+
+@pytest.mark.parametrize("k,N", [(8, 16), (1, 16)], ids=str)
+def test_mostly_empty_groups(device, k, N):
+    """Thousands of groups of which a few hold tokens, in runs of empty and bad ones."""
+    rng = np.random.default_rng(24)
+    n, T = 5000, 300
+    lens = np.where(rng.random(n) < 0.5, 0, -1)
+    some = [0, 1, 63, 64, 65, 2047, 4095, 4999]
+    lens[some] = [299, 1, 300, 17, 256, 257, 32, 33]
+    c = Cache(64, k, N, 1, T, device)
+    cache = [x.expand(n, *x.shape[1:]).contiguous() for x in c.dev]
+    c.np, c.n = [np.broadcast_to(a, (n, *a.shape[1:])) for a in c.np], n
+    c.dev = cache
+    q, q64 = queries(rng, (n, 2, 64), torch.float32, device)
+    before = torch.zeros(n, T, device=device)
+    acc = before.clone()
+    out = run_accum(c, q, lens.tolist(), acc)
+    check_accum(c, q64, out, before, acc, lens, groups=some)
+    none = torch.from_numpy(lens == 0).to(device)
+    bad = torch.from_numpy(lens < 0).to(device)
+    assert torch.count_nonzero(out[none]) == 0 and bool(out[bad].isnan().all())
+    assert torch.count_nonzero(acc[none | bad]) == 0
