@@ -1113,25 +1113,45 @@ static Kind kind_of(const Shape& s, Shape* as, int* pair_n) {
   return Kind{0, kb, 2, lds};
 }
 
-// Row tiles: 16 RT rows share the gathered codewords; registers hold 64 rows
-// at d = 64 and 32 at d = 128.
-static int tile_rows(int rows, int D) {
-  if (rows <= 16) return 16;
-  if (rows <= 32 || D == 128) return 32;
-  return 64;
-}
 constexpr int kMaxWgs = 512;
+
+// Row tiles: 16 RT rows share the gathered codewords; registers hold 64 rows
+// at d = 64 and 32 at d = 128.  Relative to a workgroup's run of units for 16 rows
+// (about 1 us), one for 32 and 64 rows takes 1.5 and 2.8, and an item's queries and
+// record take 5, 9 and 12.  Large tiles therefore win where a workgroup has many
+// runs (512 rows, 16 groups, 32k tokens, k = 8: 194, 154 and 140 us) or many short
+// items (512 rows, 64 groups, 512 tokens: 86, 74 and 73 us); small ones where it
+// has few (24 rows, 16 groups, 32k tokens: 26 and 31 us; 48 rows, 2048 tokens: 17.5,
+// 19 and 25 us) or where large ones pad the rows.  Over 210 sizes the choice is
+// 0.8 % behind the best on average and 15 % at most; the largest tile that the
+// rows fill was 19 % and 58 % behind.
+static int tile_rows(int64_t n_groups, int64_t T_stride, int rows, int D) {
+  const double run_cost[3] = {1.0, 1.5, 2.8}, item_cost[3] = {5.0, 9.0, 12.0};
+  const double runs = (double)((T_stride + kRun - 1) / kRun);
+  int best = 16;
+  double least = INFINITY;
+  for (int i = 0; i < (rows <= 16 ? 1 : D == 64 ? 3 : 2); ++i) {
+    const double work = (double)n_groups * ((rows + (16 << i) - 1) / (16 << i)) * runs;
+    const double each = work / (work < kMaxWgs / 2 ? work : kMaxWgs / 2);  // runs of a workgroup
+    const double cost = run_cost[i] * each + item_cost[i] * (each > runs ? each / runs : 1.0);
+    if (cost < least) {  // (no work at all: not a number)
+      least = cost;
+      best = 16 << i;
+    }
+  }
+  return best;
+}
 
 struct Layout {
   bool packed;
   int tile, tiles;  // rows of a tile, tiles of a group
   size_t off_qs, off_now, off_start, off_top, off_bounds, off_stat, off_rec, total;
 };
-static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s) {
+static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s, int tile) {
   Layout y{};
   const int rows = (M > 0 ? M : 1) * G;
   y.packed = rows <= 8;
-  y.tile = tile_rows(rows, s.d);
+  y.tile = tile;
   y.tiles = (rows + y.tile - 1) / y.tile;
   const size_t items = (size_t)n_groups * y.tiles;
   auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
@@ -1206,7 +1226,8 @@ static int launch_tile(const ServeAttn& v, const Args& a, const Layout& y, const
 
 template <int D>
 static int launch(const ServeAttn& v, hipStream_t st) {
-  const Layout y = make_layout(v.n_groups, v.M, v.G, v.s);
+  const Layout y = make_layout(v.n_groups, v.M, v.G, v.s,
+                               tile_rows(v.n_groups, v.T_stride, (v.M > 0 ? v.M : 1) * v.G, D));
   unsigned char* ws = static_cast<unsigned char*>(v.ws);
   Shape as;
   int pair_n;
@@ -1254,7 +1275,12 @@ static int launch(const ServeAttn& v, hipStream_t st) {
 }  // namespace sv
 
 size_t serve_attn_workspace_bytes(int64_t n_groups, int M, int G, const Shape& s) {
-  return sv::make_layout(n_groups, M, G, s).total;
+  size_t most = 0;  // (of every tile: which one is taken depends on T_stride)
+  for (int tile = 16; tile <= (s.d == 64 ? 64 : 32); tile *= 2) {
+    const size_t n = sv::make_layout(n_groups, M, G, s, tile).total;
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 int launch_serve_attn(const ServeAttn& a, void* stream) {
