@@ -50,6 +50,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kStep = 32;              // tokens per unit
 constexpr int kRun = kStep * kWaves;   // tokens per run of units
 constexpr int kTop = 64;               // partial maxima of a codebook
+constexpr int kMaxWgs = 512;           // workgroups of the main launch, at most
 constexpr float kLag = 8.0f;           // a maximum moves when a score exceeds it by this (log2)
 constexpr float kCs = 4096.0f;         // scale of the codebook's binary16 rows
 
@@ -1015,9 +1016,23 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
   }
 }
 
+__device__ __forceinline__ float wave_sum_dpp(float v) {
+#define FIBQ_ROR(n) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + n, 0xf, 0xf, false));
+  FIBQ_ROR(8) FIBQ_ROR(4) FIBQ_ROR(2) FIBQ_ROR(1)
+#undef FIBQ_ROR
+  const int i = __float_as_int(v);
+  return (__int_as_float(__builtin_amdgcn_readlane(i, 0)) + __int_as_float(__builtin_amdgcn_readlane(i, 16))) +
+         (__int_as_float(__builtin_amdgcn_readlane(i, 32)) + __int_as_float(__builtin_amdgcn_readlane(i, 48)));
+}
+
 // Block: 256 / D rows of a group, a thread per (row, dim).  Log-sum-exp over the
 // row's records, then o = Pi^T (acc / l) with Pi's rows in stripes over the
-// threads, loaded before the records; stat (nullable) receives m and l.
+// threads, loaded before the records; stat (nullable) receives m and l.  What
+// bounds it is latency: the launch, and the loads' round trips one behind the other.
+// More than kFew records are therefore read with the statistics of 64 at once over
+// the lanes, and sums whose loads depend on addresses only (64 records of 4 groups,
+// 16 rows, k = 4: 33 -> 26 us for the whole call); with few the exchange between
+// lanes costs more than it saves (a call of 17.0 us took 18.6).
 template <int D>
 __global__ __launch_bounds__(256) void merge_kernel(
     const float* __restrict__ rec, const int32_t* __restrict__ bounds,
@@ -1026,6 +1041,7 @@ __global__ __launch_bounds__(256) void merge_kernel(
   constexpr int HB = 256 / D, RI = D / HB;  // stripes = rows of the block
   __shared__ float ar[HB][D];
   __shared__ float part[HB][HB][D];
+  __shared__ float fac[4][kMaxWgs];  // of every wavefront: the records' factors
   const int blocks = (rows + HB - 1) / HB;
   const int64_t g = blockIdx.x / blocks;
   const int hr = threadIdx.x / D, dim = threadIdx.x % D;
@@ -1041,27 +1057,65 @@ __global__ __launch_bounds__(256) void merge_kernel(
     const int rl = row % tile_rows, reclen = tile_rows * (D + 2);
     const int first = bounds[2 * item], n = bounds[2 * item + 1] - first + 1;
     const float* r = rec + (item + first) * reclen;
-    for (int i0 = 0; i0 < n; i0 += 4) {
-      float mk[4], lk[4], xk[4];
+    constexpr int kFew = 8;
+    if (n <= kFew) {
+#pragma unroll 1
+      for (int i0 = 0; i0 < n; i0 += 4) {
+        float mk[4], lk[4], xk[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* x = r + (int64_t)min(i0 + i, n - 1) * reclen;
-        mk[i] = i0 + i < n ? x[rl] : -INFINITY;
-        lk[i] = i0 + i < n ? x[tile_rows + rl] : 0.0f;
-        xk[i] = i0 + i < n ? x[2 * tile_rows + rl * D + dim] : 0.0f;
-      }
-      const float mn = fmaxf(m, fmaxf(fmaxf(mk[0], mk[1]), fmaxf(mk[2], mk[3])));
-      const float sub = mn == -INFINITY ? 0.0f : mn;
-      const float f = __builtin_amdgcn_exp2f(m - sub);
-      l *= f;
-      s *= f;
+        for (int i = 0; i < 4; ++i) {
+          const float* x = r + (int64_t)min(i0 + i, n - 1) * reclen;
+          mk[i] = i0 + i < n ? x[rl] : -INFINITY;
+          lk[i] = i0 + i < n ? x[tile_rows + rl] : 0.0f;
+          xk[i] = i0 + i < n ? x[2 * tile_rows + rl * D + dim] : 0.0f;
+        }
+        const float mn = fmaxf(m, fmaxf(fmaxf(mk[0], mk[1]), fmaxf(mk[2], mk[3])));
+        const float sub = mn == -INFINITY ? 0.0f : mn;
+        const float f = __builtin_amdgcn_exp2f(m - sub);
+        l *= f;
+        s *= f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float fi = __builtin_amdgcn_exp2f(mk[i] - sub);
-        l = fmaf(lk[i], fi, l);
-        s = fmaf(xk[i], fi, s);
+        for (int i = 0; i < 4; ++i) {
+          const float fi = __builtin_amdgcn_exp2f(mk[i] - sub);
+          l = fmaf(lk[i], fi, l);
+          s = fmaf(xk[i], fi, s);
+        }
+        m = mn;
       }
-      m = mn;
+    } else {
+      const float* x = r + 2 * tile_rows + rl * D + dim;
+      constexpr int kBatch = 8;
+      float xk[kBatch];
+      auto fetch = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) xk[i] = x[(int64_t)min(i0 + i, n - 1) * reclen];
+      };
+      fetch(0);
+      const int lane = threadIdx.x & 63;
+      float* f = fac[threadIdx.x >> 6];
+#pragma unroll 1
+      for (int i = lane; i < n; i += 64) {
+        const float mk = r[(int64_t)i * reclen + rl], lk = r[(int64_t)i * reclen + tile_rows + rl];
+        const float mn = fmaxf(m, mk), sub = mn == -INFINITY ? 0.0f : mn;
+        l = l * __builtin_amdgcn_exp2f(m - sub) + lk * __builtin_amdgcn_exp2f(mk - sub);
+        m = mn;
+        f[i] = mk;
+      }
+      const float most = wave_max_dpp(m), sub = most == -INFINITY ? 0.0f : most;
+      l = wave_sum_dpp(l * __builtin_amdgcn_exp2f(m - sub));
+      m = most;
+#pragma unroll 1
+      for (int i = lane; i < (n + kBatch - 1) / kBatch * kBatch; i += 64)
+        f[i] = i < n ? __builtin_amdgcn_exp2f(f[i] - sub) : 0.0f;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+      for (int i0 = 0;;) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) s = i0 + i < n ? fmaf(xk[i], f[i0 + i], s) : s;
+        i0 += kBatch;
+        if (i0 >= n) break;
+        fetch(i0);
+      }
     }
   }
   ar[hr][dim] = l == 0.0f ? 0.0f : s / l;
@@ -1112,8 +1166,6 @@ static Kind kind_of(const Shape& s, Shape* as, int* pair_n) {
   }
   return Kind{0, kb, 2, lds};
 }
-
-constexpr int kMaxWgs = 512;
 
 // Row tiles: 16 RT rows share the gathered codewords; registers hold 64 rows
 // at d = 64 and 32 at d = 128.  Relative to a workgroup's run of units for 16 rows
