@@ -1255,10 +1255,22 @@ static hipError_t launch_kind(const Args& a, const Kind& x, int wgs, hipStream_t
 template <int D, int RT, bool PK>
 static int launch_tile(const ServeAttn& v, const Args& a, const Layout& y, const Kind& x, hipStream_t st) {
   const int64_t items = v.n_groups * y.tiles;
-  // as many workgroups as run at once, two per compute unit where registers and
-  // LDS allow, or one per run if those are fewer
-  const int64_t most = items * ((v.T_stride + kRun - 1) / kRun);
+  // As many workgroups as run at once: two per compute unit where registers and LDS
+  // allow (packed rows at d = 64: 704 groups of 2048 tokens 70 -> 61 us, 352 of 32k
+  // 219 -> 182), or one per run if those are fewer.  A workgroup's run takes about
+  // as long as the merge of 8 records (16 at d = 128), so an item of n runs is best
+  // cut in sqrt(8 n) (one group of 131072 tokens: 61 us in 512 workgroups, 27 in 128,
+  // 25 in 64, 28 in 32; of 32768 tokens: 25 us in 128, 19-20 in 32 or 64); 32 are never
+  // too many (4 groups of 8192 tokens: 22.0 us, in 16 each 24.8).  A power of two, so
+  // that ranges of usual capacities end where items do (d = 128, 4 items of 32768
+  // tokens: 33.6 us in 45 each, 28.9 in 32).
+  const int64_t runs = (v.T_stride + kRun - 1) / kRun;
+  const int64_t most = items * runs;
+  int64_t cut = 32;
+  while (4 * cut * cut <= D / 8 * runs) cut *= 2;
+  cut *= items;
   int64_t wgs = PK && D == 64 && x.qw > 0 ? kMaxWgs : kMaxWgs / 2;
+  if (wgs > cut) wgs = cut;
   if (wgs > most) wgs = most;
   // (also without any row in the cache: the merge goes by the lengths that prep leaves)
   hipLaunchKernelGGL((prep_kernel<D, RT, PK>), dim3((unsigned)(items + 1 + (x.qw == 0 ? kTop : 0))),
