@@ -63,9 +63,11 @@ __global__ __launch_bounds__(256) void accept_kernel(
 }
 
 // Order of the accumulators as unsigned numbers: NaN below everything, both
-// zeros equal.
+// zeros equal.  No accumulator has key 0 (tokens behind the last one) or kRecent
+// (tokens that are kept in any case), so that the passes compare keys alone.
+constexpr uint32_t kRecent = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t key_of(float a) {
-  if (a != a) return 0;
+  if (a != a) return 1;
   const uint32_t u = __float_as_uint(a + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -76,9 +78,12 @@ __device__ __forceinline__ uint32_t key_of(float a) {
 // equals before it.  Up to 32768 tokens, one workgroup per group reads them once,
 // keeps the keys in registers and does all of it in one launch; longer groups are
 // cut into slices, a workgroup each, whose histograms meet in the workspace
-// between four launches.  What bounds it: the LDS atomics of the histograms
-// (attention weights share few exponents, so the bins are kept in kCopies copies
-// by lane) and the passes' barriers.
+// between four launches (352 groups of 32768 tokens: 88 us in registers, 188 in
+// slices; 8 groups: 27 and 31; of 16384: 17 and 28).  What bounds it: the vector
+// instructions per key and the passes' barriers (32768 keys: 44 us for 352
+// groups, two workgroups per compute unit although some registers spill then; 51 us
+// at one).  The bins are kept in kCopies copies by lane, since attention weights
+// share few exponents (spread ones: 1 to 2 % faster than one copy).
 constexpr int kSel = 1024;      // threads
 constexpr int kBins = 2048;
 constexpr int kCopies = 4;
@@ -182,111 +187,117 @@ __device__ bool whole_group(const Sel& p, int g, int len, int32_t* out, bool fir
 }
 
 // Keys of tokens t0 .. t0 + 1024 E - 1 in registers: u[4 j + i] is token
-// t0 + 4096 j + 4 tid + i, valid below `old`.
+// t0 + 4096 j + 4 tid + i; from `old` on kRecent, from `end` on 0.
 template <int E>
-__device__ __forceinline__ void load_keys(const float* a, int t0, int old, uint32_t (&u)[E]) {
+__device__ __forceinline__ void load_keys(const float* a, int t0, int old, int end, uint32_t (&u)[E]) {
 #pragma unroll
   for (int j = 0; j < E / 4; ++j) {
     const int t = t0 + 4096 * j + 4 * (int)threadIdx.x;
     float v[4] = {};
-    if (t + 4 <= old) {
+    if (t + 4 <= min(old, end)) {
       __builtin_memcpy(v, a + t, 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[4 * j + i] = key_of(v[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (t + i < old) v[i] = a[t + i];
+        u[4 * j + i] = t + i >= end ? 0 : t + i >= old ? kRecent : key_of(a[t + i]);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[4 * j + i] = key_of(v[i]);
   }
 }
 
-// Places of the kept ones of those tokens (below `len`), with `larger` and
-// `equal` keys before t0.  any: some of the first `old` are kept.
+// counts the digits of those tokens' keys, by whole 4096-token pieces before `end`
 template <int E>
-__device__ void emit(const uint32_t (&u)[E], int t0, int len, int old, bool any, const Found& f,
-                     int larger, int equal, uint32_t (*sums)[kSel / 64], int32_t* out, int keep) {
+__device__ __forceinline__ void count_keys(const uint32_t (&u)[E], int t0, int end, int d, const Found& f, int* bins) {
+#pragma unroll
+  for (int j = 0; j < E / 4; ++j) {
+    if (t0 + 4096 * j >= end) break;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) count_key(u[4 * j + i], d, f, bins);
+  }
+}
+
+// Places of the kept ones of those tokens, with `larger` and `equal` keys before
+// t0.  sums: a number per 4096-token piece and wavefront, and (behind them) how
+// many keys were larger | equal << 16 in all (at most 32768 each).
+template <int E>
+__device__ void emit(const uint32_t (&u)[E], int t0, const Found& f, int larger, int equal,
+                     uint32_t* sums, int32_t* out, int keep) {
+  constexpr int kWaves = kSel / 64, kSums = E / 4 * kWaves;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t before[E / 4];  // of a 4096-token piece: larger keys | equal keys << 16
+  uint32_t before[E / 4];  // of a piece: larger keys | equal keys << 16
 #pragma unroll
   for (int j = 0; j < E / 4; ++j) {
     uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = t0 + 4096 * j + 4 * (int)threadIdx.x + i;
-      const bool is_old = any && t < old;
-      n += (t < len && (t >= old || (is_old && u[4 * j + i] > f.top))) ? 1u : 0u;
-      n += (is_old && u[4 * j + i] == f.top) ? 1u << 16 : 0u;
-    }
+    for (int i = 0; i < 4; ++i)
+      n += u[4 * j + i] > f.top ? 1u : u[4 * j + i] == f.top ? 1u << 16 : 0u;
     const uint32_t upto = wave_upto(n);
-    if (lane == 63) sums[j][wave] = upto;
+    if (lane == 63) sums[j * kWaves + wave] = upto;
     before[j] = upto - n;
   }
   __syncthreads();
+  if (wave == 0) {  // exclusive sums, two per lane
+    const uint32_t s0 = 2 * lane < kSums ? sums[2 * lane] : 0, s1 = 2 * lane < kSums ? sums[2 * lane + 1] : 0;
+    const uint32_t upto = wave_upto(s0 + s1);
+    if (2 * lane < kSums) {
+      sums[2 * lane] = upto - s1 - s0;
+      sums[2 * lane + 1] = upto - s1;
+    }
+    if (lane == 63) sums[kSums] = upto;
+  }
+  __syncthreads();
+  uint32_t top = f.top;
+  asm("" : "+v"(top));  // (else the comparisons above are kept, in spilled scalar registers)
+
 #pragma unroll
   for (int j = 0; j < E / 4; ++j) {
-    uint32_t all = 0, mine = before[j];
-#pragma unroll
-    for (int i = 0; i < kSel / 64; ++i) {
-      const uint32_t y = sums[j][i];
-      mine += i < wave ? y : 0;
-      all += y;
-    }
+    const uint32_t mine = before[j] + sums[j * kWaves + wave];
     int g = larger + (int)(mine & 0xFFFFu), e = equal + (int)(mine >> 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int t = t0 + 4096 * j + 4 * (int)threadIdx.x + i;
-      const bool is_old = any && t < old;
-      const bool gt = t < len && (t >= old || (is_old && u[4 * j + i] > f.top));
-      const bool eq = is_old && u[4 * j + i] == f.top;
+      const bool gt = u[4 * j + i] > top, eq = u[4 * j + i] == top;
       // (the bound holds by the counts; it is checked, since sliced passes read
       // accumulators that another stream might be writing)
       const int at = g + min(e, f.need);
-      if ((gt || (eq && e < f.need)) && (uint32_t)at < (uint32_t)keep) out[at] = t;
+      if ((gt || (eq && e < f.need)) && (uint32_t)at < (uint32_t)keep)
+        out[at] = t0 + 4096 * j + 4 * (int)threadIdx.x + i;
       g += gt;
       e += eq;
     }
-    larger += (int)(all & 0xFFFFu);
-    equal += (int)(all >> 16);
   }
 }
 
 template <int E>
-__global__ __launch_bounds__(kSel) void select_kernel(const Sel p) {
+__global__ __launch_bounds__(kSel, 8) void select_kernel(const Sel p) {
   __shared__ int bins[kBins * kCopies];
-  __shared__ uint32_t sums[E / 4][kSel / 64];
+  __shared__ uint32_t sums[E / 4 * (kSel / 64) + 1];
   __shared__ int found[2];
   __shared__ int read;  // (one reading for all threads)
   const int g = blockIdx.x;
   if (threadIdx.x == 0) read = p.lens[g];
   __syncthreads();
-  const int len = read;
+  const int len = __builtin_amdgcn_readfirstlane(read);
   int32_t* out = p.index + (int64_t)g * p.keep;
   if (whole_group(p, g, len, out, true)) return;
-  const int old = len - p.recent;
-  const bool any = p.keep > p.recent;  // some of the first `old` are kept
-  Found f{0, p.keep - p.recent};
+  Found f{0, p.keep};
   uint32_t u[E];
-  load_keys<E>(p.acc + g * p.T_stride, 0, any ? old : 0, u);
-  if (any) {
+  load_keys<E>(p.acc + g * p.T_stride, 0, len - p.recent, len, u);
 #pragma unroll 1
-    for (int d = 0; d < 3; ++d) {
-      clear_bins(bins);
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (4096 * (i / 4) + 4 * (int)threadIdx.x + (i & 3) < old) count_key(u[i], d, f, bins);
-      __syncthreads();
-      find_digit(d, [&](int b) { return bin_count(bins, b); }, sums[0], found, &f);
-    }
+  for (int d = 0; d < 3; ++d) {
+    clear_bins(bins);
+    count_keys<E>(u, 0, len, d, f, bins);
+    __syncthreads();
+    find_digit(d, [&](int b) { return bin_count(bins, b); }, sums, found, &f);
   }
-  emit<E>(u, 0, len, old, any, f, 0, 0, sums, out, p.keep);
+  emit<E>(u, 0, f, 0, 0, sums, out, p.keep);
 }
 
 // Sliced: pass d < 3 counts digit d of a slice, pass 3 writes the places; a pass
 // first finds the digit that the pass before counted.
 __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
   __shared__ int bins[kBins * kCopies];
-  __shared__ uint32_t sums[1][kSel / 64];
+  __shared__ uint32_t sums[kSel / 64 + 1];
   __shared__ int found[2];
   __shared__ int total[2];
   __shared__ int read;  // (one reading for all threads)
@@ -294,19 +305,18 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
   if (tid == 0) read = p.lens[g];
   if (tid < 2) found[tid] = 0;
   __syncthreads();
-  const int len = read;
+  const int len = __builtin_amdgcn_readfirstlane(read);
   int32_t* out = p.index + (int64_t)g * p.keep;
   if (whole_group(p, g, len, out, pass == 0 && s == 0)) return;
   const float* a = p.acc + g * p.T_stride;
   const int old = len - p.recent;
-  const bool any = p.keep > p.recent;
-  Found f{0, p.keep - p.recent};
+  Found f{0, p.keep};
   auto counts = [&](int d, int slice) {
     return p.hist + (((int64_t)d * p.n_groups + g) * p.slices + slice) * kBins;
   };
   auto state = [&](int d) { return p.found + ((int64_t)d * p.n_groups + g) * 2; };
   if (tid < 2) total[tid] = 0;
-  if (any && pass > 0) {
+  if (pass > 0) {
     const int d = pass - 1;
     if (d > 0) f = Found{(uint32_t)state(d - 1)[0], state(d - 1)[1]};
     find_digit(d, [&](int b) {
@@ -314,7 +324,7 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
 #pragma unroll 8
       for (int i = 0; i < p.slices; ++i) n += counts(d, i)[b];
       return n;
-    }, sums[0], found, &f);
+    }, sums, found, &f);
     if (d < 2) {
       // every slice's workgroup finds the same; slice 0's hands it on
       if (s == 0 && tid == 0) {
@@ -335,43 +345,33 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
   const int from = (int)min((int64_t)s * p.slice_len, (int64_t)len);
   const int to = (int)min((int64_t)(s + 1) * p.slice_len, (int64_t)len);
   if (pass < 3) {
-    if (!any) return;
     clear_bins(bins);
-    const int end = min(to, old);
-    for (int t0 = from; t0 < end; t0 += 8 * kSel) {
+    for (int t0 = from; t0 < to; t0 += 8 * kSel) {
       uint32_t u[8];
-      load_keys<8>(a, t0, end, u);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (t0 + 4096 * (i / 4) + 4 * tid + (i & 3) < end) count_key(u[i], pass, f, bins);
+      load_keys<8>(a, t0, old, to, u);
+      count_keys<8>(u, t0, to, pass, f, bins);
     }
     __syncthreads();
     for (int b = tid; b < kBins; b += kSel) counts(pass, s)[b] = bin_count(bins, b);
     return;
   }
   // larger and equal keys of the slices before this one
-  if (any) {
-    const int b2 = (int)digit_of(f.top, 2);
-    int larger = 0;
-    for (int i = tid; i < s * 1024; i += kSel)
-      if ((i & 1023) > b2) larger += counts(2, i >> 10)[i & 1023];
-    if (tid < s) {
-      larger += p.ahead[(int64_t)g * p.slices + tid];
-      atomicAdd(&total[1], counts(2, tid)[b2]);
-    }
-    if (larger) atomicAdd(&total[0], larger);
+  const int b2 = (int)digit_of(f.top, 2);
+  int ahead = 0;
+  for (int i = tid; i < s * 1024; i += kSel)
+    if ((i & 1023) > b2) ahead += counts(2, i >> 10)[i & 1023];
+  if (tid < s) {
+    ahead += p.ahead[(int64_t)g * p.slices + tid];
+    atomicAdd(&total[1], counts(2, tid)[b2]);
   }
+  if (ahead) atomicAdd(&total[0], ahead);
   __syncthreads();
-  // (recent tokens of earlier slices count as larger)
-  int larger = total[0] + max(0, from - old), equal = total[1];
+  int larger = total[0], equal = total[1];
   for (int t0 = from; t0 < to; t0 += 4 * kSel) {
     uint32_t u[4];
-    load_keys<4>(a, t0, any ? min(old, to) : 0, u);
-    emit<4>(u, t0, to, old, any, f, larger, equal, sums, out, p.keep);
-    // what this piece held
-    uint32_t all = 0;
-#pragma unroll
-    for (int i = 0; i < kSel / 64; ++i) all += sums[0][i];
+    load_keys<4>(a, t0, old, to, u);
+    emit<4>(u, t0, f, larger, equal, sums, out, p.keep);
+    const uint32_t all = sums[kSel / 64];  // what this piece held
     larger += (int)(all & 0xFFFFu);
     equal += (int)(all >> 16);
     __syncthreads();
@@ -379,8 +379,10 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
 }
 
 // Copies the kept rows, V bytes of a payload row at a time (the largest that
-// divides P and that all addresses are aligned to): P = 4 with single bytes took
-// 35 us for 2.9 M rows, whose bytes take 18 at the rate of a large copy.
+// divides P and that all addresses are aligned to: at P = 48, 262144 rows, 12 us
+// against 26 with single bytes).  What bounds it is the lines that it touches: at
+// P = 4 a quarter of the rows is kept and nearly every 128-byte line holds one (2.9 M
+// of 11.5 M rows: 36 us, 248 MB, whatever the width).
 template <typename V>
 __global__ __launch_bounds__(256) void gather_kernel(
     const uint8_t* __restrict__ kp, const uint16_t* __restrict__ kn,
