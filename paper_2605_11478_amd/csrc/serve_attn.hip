@@ -30,8 +30,22 @@
 //   Up to 8 rows ("packed") share a product between their parts: columns h and
 //   h + 8 of B are row h's high and low part, summed by one exchange in which
 //   lane h keeps the first tile's tokens and lane h + 8 the second's; rows h and
-//   h + 8 of the weights are row h's parts.
+//   h + 8 of the weights are row h's parts (against a tile of 16 rows: 352 groups of 8
+//   rows, 32k tokens, k = 8, with the weights' pass 280 -> 180 us; 704 of 2048 tokens,
+//   k = 4, 68 -> 54; 144 of one row 30 -> 27; 8 of 4 rows at d = 128 72 -> 66).
 // merge_kernel combines an item's records by log-sum-exp and applies Pi^T.
+// For accumulated weights rows_kernel then goes over the same ranges once more with
+// the rows' statistics (m, l), recomputes the scores and adds the weights of a
+// token, summed over the rows in a fixed order, to its accumulator: no atomics.
+//
+// What bounds them.  The work is far above the bytes (352 groups of 32k tokens at
+// k = 8 hold 138 MB, 27 us at a large copy's rate): rows_kernel is bound by the
+// vector instructions per unit with few rows (that cache, 8 rows: 113 us, 120
+// instructions per unit, 75 % of all issue cycles; its weights' pass 76 us), and
+// by vector and matrix instructions together with many (16 groups of 512 rows, 32k
+// tokens: 140 us, of which the two-part products take 63 at the rate of a large
+// matrix product; the two hardly overlap).  Small calls are three or four launches,
+// 12 to 20 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -129,7 +143,9 @@ __device__ __forceinline__ f4 load4(const void* q, int64_t at) {
 // The rotation runs on v_mfma_f32_16x16x4_f32 (float32 products and sums; K slot
 // kk of lane group gq is column D / 4 gq + kk).  Operands are at the power of two
 // that takes the item's largest finite entry to [2^13, 2^14), so that the low
-// parts are normal numbers.
+// parts are normal numbers.  A launch of its own (3 to 6 us) costs less than the
+// rotation in every workgroup that meets an item: 309 -> 234 us for 352 groups of
+// 32k tokens, 118 -> 78 for 704 of 2048.
 template <int D, int RT, bool PK>
 __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args a, int wgs) {
   constexpr int KS = D / 32, KQ = D / 4, Q = D / 16;
@@ -304,7 +320,8 @@ struct Unit {
 // rows of an LDS table (k = 1, most of k = 2, quarters of a payload that share
 // a codeword, tables above 64 KB): each wavefront writes the decoded rows of
 // its unit, keys and then values, into a tile of its own and reads the operands
-// from there.
+// from there.  Codes that both serve go through the table: 208 rows, 2048 tokens,
+// k = 4, 37 us against 81; 704 groups of 8 rows, k = 2, 62 against 197.
 template <int D, int RT, int W, int KB, int QW, bool PK, bool WT>
 __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) void rows_kernel(const Args a) {
   constexpr int NB = D / 4, Q = NB / 4;  // 4-dim rows, of them per quarter
