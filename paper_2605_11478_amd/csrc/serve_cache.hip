@@ -79,11 +79,12 @@ __device__ __forceinline__ uint32_t key_of(float a) {
 // keeps the keys in registers and does all of it in one launch; longer groups are
 // cut into slices, a workgroup each, whose histograms meet in the workspace
 // between four launches (352 groups of 32768 tokens: 88 us in registers, 188 in
-// slices; 8 groups: 27 and 31; of 16384: 17 and 28).  What bounds it: the vector
-// instructions per key and the passes' barriers (32768 keys: 44 us for 352
-// groups, two workgroups per compute unit although some registers spill then; 51 us
-// at one).  The bins are kept in kCopies copies by lane, since attention weights
-// share few exponents (spread ones: 1 to 2 % faster than one copy).
+// slices; 8 groups: 27 and 31; of 16384: 17 and 28).  What bounds it: the LDS
+// atomics, scans and barriers of the passes, one behind the other (352 groups of 32768
+// keys: 44 us, vector units 28 % busy, two workgroups per compute unit although some
+// registers spill then; 51 us at one).  The bins are kept in kCopies copies by
+// lane, since attention weights share few exponents (1, 4 and 8 copies: 144 groups of
+// 1024 tokens 13.1, 11.0 and 12.8 us, 352 of 32768 87.8, 85.0 and 88.7).
 constexpr int kSel = 1024;      // threads
 constexpr int kBins = 2048;
 constexpr int kCopies = 4;
