@@ -112,3 +112,22 @@ def test_tiles_agree_on_long_groups(device, d, k, N):
     masks = random_masks(rng, M)
     check_tree(c, q, q64, run_tree(c, q, lens, masks), lens, masks)
     check_tree(c, q, q64, base.run_tree(c, q, lens, masks), lens, masks)
+
+
+@pytest.mark.parametrize("M,G", [(2, 3), (3, 5)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_records_of_one_group(device, d, M, G):
+    """A group of which up to 157 workgroups hold a part each, in the outputs and the weights."""
+    rng = np.random.default_rng(13)
+    lens = [40000]
+    c = Cache(d, 4, 256, 1, 40100, device)
+    w = wide(c, 1 << 21)
+    q, q64 = queries(rng, (1, M, G, d), torch.float32, device)
+    q, q64 = 4 * q, 4 * q64  # (weights far from equal)
+    masks = random_masks(rng, M)
+    check_tree(c, q, q64, base.run_tree(w, q, lens, masks), lens, masks)
+    before = torch.rand(1, 1 << 21, device=device)
+    acc = before.clone()
+    out = base.run_accum(w, q[:, 0].contiguous(), lens, acc)
+    assert torch.equal(acc[:, 40000:], before[:, 40000:])
+    base.check_accum(c, q64[:, 0], out, before[:, :c.T], acc[:, :c.T], lens)
