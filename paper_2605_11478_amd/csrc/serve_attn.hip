@@ -1003,6 +1003,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
         for (int i = 0; i < 4; ++i) v = fmaf(st[i * state_floats(D, RT, PK)], fac[i * ROWS + row], v);
         r[2 * ROWS + x] = v;
       }
+      // (the next item's first staged rows share LDS with the states; the barrier
+      // behind its queries' low parts stands before them where there is one)
+      if constexpr (kStaged && RT == 1) lds_barrier();
     }
   };
 
