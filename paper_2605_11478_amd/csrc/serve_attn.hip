@@ -546,10 +546,16 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
 #pragma unroll
       for (int mu = 0; mu < VM; ++mu) acc[t][mu] = f4{0, 0, 0, 0};
     }
-    if constexpr (WT) {  // this row's statistics
-      const int64_t at = ((int64_t)g * a.rows + min(hr, a.rows - 1)) * 2;
-      m[0] = a.stat[at] == -INFINITY ? 0.0f : a.stat[at];
-      l[0] = hr < a.rows && a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
+    if constexpr (WT) {
+      // this row's statistics; against +inf the scores of rows behind the last one
+      // have weight 0 (their scores of 0 against a reference below -128 would be
+      // infinite weights, and no number times l = 0)
+      m[0] = INFINITY;
+      if (hr < a.rows) {
+        const int64_t at = ((int64_t)g * a.rows + hr) * 2;
+        m[0] = a.stat[at] == -INFINITY ? 0.0f : a.stat[at];
+        l[0] = a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
+      }
     }
 
     // staged codes: rows of the unit's tokens into the tile; whether any has a residual
