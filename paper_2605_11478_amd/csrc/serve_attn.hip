@@ -91,8 +91,8 @@ struct Args {
   const float* R;
   const float* C;
   float qscale;
-  h8* ops;            // the items' query operands, and their divisors
-  float* qs;
+  h8* ops;            // the items' query operands
+  float* qs;          // and their divisors (qs_floats of an item)
   Start* start;       // of every workgroup
   float* rec;
   int32_t* bounds;    // first and last workgroup of every item
@@ -109,6 +109,9 @@ constexpr int state_regs(int D, int RT) { return RT * (D / 16) * 4 + 2 * RT; }
 // half the lanes, which lets two workgroups with 64 KB tables share a compute unit.
 constexpr int reg_floats(bool PK) { return PK ? 36 : 68; }
 constexpr int state_floats(int D, int RT, bool PK) { return state_regs(D, RT) * reg_floats(PK); }
+// an item's divisors: a row's own with one row tile, else the rows' relative to the
+// item's, which is the last (negative: not all rows' are 1)
+__host__ __device__ constexpr int qs_floats(int RT) { return RT > 1 ? 16 * RT + 1 : 16; }
 // the queries' low parts: in registers for one row tile, else in LDS (they are 32
 // of 256 registers at four tiles, where the unit loop spilled without)
 constexpr int ops_bytes(int D, int RT) { return RT > 1 ? RT * (D / 32) * 1024 : 0; }
@@ -141,9 +144,12 @@ __device__ __forceinline__ f4 load4(const void* q, int64_t at) {
 // (staged codes) kTop that write partial maxima of the codebook.
 //
 // The rotation runs on v_mfma_f32_16x16x4_f32 (float32 products and sums; K slot
-// kk of lane group gq is column D / 4 gq + kk).  Operands are at the power of two
-// that takes the item's largest finite entry to [2^13, 2^14), so that the low
-// parts are normal numbers.  A launch of its own (3 to 6 us) costs less than the
+// kk of lane group gq is column D / 4 gq + kk).  A row's operands are at the power
+// of two that takes its largest finite entry to [2^13, 2^14), so that the low parts
+// of the entries that count are normal numbers.  With more than one row tile, rows
+// whose largest entry is within 2^12 of the item's share the item's power (both
+// parts then hold 25 bits of that entry), so that only items of rows further apart
+// pay a multiplication per score (unit loop).  A launch of its own (3 to 6 us) costs less than the
 // rotation in every workgroup that meets an item: 309 -> 234 us for 352 groups of
 // 32k tokens, 118 -> 78 for 704 of 2048.
 template <int D, int RT, bool PK>
@@ -151,6 +157,7 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
   constexpr int KS = D / 32, KQ = D / 4, Q = D / 16;
   constexpr int ROWS = 16 * RT, QS = D + 4;
   __shared__ __align__(16) float qt[ROWS * QS];
+  __shared__ float tops[D / 16][ROWS];  // the rows' largest finite entries, of 16 dims
   constexpr int kT = 256 * (RT > 1 ? 2 : 1);
   __shared__ uint64_t sums[kT];
   __shared__ float red[kT / 64];
@@ -253,26 +260,45 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         s = __builtin_amdgcn_mfma_f32_16x16x4f32(pa[p][e], pb[p][e], s, 0, 0, 0);
+    float most = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       s[e] *= a.qscale;
-      top = fmaxf(top, fabsf(s[e]) < INFINITY ? fabsf(s[e]) : 0.0f);
+      most = fmaxf(most, fabsf(s[e]) < INFINITY ? fabsf(s[e]) : 0.0f);
     }
+    most = xmax(xmax(most, 16), 32);
+    if (g16 == 0) tops[dt][16 * t + c] = most;
+    top = fmaxf(top, most);
     *reinterpret_cast<f4*>(qt + (16 * t + c) * QS + 16 * dt + 4 * g16) = s;
   }
-  top = wave_max_dpp(top);
-  if (lane == 0) red[wave] = top;
-  __syncthreads();
-  top = wave_max_of(red);
-  float qs = 1.0f, qi = 1.0f;
-  if (top > 0.0f) {
-    int e2 = 0;
-    frexpf(top, &e2);
-    e2 = max(e2 - 14, -100);
-    qs = ldexpf(1.0f, e2);
-    qi = ldexpf(1.0f, -e2);
+  if constexpr (RT > 1) {
+    top = wave_max_dpp(top);
+    if (lane == 0) red[wave] = top;
   }
-  if (tid == 0) a.qs[blockIdx.x] = qs;
+  __syncthreads();
+  auto power = [](float x) {
+    int e2 = 0;
+    frexpf(x, &e2);
+    return max(e2 - 14, -100);
+  };
+  const int shared = RT > 1 ? power(wave_max_of(red)) : 0;
+  auto row_power = [&](int r) {
+    float x = 0.0f;
+    if (row0 + r < a.rows) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) x = fmaxf(x, tops[i][r]);
+    }
+    if (x == 0.0f) return shared;
+    const int e2 = power(x);
+    return RT > 1 && shared - e2 <= 12 ? shared : e2;
+  };
+  if (wave == 0) {
+    const int e2 = row_power(min(tid, ROWS - 1)) - shared;
+    float* to = a.qs + (int64_t)blockIdx.x * qs_floats(RT);
+    if (tid < ROWS) to[tid] = ldexpf(1.0f, e2);
+    const bool uneven = __any(e2 != 0);
+    if (RT > 1 && tid == 0) to[ROWS] = ldexpf(uneven ? -1.0f : 1.0f, shared);
+  }
   // B operand of K-step kap: lane l holds column l % 16 (PK: row l % 8, its high
   // part below 8, else its low part), K slots = dims 4 (l / 16 Q + 2 kap) .. + 7
   h8* to = a.ops + (int64_t)blockIdx.x * RT * KS * (PK ? 1 : 2) * 64;
@@ -281,6 +307,7 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
     const int r = 16 * t + (PK ? l & 7 : l & 15);
     uint32_t hi[4] = {}, lo[4] = {};
     if (row0 + r < a.rows) {
+      const float qi = ldexpf(1.0f, -row_power(r));
       const float* at = qt + r * QS + 4 * ((l >> 4) * Q + 2 * kap);
 #pragma unroll
       for (int i = 0; i < 4; ++i) split2(at[2 * i] * qi, at[2 * i + 1] * qi, &hi[i], &lo[i]);
@@ -511,7 +538,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
         bh[t][kap] = op[(t * KS + kap) * (PK ? 64 : 128)];
         if constexpr (RT == 1 && !PK) bl[kap] = op[kap * 128 + 64];
       }
-    const float qs = a.qs[item];
+    const float qs = a.qs[item * qs_floats(RT) + (RT > 1 ? ROWS : hr)];
     if constexpr (RT > 1) {
       h8* to = reinterpret_cast<h8*>(smem + a.lds_ops);
       for (int x = tid; x < RT * KS * 64; x += kThreads)
@@ -528,7 +555,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
       }
       has_lo = __any(lane < kWaves && redi[lane & (kWaves - 1)] != 0);
     }
-    const float ks = qs * ci;  // scores: products times nu_K times this, in log2 units
+    // scores: products times nu_K times this, in log2 units (RT > 1: negative if
+    // some rows have a factor of their own)
+    const float ks = qs * ci;
 
     f4 acc[RT][VM];
     float m[RT], l[RT];
@@ -699,13 +728,25 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
           s[0][0][e] = own + ror8(other);
         }
       }
+      if constexpr (RT > 1) {
+        if (ks < 0.0f) {
+          int64_t at = item;
+          asm volatile("" : "+s"(at));  // (an address computed here costs the loop no register)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const float f = a.qs[at * qs_floats(RT) + 16 * t + c];
+            s[t][0] *= f;
+            s[t][1] *= f;
+          }
+        }
+      }
       // (one tile scales its scores, and the norms stay binary16 operands; more
       // tiles share the scaled norms)
       float nk[NE];
 #pragma unroll
       for (int i = 0; i < NE; ++i) {
         nk[i] = (float)__builtin_bit_cast(h2, x.nk[i >> 1])[i & 1];
-        if constexpr (RT > 1) nk[i] *= ks;
+        if constexpr (RT > 1) nk[i] *= fabsf(ks);
         else s[0][i >> 2][i & 3] *= ks;
       }
       float nv[NE];
@@ -1234,7 +1275,7 @@ static Layout make_layout(int64_t n_groups, int M, int G, const Shape& s, int ti
   const size_t items = (size_t)n_groups * y.tiles;
   auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
   y.off_qs = al(items * (y.tile / 16) * (s.d / 32) * (y.packed ? 1 : 2) * 1024);
-  y.off_now = al(y.off_qs + items * 4);
+  y.off_now = al(y.off_qs + items * qs_floats(y.tile / 16) * 4);
   y.off_start = al(y.off_now + (size_t)n_groups * 4);
   y.off_top = al(y.off_start + kMaxWgs * sizeof(Start));
   y.off_bounds = al(y.off_top + kTop * 4);
