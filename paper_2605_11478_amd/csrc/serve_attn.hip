@@ -65,7 +65,15 @@ constexpr int kStep = 32;              // tokens per unit
 constexpr int kRun = kStep * kWaves;   // tokens per run of units
 constexpr int kTop = 64;               // partial maxima of a codebook
 constexpr int kMaxWgs = 512;           // workgroups of the main launch, at most
-constexpr float kLag = 8.0f;           // a maximum moves when a score exceeds it by this (log2)
+// A row's reference m moves when a weight 2^(score - m) times its value norm exceeds
+// 2^kMostProduct, or a weight 2^kMostWeight; it then leaves products of 2^kProduct and
+// weights of 2^kWeight at most.  (binary16 ends at 65504 = 2^15.999 and a pair of parts
+// rounds at 2^-25, so a product keeps bits down to 2^-32 of its row's largest.  Between
+// 7 and 15.9 a reference moves in 0.14 of the units at 32 rows of d = 128, in 0.05 at 8
+// of d = 64; a tile moves alone, since moving all four for one row took 149 us where
+// this takes 135, 512 rows of 16 groups.)
+constexpr float kMostProduct = 15.9f, kMostWeight = 96.0f;
+constexpr float kProduct = 7.0f, kWeight = 80.0f;
 constexpr float kCs = 4096.0f;         // scale of the codebook's binary16 rows
 
 struct Start {  // of a workgroup's range: a group, runs before it, runs in all
@@ -561,13 +569,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
 
     f4 acc[RT][VM];
     float m[RT], l[RT];
-    // The reference m of a row: weights are 2^(score - m).  It is the running
-    // maximum less `head`, which keeps weight times value norm within binary16:
-    // norms so far are below 2^(7 - head), so the maximum's weight 2^head times a
-    // norm is at most 2^7, and a score may exceed the maximum by 2^kLag before the
-    // reference moves.
-    float vlim = 0.0f, head = 0.0f;  // bound of the value norms so far
-    uint16_t vbits = 0;              // the largest binary16 below the bound, as bits
+    // The reference m of a row: weights are 2^(score - m).  It follows the largest
+    // product of a weight and its value norm, so that both binary16 parts of those
+    // that count are normal numbers, however far the row's value norms are apart;
+    // weights themselves are float32 numbers up to 2^96, which is where a token of a
+    // far larger score and value norm 0 moves it.
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       m[t] = -INFINITY;
@@ -756,11 +762,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
       // A unit that holds drafted tokens or ends behind the last one: unseen
       // scores become -inf.  Norms may be anything there: one that is not a
       // positive number is multiplied into the seen scores (a value norm that is
-      // no number makes them NaN), and leaves the unseen ones alone.  A token that
-      // no row of the tile sees gets value norm 0, so that it has no part in the
-      // scale of the weights either.
+      // no number makes them NaN), and leaves the unseen ones alone.
       if (tb + kStep > len) {
-        uint32_t seen = 0;  // by this lane's rows
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           uint64_t mask = 0;
@@ -773,15 +776,12 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
             if (!(fabsf(nv[i]) < INFINITY)) v = NAN;
             const bool in = j < 0 || (j < a.M && (mask >> (j & 63) & 1));
             s[t][i >> 2][i & 3] = in ? v : -INFINITY;
-            seen |= (uint32_t)in << i;
           }
         }
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-          // (the lanes that hold this token's scores)
-          const uint64_t any = __ballot(seen >> i & 1) >> (lane & (PK ? 56 : 48)) & (PK ? 0xFF : 0xFFFF);
           nk[i] = nk[i] > 0.0f && nk[i] < INFINITY ? nk[i] : 1.0f;
-          nv[i] = any != 0 && fabsf(nv[i]) < INFINITY ? nv[i] : 0.0f;
+          nv[i] = fabsf(nv[i]) < INFINITY ? nv[i] : 0.0f;
         }
       }
       auto against = [&](int t, float ref, float (&p)[NE]) {
@@ -814,62 +814,51 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
         const int at = tb + acc_tok;
         if ((c & 1) == 0 && at < tot) a.acc[base + at] = x.acc + x1;
       } else {
-        // ---- larger value norms than so far: the references move
+        // ---- a weight that its lane's largest value norm may take above the bound, or
+        //      (not a number or infinite) a row without a reference yet: the rows whose
+        //      own products or weights are too large move
         typedef uint16_t u2 __attribute__((ext_vector_type(2)));
         u2 most_v = __builtin_bit_cast(u2, x.nv[0]);
 #pragma unroll
         for (int i = 1; i < NE / 2; ++i) most_v = __builtin_elementwise_max(most_v, __builtin_bit_cast(u2, x.nv[i]));
-        // (norms as binary16 bits: one that is no positive number compares above all)
-        if (__any(__builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(most_v, u2(vbits))) != 0)) {
-          float top = 0.0f;
-#pragma unroll
-          for (int i = 0; i < NE; ++i)
-            top = fmaxf(top, fabsf(nv[i]) < INFINITY ? fabsf(nv[i]) : 0.0f);
-          top = xmax(xmax(top, 16), 32);
-          if constexpr (PK) top = xmax(top, 8);
-          if (top > vlim) {  // (uniform)
-            int e2 = 0;
-            frexpf(top, &e2);
-            const float d = (float)(7 - e2) - head, f = __builtin_amdgcn_exp2f(d);
-            vlim = ldexpf(1.0f, e2);
-            vbits = (uint16_t)(__builtin_bit_cast(uint16_t, (_Float16)vlim) - 1);
-            head = (float)(7 - e2);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-              m[t] -= d;  // (-inf stays)
-              l[t] *= f;
-#pragma unroll
-              for (int mu = 0; mu < VM; ++mu) acc[t][mu] *= f;
-            }
-          }
-        }
-        // ---- a score far above its row's maximum, or (not a number or infinite)
-        //      no finite one yet: the maxima move
-        bool over = false;
-        float p[RT][NE], most[RT];
+        // (as bits, negative ones and those that are no numbers are above all; nothing is
+        // below their bound, which is no number)
+        const uint16_t most_b = max(most_v[0], most_v[1]);
+        const float lim = kMostProduct - __builtin_amdgcn_logf((float)__builtin_bit_cast(_Float16, most_b) + 0x1p-80f);
+        uint64_t over[RT], any_over = 0;
+        float p[RT][NE];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           against(t, m[t], p[t]);
-          most[t] = fmaxf(fmaxf(p[t][0], p[t][1]), fmaxf(p[t][2], p[t][3]));
+          float most = fmaxf(fmaxf(p[t][0], p[t][1]), fmaxf(p[t][2], p[t][3]));
           if constexpr (!PK)
-            most[t] = fmaxf(most[t], fmaxf(fmaxf(p[t][4], p[t][5]), fmaxf(p[t][6], p[t][7])));
-          over |= !(most[t] <= head + kLag);
+            most = fmaxf(most, fmaxf(fmaxf(p[t][4], p[t][5]), fmaxf(p[t][6], p[t][7])));
+          over[t] = __ballot(!(most <= lim));
+          any_over |= over[t];
         }
-        if (__any(over)) {
+        if (any_over) {
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
-            const bool first = m[t] == -INFINITY;
-            float mh = most[t];
-            if (first) {
-              mh = -INFINITY;
+            if (over[t] == 0) continue;
+            // the row's largest score, and largest score + log2 of the value norm
+            float top = -INFINITY, top_v = -INFINITY;
 #pragma unroll
-              for (int i = 0; i < NE; ++i)
-                mh = fmaxf(mh, s[t][i >> 2][i & 3] * nk[i]);
+            for (int i = 0; i < NE; ++i) {
+              const float v = s[t][i >> 2][i & 3] * nk[i];
+              top = fmaxf(top, v);
+              top_v = fmaxf(top_v, v + __builtin_amdgcn_logf(fabsf(nv[i])));
             }
-            mh = xmax(xmax(mh, 16), 32);
-            if constexpr (PK) mh = xmax(mh, 8);
-            const float m_new = first ? mh - head : m[t] + fmaxf(mh - head, 0.0f);
-            const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
+            const bool large = m[t] == -INFINITY || top_v - m[t] > kMostProduct || top - m[t] > kMostWeight;
+            uint64_t rows = __ballot(large);  // of a lane's row: bits c + 16 i (packed: hr + 8 i)
+            if (rows == 0) continue;
+            rows |= rows >> 32;
+            rows |= rows >> 16;
+            if constexpr (PK) rows |= rows >> 8;
+            float to = fmaxf(top_v - kProduct, top - kWeight);
+            to = xmax(xmax(to, 16), 32);
+            if constexpr (PK) to = xmax(to, 8);
+            const float m_new = (uint32_t)rows >> hr & 1 ? fmaxf(m[t], to) : m[t];
+            const float f = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
             m[t] = m_new;
             against(t, m_new == -INFINITY ? 0.0f : m_new, p[t]);  // (scores of -inf have weight 0)
             l[t] *= f;

@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import codec as occ
 from oracle import serving as osv
 from test_gpu_serving import Cache, close, queries, random_masks, run_accum, run_tree, weight_tol
 
@@ -66,3 +67,50 @@ def test_staged_codes_with_several_items_per_workgroup(device, d, k, N, M, G):
     acc = before.clone()
     out = run_accum(c, q[:, 0].contiguous(), lens, acc)
     c.check_accum(out, q64[:, 0], before, acc, lens, range(n))
+
+
+def along(c, device, key, value):
+    """All keys of a group become its first one's codewords; key and value norms by token."""
+    c.np[0][:] = c.np[0][:, :1]
+    for i, h in ((1, key), (3, value)):
+        c.np[i] = occ.fp16_bits(np.broadcast_to(h.astype(np.float16), (c.base, c.T)).copy())
+    c.spread(device)
+
+
+@pytest.mark.parametrize("falling", [False, True])
+@pytest.mark.parametrize("M,G", [(1, 5), (3, 4), (6, 5), (8, 8)], ids=str)
+@pytest.mark.parametrize("d,k,N", [(64, 4, 256), (64, 8, 16), (64, 2, 64), (64, 1, 16), (128, 4, 256)], ids=str)
+def test_references_that_move_from_unit_to_unit(device, d, k, N, M, G, falling):
+    """Up to 16 units per wavefront, whose scores rise, stay or fall by up to 12 nats from one to
+    the next while the value norms go from 1e-6 to 1e4 or back; one to four row tiles, items
+    that end inside a workgroup's range and begin in it."""
+    rng = np.random.default_rng(32)
+    n, T = 256, 4096
+    c = Repeated(d, k, N, 2, n, T, device)
+    value = 10.0 ** np.linspace(-6, 4, T)
+    value[[0, 700]] = 0
+    along(c, device, np.linspace(0.5, 64, T), value[::-1] if falling else value)
+    slopes = np.linspace(-3, 3, M * G)
+    slopes[M * G // 2] = 0
+    q = np.zeros((n, M * G, d))
+    for g in range(n):
+        u = c.rows[g % 2][0][0] / 0.5
+        q[g] = rng.permutation(slopes)[:, None] * u / (u @ u)
+    q = torch.from_numpy(q.reshape(n, M, G, d).astype(np.float32)).to(device)
+    q64 = q.double().cpu().numpy()
+    lens = rng.integers(0, T - M + 1, n)
+    lens[:8] = [T - M, 0, 257, 256, 255, T - M, T - M - 31, 1]
+    lens = lens.tolist()
+    masks = random_masks(rng, M)
+    groups = list(range(8)) + [100, 101, 255]
+    c.check_tree(run_tree(c, q, lens, masks, scale=1.0), q64, lens, masks, groups, 1.0)
+    if M == 3:  # (rows of one token; the accumulating form has up to 16)
+        q, q64 = q.reshape(n, 12, d), q64.reshape(n, 12, d)
+    elif M == 1:
+        q, q64 = q[:, 0], q64[:, 0]
+    else:
+        return
+    before = torch.rand(n, T, device=device)
+    acc = before.clone()
+    out = run_accum(c, q.contiguous(), lens, acc, scale=1.0)
+    c.check_accum(out, q64, before, acc, lens, groups, 1.0)
