@@ -74,6 +74,10 @@ constexpr int kMaxWgs = 512;           // workgroups of the main launch, at most
 // this takes 135, 512 rows of 16 groups.)
 constexpr float kMostProduct = 15.9f, kMostWeight = 96.0f;
 constexpr float kProduct = 7.0f, kWeight = 80.0f;
+// Scores beyond this stand as rounded numbers against their row's reference: an exact
+// product less a rounded one is off by up to half a step, which from 2^31 on is 64 and
+// more and would be the exponent of a weight.
+constexpr float kFar = 0x1p24f;
 constexpr float kCs = 4096.0f;         // scale of the codebook's binary16 rows
 
 struct Start {  // of a workgroup's range: a group, runs before it, runs in all
@@ -563,9 +567,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
       }
       has_lo = __any(lane < kWaves && redi[lane & (kWaves - 1)] != 0);
     }
-    // scores: products times nu_K times this, in log2 units (RT > 1: negative if
-    // some rows have a factor of their own)
-    const float ks = qs * ci;
+    // scores: products times nu_K times this, in log2 units (RT > 1: negative if some
+    // rows have a factor of their own or a reference beyond kFar; its sign costs the
+    // loop no register)
+    float ks = qs * ci;
+    bool far = false;  // (uniform, RT = 1) a reference is beyond kFar
 
     f4 acc[RT][VM];
     float m[RT], l[RT];
@@ -590,7 +596,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
         const int64_t at = ((int64_t)g * a.rows + hr) * 2;
         m[0] = a.stat[at] == -INFINITY ? 0.0f : a.stat[at];
         l[0] = a.stat[at + 1] != 0.0f ? 1.0f / a.stat[at + 1] : 0.0f;
+        far = fabsf(m[0]) > kFar;
       }
+      far = __any(far);
     }
 
     // staged codes: rows of the unit's tokens into the tile; whether any has a residual
@@ -788,9 +796,15 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
 #pragma unroll
         for (int i = 0; i < NE; ++i) p[i] = fmaf(s[t][i >> 2][i & 3], nk[i], -ref);
       };
+      auto far_rows = [&](float ref, float (&p)[NE]) {  // scores to their steps, where ref is beyond kFar
+        const float r = fabsf(ref) > kFar && fabsf(ref) < INFINITY ? ref : 0.0f;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) p[i] = (p[i] + r) - r;
+      };
       if constexpr (WT) {
         float p[NE];
         against(0, m[0], p);
+        if (__builtin_expect(far, 0)) far_rows(m[0], p);
 #pragma unroll
         for (int i = 0; i < NE; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]) * l[0];
         // sums over the rows (lanes of a 16-lane row), each step halving the
@@ -824,7 +838,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
         // (as bits, negative ones and those that are no numbers are above all; nothing is
         // below their bound, which is no number)
         const uint16_t most_b = max(most_v[0], most_v[1]);
-        const float lim = kMostProduct - __builtin_amdgcn_logf((float)__builtin_bit_cast(_Float16, most_b) + 0x1p-80f);
+        const float log_v = __builtin_amdgcn_logf((float)__builtin_bit_cast(_Float16, most_b) + 0x1p-80f);
+        const float lim = kMostProduct - log_v;
         uint64_t over[RT], any_over = 0;
         float p[RT][NE];
 #pragma unroll
@@ -848,6 +863,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
               top = fmaxf(top, v);
               top_v = fmaxf(top_v, v + __builtin_amdgcn_logf(fabsf(nv[i])));
             }
+            // (of a far row, the rounded score + a logarithm, not the exact product + one)
+            const bool far_row = fabsf(top) > kFar;
+            top_v = far_row ? top + fminf(log_v, 16.0f) : top_v;
             const bool large = m[t] == -INFINITY || top_v - m[t] > kMostProduct || top - m[t] > kMostWeight;
             uint64_t rows = __ballot(large);  // of a lane's row: bits c + 16 i (packed: hr + 8 i)
             if (rows == 0) continue;
@@ -860,6 +878,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
             const float m_new = (uint32_t)rows >> hr & 1 ? fmaxf(m[t], to) : m[t];
             const float f = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - m_new);
             m[t] = m_new;
+            if (__any(far_row && top > -INFINITY)) {
+              far = true;
+              if constexpr (RT > 1) ks = -fabsf(ks);
+            }
             against(t, m_new == -INFINITY ? 0.0f : m_new, p[t]);  // (scores of -inf have weight 0)
             l[t] *= f;
 #pragma unroll
@@ -869,6 +891,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && QW > 0 && (PK || WT) ? 4 : 2) 
               for (int mu = 0; mu < VM; ++mu) acc[t][mu][e] *= fr;
             }
           }
+        }
+        if (__builtin_expect(RT > 1 ? ks < 0.0f : far, 0)) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) far_rows(m[t], p[t]);
         }
         // ---- weights in two binary16 parts
         h8 wh[RT], wl[RT];

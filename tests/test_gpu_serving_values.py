@@ -93,6 +93,35 @@ def test_finite_query_heads_are_independent(device):
               np.ones((G - 1, 165), dtype=bool))
 
 
+@pytest.mark.parametrize("big", [1e5, 1e8, 1e10, 1e14, 1e30])
+@pytest.mark.parametrize("M,G,large", [(2, 2, False), (3, 4, False), (6, 5, True), (8, 8, True)], ids=str)
+@pytest.mark.parametrize("d,k,N", [(64, 4, 256), (64, 8, 16), (64, 1, 16), (128, 4, 256)], ids=str)
+def test_scores_beyond_the_steps_of_float32(device, d, k, N, M, G, large, big):
+    """Finite queries of any size have finite outputs, and weights that sum to 1, in caches of one
+    unit per wavefront and of many, where such scores and ordinary ones meet."""
+    rng = np.random.default_rng(47)
+    n, T = 256, 2500
+    c = Repeated(d, k, N, 2, n, T, device)
+    lens = rng.integers(T // 2, T - M, n).tolist()
+    q, _ = queries(rng, (n, M, G, d), torch.float32, device)
+    q[:, 1] *= big
+    q[1, 0, 0] *= big
+    q64 = q.double().cpu().numpy()
+    masks = np.array([1 << i for i in range(M)], dtype=np.int64)
+    out = run_tree(c, q, lens, masks)
+    assert bool(out.isfinite().all())
+    c.check_tree(out, q64, lens, masks, [0, 1, 2, 255])
+    if M * G <= 16:
+        acc = torch.zeros(n, T, device=device)
+        out = run_accum(c, q.reshape(n, M * G, d), lens, acc)
+        assert bool(out.isfinite().all()) and bool((acc >= 0).all())
+        # every weight to 2^-17 (exponentials, the sum's parts) of itself
+        assert bool(((acc.double().sum(1) - M * G).abs() <= 2.0**-16 * M * G).all())
+    one = Cache(d, k, N, 2, 170, device)
+    out = run_tree(wide(one, 1 << 18) if large else one, q[:2], [150, 9], masks)
+    assert bool(out.isfinite().all())
+
+
 @pytest.mark.parametrize("outlier", [1e3, 3e4, 65504.0])
 @pytest.mark.parametrize("M,G", [(2, 2), (3, 4), (6, 5), (8, 8)], ids=str)
 @pytest.mark.parametrize("d,k,N", [(64, 4, 256), (64, 8, 16), (64, 1, 16), (128, 4, 256)], ids=str)
