@@ -152,7 +152,8 @@ __device__ __forceinline__ f4 load4(const void* q, int64_t at) {
   return f4{to_float(w[0]), to_float(w[1]), to_float(w[2]), to_float(w[3])};
 }
 
-// One block per item, then one that writes the ranges of `wgs` workgroups, then
+// One block per item (whatever its group's length: the lengths are read by the next
+// block alone, once), then one that writes the ranges of `wgs` workgroups, then
 // (staged codes) kTop that write partial maxima of the codebook.
 //
 // The rotation runs on v_mfma_f32_16x16x4_f32 (float32 products and sums; K slot
@@ -245,7 +246,6 @@ __global__ __launch_bounds__(256 * (RT > 1 ? 2 : 1)) void prep_kernel(const Args
   }
   const int64_t g = blockIdx.x / a.tiles;
   const int row0 = (int)(blockIdx.x % a.tiles) * ROWS;
-  if (runs_of(a, checked(a, a.lens[g])) == 0) return;
   const int c = lane & 15, g16 = lane >> 4;
   const int live = (min(ROWS, a.rows - row0) + 15) / 16;
   float top = 0.0f;
