@@ -365,7 +365,9 @@ size_t fibq_evict_workspace_bytes(int64_t n_groups, int64_t T_stride);
  * copied to the *_out arrays of T_out >= keep rows per group; new_lens[g] is
  * the number kept, index (device int32 [n_groups][keep]) is -1 behind it, and
  * rows of the new cache behind it are left as they are.  A length outside
- * [0, T_stride] gives new_lens[g] = -1, an index of -1 and no rows.
+ * [0, T_stride] gives new_lens[g] = -1, an index of -1 and no rows.  lens and
+ * acc must stay as they are until the call has run: it reads them more than
+ * once (else nothing is accessed out of range, but what is kept is open).
  * 1 <= keep < 2^30, 0 <= recent <= keep, 1 <= P <= 256.  No output may overlap
  * an input (FIBQ_EINVAL for the same address).  workspace: device, at least
  * fibq_evict_workspace_bytes(...) bytes, 256-byte aligned, else

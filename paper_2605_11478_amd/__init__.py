@@ -682,7 +682,8 @@ def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=N
     of T_out rows per group (keep, or what ``out`` has), its lengths and the old
     index of every row (int32 [n_groups, keep], -1 behind the last).  Rows
     behind the new length are not written.  ``out``: seven such tensors, none
-    sharing memory with an input.
+    sharing memory with an input.  ``acc`` and ``lens`` must not be written while
+    the call runs.
     """
     fast = _compiled(lens)
     if fast is not None and out is not None:

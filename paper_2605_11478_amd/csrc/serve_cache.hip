@@ -259,7 +259,8 @@ __device__ void emit(const uint32_t (&u)[E], int t0, const Found& f, int larger,
     for (int i = 0; i < 4; ++i) {
       const bool gt = u[4 * j + i] > top, eq = u[4 * j + i] == top;
       // (the bound holds by the counts; it is checked, since sliced passes read
-      // accumulators that another stream might be writing)
+      // lengths and accumulators that another stream might be writing.  Places may
+      // then stay unwritten, so that gather_kernel checks what it reads there.)
       const int at = g + min(e, f.need);
       if ((gt || (eq && e < f.need)) && (uint32_t)at < (uint32_t)keep)
         out[at] = t0 + 4096 * j + 4 * (int)threadIdx.x + i;
@@ -383,7 +384,8 @@ __global__ __launch_bounds__(kSel) void slice_kernel(const Sel p, int pass) {
 // divides P and that all addresses are aligned to: at P = 48, 262144 rows, 12 us
 // against 26 with single bytes).  What bounds it is the lines that it touches: at
 // P = 4 a quarter of the rows is kept and nearly every 128-byte line holds one (2.9 M
-// of 11.5 M rows: 36 us, 248 MB, whatever the width).
+// of 11.5 M rows: 36 us, 248 MB, whatever the width).  An index outside the old cache
+// copies nothing.
 template <typename V>
 __global__ __launch_bounds__(256) void gather_kernel(
     const uint8_t* __restrict__ kp, const uint16_t* __restrict__ kn,
@@ -397,7 +399,8 @@ __global__ __launch_bounds__(256) void gather_kernel(
   const int n = min(256, keep - i0), tid = threadIdx.x;
   __shared__ int32_t id[256];
   if (tid < n) {
-    const int32_t t = index[g * keep + i0 + tid];
+    int32_t t = index[g * keep + i0 + tid];
+    if (t >= T_stride) t = -1;
     id[tid] = t;
     if (t >= 0) {
       const int64_t to = g * T_out + i0 + tid, from = g * T_stride + t;

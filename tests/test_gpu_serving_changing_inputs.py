@@ -45,3 +45,37 @@ def test_lengths_written_meanwhile(device, k, N, G):
         # (a group's range may be cut elsewhere: two float32 results of one row)
         assert err.numel() == 0 or bool((err <= 2.0**-16 * ref.norm(dim=-1, keepdim=True)).all())
     assert bool(acc.isfinite().all()) and torch.count_nonzero(acc[:, L:]) == 0
+
+
+def test_evict_inputs_written_meanwhile(device):
+    """A cache in slices whose accumulators and lengths change between the passes, and index
+    places that hold large numbers before the call: rows come from the old cache or stay."""
+    rng = np.random.default_rng(52)
+    n, T, keep = 4, 40000, 9000
+    c = Cache(64, 8, 16, n, T, device)
+    laws = [torch.from_numpy(rng.random((n, T)).astype(np.float32) * s).to(device) for s in (1, -1, 1e-20)]
+    acc = laws[0].clone()
+    lens = torch.full((n,), T, dtype=torch.int32, device=device)
+    out = [torch.zeros(n, keep, *x.shape[2:], dtype=x.dtype, device=device) for x in c.dev]
+    out += [torch.zeros(n, keep, device=device), lens.clone(), torch.zeros(n, keep, dtype=torch.int32, device=device)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for r in range(8):
+        out[6].fill_(2**31 - 1 - r)
+        for o in out[:5]:
+            o.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for i in range(16):
+                acc.copy_(laws[i % 3])
+                lens.fill_((T, keep + 1, -1, T + 1)[i % 4])
+        fq.evict(*c.dev, acc, lens, keep, 100, out=out)
+        torch.cuda.synchronize()
+        index = out[6].long()
+        live = (index >= 0) & (index < T)
+        assert bool(((index == -1) | live | (index == 2**31 - 1 - r)).all())
+        at = index.clamp(0, T - 1)
+        for x, o in zip(c.dev, out):
+            rows = x.gather(1, at[:, :, None].expand(-1, -1, x.shape[2]) if x.dim() == 3 else at)
+            keepers = live[:, :, None] if x.dim() == 3 else live
+            assert torch.equal(torch.where(keepers, rows, torch.zeros_like(rows)), o)
