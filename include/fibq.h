@@ -369,7 +369,7 @@ size_t fibq_evict_workspace_bytes(int64_t n_groups, int64_t T_stride);
  * acc must stay as they are until the call has run: it reads them more than
  * once (else nothing is accessed out of range, but what is kept is open).
  * 1 <= keep < 2^30, 0 <= recent <= keep, 1 <= P <= 256.  No output may overlap
- * an input (FIBQ_EINVAL for the same address).  workspace: device, at least
+ * an input or another output (FIBQ_EINVAL for the same address).  workspace: device, at least
  * fibq_evict_workspace_bytes(...) bytes, 256-byte aligned, else
  * FIBQ_EWORKSPACE. */
 int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t* v_payload,

@@ -682,7 +682,7 @@ def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=N
     of T_out rows per group (keep, or what ``out`` has), its lengths and the old
     index of every row (int32 [n_groups, keep], -1 behind the last).  Rows
     behind the new length are not written.  ``out``: seven such tensors, none
-    sharing memory with an input.  ``acc`` and ``lens`` must not be written while
+    sharing memory with an input or another of them.  ``acc`` and ``lens`` must not be written while
     the call runs.
     """
     fast = _compiled(lens)
@@ -717,11 +717,13 @@ def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=N
     outs = dict(k_payload_out=kpo, k_norms_out=kno, v_payload_out=vpo, v_norms_out=vno,
                 acc_out=acco, new_lens=lenso, index=index)
     _here(lens, workspace=workspace, **ins, **outs)
-    for x, a in ins.items():
-        for y, b in outs.items():
+    taken = dict(ins)
+    for y, b in outs.items():
+        for x, a in taken.items():
             if (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size()
                     and b.data_ptr() < a.data_ptr() + a.numel() * a.element_size()):
                 raise ValueError(f"{y} overlaps {x}")
+        taken[y] = b
     st = lib().fibq_evict(k_payload.data_ptr(), k_norms.data_ptr(), v_payload.data_ptr(),
                           v_norms.data_ptr(), acc.data_ptr(), lens.data_ptr(), n_groups, T_stride,
                           P, keep, recent, T_out, kpo.data_ptr(), kno.data_ptr(), vpo.data_ptr(),

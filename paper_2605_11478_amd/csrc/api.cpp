@@ -474,9 +474,12 @@ int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t*
   const void* in[] = {k_payload, k_norms, v_payload, v_norms, acc, lens};
   const void* o[] = {k_payload_out, k_norms_out, v_payload_out, v_norms_out, acc_out, new_lens,
                      index};
-  for (const void* x : in)
-    for (const void* y : o)
+  for (const void*& y : o) {
+    for (const void* x : in)
       if (x == y) return FIBQ_EINVAL;
+    for (const void** x = o; x != &y; ++x)
+      if (*x == y) return FIBQ_EINVAL;
+  }
   const int rc = check_workspace(workspace, workspace_bytes,
                                  fibq::dev::evict_workspace_bytes(n_groups, T_stride));
   if (rc != FIBQ_OK) return rc;

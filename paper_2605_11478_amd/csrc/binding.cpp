@@ -457,11 +457,16 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                         given(outs[4], at::kFloat, {r.n, o.T}, r.dev), given(outs[5], at::kInt, {r.n}, r.dev),
                         given(outs[6], at::kInt, {r.n, n_keep}, r.dev)};
   if (!in[4] || !in[5] || !to[4] || !to[5] || !to[6]) FIBQ_NONE;
-  for (const Tensor* x : in)  // (no output may share memory with an input)
-    for (const Tensor* y : to) {
-      const char *px = static_cast<const char*>(ptr(*x)), *py = static_cast<const char*>(ptr(*y));
-      if (px < py + y->nbytes() && py < px + x->nbytes()) FIBQ_NONE;
-    }
+  auto shared = [](const Tensor* x, const Tensor* y) {
+    const char *px = static_cast<const char*>(ptr(*x)), *py = static_cast<const char*>(ptr(*y));
+    return px < py + y->nbytes() && py < px + x->nbytes();
+  };
+  for (const Tensor*& y : to) {  // (no output may share memory with an input or another output)
+    for (const Tensor* x : in)
+      if (shared(x, y)) FIBQ_NONE;
+    for (const Tensor** x = to; x != &y; ++x)
+      if (shared(*x, y)) FIBQ_NONE;
+  }
   const int64_t need = (int64_t)g_evict_ws(r.n, r.T);
   Tensor ws;
   if (!workspace(a[9], need, r.dev, &ws)) FIBQ_NONE;
