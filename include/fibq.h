@@ -324,7 +324,7 @@ int fibq_attn_tree(const void* q, int q_dtype, const uint8_t* k_payload,
 /* Acceptance of a drafted path, in place: row lens[g] + i of K and V (payload
  * and norm) becomes row lens[g] + path[g * path_len + i] for i < n_acc[g] (all
  * are read before any is written), and new_lens[g] = lens[g] + n_acc[g].
- * new_lens may be lens.  P: payload bytes of a row (fibq_payload_bytes),
+ * new_lens may be lens, and overlaps no input otherwise.  P: payload bytes of a row (fibq_payload_bytes),
  * 1 <= P <= 256; 1 <= M <= 64 drafted tokens, 1 <= path_len <= 64.  A group
  * with a length outside [0, T_stride - M], a count outside
  * [0, min(path_len, M)] or a path entry (of the first n_acc[g]) outside [0, M)

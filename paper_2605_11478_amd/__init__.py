@@ -535,6 +535,12 @@ def _here(t, **tensors):
         raise ValueError(f"tensors are on {t.device}, which is not the current device")
 
 
+def _shared(a, b):
+    """Whether two dense tensors have any memory in common."""
+    return (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size()
+            and b.data_ptr() < a.data_ptr() + a.numel() * a.element_size())
+
+
 def _check_cache(k_payload, k_norms, v_payload, v_norms, lens, P=None):
     """One cache of groups and its lengths; returns (n_groups, T_stride, P)."""
     torch = _torch()
@@ -604,7 +610,8 @@ def accept_draft(k_payload, k_norms, v_payload, v_norms, lens, M, path, n_acc, n
     """Moves the accepted path of M drafted tokens to the end of each group's
     context, in place: row lens[g] + i <- row lens[g] + path[g, i] for
     i < n_acc[g].  path int32 [n_groups, A], n_acc int32 [n_groups].
-    -> new_lens = lens + n_acc (pass ``new_lens=lens`` to update it in place);
+    -> new_lens = lens + n_acc (pass ``new_lens=lens`` to update it in place; it
+    may not share memory with the inputs otherwise);
     -1 for a group with a bad length, count or path, whose rows stay.
     """
     fast = _compiled(lens)
@@ -622,6 +629,9 @@ def accept_draft(k_payload, k_norms, v_payload, v_norms, lens, M, path, n_acc, n
     _want(new_lens, "new_lens", (torch.int32,), (n_groups,))
     _here(lens, k_payload=k_payload, k_norms=k_norms, v_payload=v_payload, v_norms=v_norms,
           lens=lens, path=path, n_acc=n_acc, new_lens=new_lens)
+    for x, t in dict(lens=lens, n_acc=n_acc, path=path).items():
+        if _shared(t, new_lens) and (x == "path" or t.data_ptr() != new_lens.data_ptr()):
+            raise ValueError(f"new_lens overlaps {x}")
     st = lib().fibq_accept_draft(k_payload.data_ptr(), k_norms.data_ptr(), v_payload.data_ptr(),
                                  v_norms.data_ptr(), lens.data_ptr(), n_groups, T_stride, P, M,
                                  path.data_ptr(), path.shape[1], n_acc.data_ptr(),
@@ -720,8 +730,7 @@ def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=N
     taken = dict(ins)
     for y, b in outs.items():
         for x, a in taken.items():
-            if (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size()
-                    and b.data_ptr() < a.data_ptr() + a.numel() * a.element_size()):
+            if _shared(a, b):
                 raise ValueError(f"{y} overlaps {x}")
         taken[y] = b
     st = lib().fibq_evict(k_payload.data_ptr(), k_norms.data_ptr(), v_payload.data_ptr(),

@@ -289,6 +289,10 @@ const Tensor* given(PyObject* o, at::ScalarType ty, std::initializer_list<int64_
   const Tensor* t = tensor(o);
   return shaped(t, ty, s) && t->device() == dev ? t : nullptr;
 }
+bool shared(const Tensor* x, const Tensor* y) {  // any memory
+  const char *px = static_cast<const char*>(ptr(*x)), *py = static_cast<const char*>(ptr(*y));
+  return px < py + y->nbytes() && py < px + x->nbytes();
+}
 // an optional workspace of at least `need` bytes; false: not a valid one
 bool workspace(PyObject* o, int64_t need, at::Device dev, Tensor* ws) {
   if (o == Py_None) return true;
@@ -421,6 +425,8 @@ PyObject* accept(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (a[8] != Py_None) {
     const Tensor* t = given(a[8], at::kInt, {r.n}, r.dev);
     if (!t) FIBQ_NONE;
+    for (const Tensor* x : {lens, n_acc, path})  // (lens or n_acc itself is fine)
+      if (shared(x, t) && (x == path || ptr(*x) != ptr(*t))) FIBQ_NONE;
     out = *t;
   }
   const int32_t *pl = static_cast<const int32_t*>(ptr(*lens)), *pp = static_cast<const int32_t*>(ptr(*path)),
@@ -457,10 +463,6 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                         given(outs[4], at::kFloat, {r.n, o.T}, r.dev), given(outs[5], at::kInt, {r.n}, r.dev),
                         given(outs[6], at::kInt, {r.n, n_keep}, r.dev)};
   if (!in[4] || !in[5] || !to[4] || !to[5] || !to[6]) FIBQ_NONE;
-  auto shared = [](const Tensor* x, const Tensor* y) {
-    const char *px = static_cast<const char*>(ptr(*x)), *py = static_cast<const char*>(ptr(*y));
-    return px < py + y->nbytes() && py < px + x->nbytes();
-  };
   for (const Tensor*& y : to) {  // (no output may share memory with an input or another output)
     for (const Tensor* x : in)
       if (shared(x, y)) FIBQ_NONE;
