@@ -6,10 +6,12 @@
 // Mathematics.  In rotated space a score is nu_t <q~, c_(t)> with q~ = Pi q
 // times scale * log2 e, the softmax is base 2, and the values are
 // sum_t p_t nu_t c_(t), rotated back once per row.  q~ and the weights p nu are
-// held as two binary16 parts (22 bits together) against the binary16 codewords,
-// so the products on the matrix cores carry float32 accuracy; a codebook that
-// binary16 does not hold adds its residual rows' products.  Statistics and sums
-// are float32.
+// held as two binary16 parts (22 bits together) against the binary16 codewords:
+// q~ at a power of two of its row, weights down to 2^-32 of their row's largest
+// p nu (a smaller one is lost: at most 2^-33 of that, for each token).  A codebook
+// that binary16 does not hold adds its residual rows' products with the high parts
+// (packed queries: with both), which leaves out 2^-22 of a product.  Statistics and
+// sums are float32.
 //
 // An item is (group, tile of 16 RT query rows); its work is cut into units of 32
 // tokens.  The units of all items, in runs of 8 (one per wavefront of a
@@ -40,12 +42,13 @@
 //
 // What bounds them.  The work is far above the bytes (352 groups of 32k tokens at
 // k = 8 hold 138 MB, 27 us at a large copy's rate): rows_kernel is bound by the
-// vector instructions per unit with few rows (that cache, 8 rows: 113 us, 120
-// instructions per unit, 75 % of all issue cycles; its weights' pass 76 us), and
-// by vector and matrix instructions together with many (16 groups of 512 rows, 32k
-// tokens: 140 us, of which the two-part products take 63 at the rate of a large
-// matrix product; the two hardly overlap).  Small calls are three or four launches,
-// 12 to 20 us.
+// vector instructions per unit with few rows (that cache, 8 rows: 119 us, 126
+// instructions per unit, 71 % of all issue cycles; its weights' pass 77 us), and
+// by vector and matrix instructions and by unequal ranges with many (16 groups of up
+// to 512 rows, 32k tokens: 142 us, vector units 47 % and matrix units 25 % busy, compute
+// units 73 %, since a range that meets six items costs more than one that meets five;
+// the two-part products take 63 us at the rate of a large matrix product).  Small
+// calls are three or four launches, 12 to 21 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -125,7 +128,8 @@ constexpr int state_floats(int D, int RT, bool PK) { return state_regs(D, RT) * 
 // item's, which is the last (negative: not all rows' are 1)
 __host__ __device__ constexpr int qs_floats(int RT) { return RT > 1 ? 16 * RT + 1 : 16; }
 // the queries' low parts: in registers for one row tile, else in LDS (they are 32
-// of 256 registers at four tiles, where the unit loop spilled without)
+// of 256 registers at four tiles; 26 to 39 still spill there, outside the unit loop, and
+// 60 of staged codes)
 constexpr int ops_bytes(int D, int RT) { return RT > 1 ? RT * (D / 32) * 1024 : 0; }
 
 // runs of units of a group of this length (-1: bad, none)
