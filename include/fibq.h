@@ -379,6 +379,129 @@ int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t*
                uint16_t* v_norms_out, float* acc_out, int32_t* new_lens, int32_t* index,
                void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------- paged 8-bit cache --
+ * Keys and values in 8 bits with one scale per page and head, for layers or
+ * tokens that are not coded, with the block tables, the rotary positions and
+ * the attention of a serving loop.  A page holds `page` tokens of one sequence;
+ * sequence g's token t is row t % page of page table[g][t / page].
+ * k_pages, v_pages: device [n_pages][H][page][d] bytes, 16-byte aligned, of
+ * codes FIBQ_INT8 (-127 .. 127) or FIBQ_E4M3 (1-4-3 floating point, largest 448,
+ * no infinities); k_scales, v_scales: device float [n_pages][H]; an element is
+ * code x scale.  H key/value heads, G query heads on each (query head h uses
+ * head h / G).  Lengths and tables live on the device (int32), so a captured
+ * call follows them.  Common limits (else FIBQ_EINVAL): 0 <= n_seqs <= 65535,
+ * 0 <= n_rows and fewer than 2^31 elements in a matrix of rows, page in
+ * {16, 32, 64, 128}, max_pages * page < 2^30, 1 <= H <= 1024,
+ * 1 <= n_pages < 2^31; d in {64, 128, 256} (else FIBQ_EUNSUPPORTED).  Rows are
+ * those of all sequences, one sequence behind the other: sequence g has rows
+ * starts[g] .. starts[g + 1] - 1. */
+#define FIBQ_INT8 0
+#define FIBQ_E4M3 1
+
+#define FIBQ_ROPE_HALF 0        /* pair i: elements i and i + rot / 2 */
+#define FIBQ_ROPE_INTERLEAVED 1 /* pair i: elements 2 i and 2 i + 1   */
+
+/* Rotary positions: in every head of row r of q and k, pair i (x0, x1) of the
+ * first `rot` elements becomes
+ *   scale (x0 cos a - x1 sin a), scale (x1 cos a + x0 sin a),
+ *   a = positions[r] freqs[i]  (inverse != 0: -a),
+ * and the elements from rot on are copied.  The inverse with the same scale is
+ * the gradient.  Angles are reduced in double; products and sums are float, and
+ * the result is rounded once to dtype.  q: device, element e of head h of row r
+ * at r * q_row_stride + h * q_head_stride + e, q_heads heads; k likewise, or
+ * k_heads = 0.  Outputs likewise; an output may be its input (the same address
+ * and strides) and has no memory in common with any other tensor.  positions:
+ * device int32 [n_rows], any value; freqs: device double [rot / 2], radians per
+ * position.  d even, 2 <= d <= 512, rot even, 2 <= rot <= d; heads in all at
+ * most 2048; fewer than 2^31 rows. */
+int fibq_rope(const void* q, const void* k, int dtype, int64_t n_rows, int q_heads, int k_heads,
+              int d, int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride,
+              int64_t k_head_stride, const int32_t* positions, const double* freqs, int rot,
+              int layout, float scale, int inverse, void* q_out, void* k_out,
+              int64_t q_out_row_stride, int64_t q_out_head_stride, int64_t k_out_row_stride,
+              int64_t k_out_head_stride, void* stream);
+
+/* Workspace bytes of fibq_page_resize. */
+size_t fibq_page_resize_workspace_bytes(int64_t n_seqs);
+
+/* Block tables and slot maps from request lengths.  Request g holds lens[g]
+ * tokens and gets grow[g] new ones, or gives -grow[g] of its last ones back.
+ * Its tokens' pages are table[g * max_pages ..].  free_pages (device int32, room
+ * for free_cap) is a stack of page ids, *n_free of them free.  In this order:
+ *   starts[g] = the positive grow of the requests before g, summed (clipped to
+ *     n_rows); starts has n_seqs + 1 entries;
+ *   pages that a request needs no more go onto the stack (requests and pages in
+ *     order; those behind free_cap are lost);
+ *   pages for new tokens are taken from its top, first come, first served: a
+ *     request whose pages, with those of all before it, are more than the stack
+ *     holds gets none and is refused (one that needs no page never is);
+ *   new_lens[g] = lens[g] + grow[g], or -1 for a refused request, for one whose
+ *     old or new length is outside [0, max_pages * page], and for one whose rows
+ *     end behind n_rows; such a request's table stays as it is;
+ *   row r of request g, its i-th, gets position positions[r] = lens[g] + i and
+ *     slot slots[r] = table[g][position / page] * page + position % page; rows of
+ *     a request with new_lens -1 and rows behind the last get -1 and -1, and a
+ *     page id outside [0, n_pages) gives slot -1;
+ *   *new_free = the pages that are left.
+ * A slot is a row of a cache of n_pages * page rows; fibq_decode takes slots as
+ * token_ids.  new_lens may be lens, and new_free n_free; outputs overlap nothing
+ * otherwise.  lens, grow, table and free_pages are not written by others while
+ * the call runs.  1 <= page <= 65536 here; free_cap < 2^31, n_rows < 2^31. */
+int fibq_page_resize(int32_t* table, const int32_t* lens, const int32_t* grow, int64_t n_seqs,
+                     int64_t max_pages, int page, int64_t n_pages, int32_t* free_pages,
+                     int64_t free_cap, const int32_t* n_free, int64_t n_rows, int32_t* new_lens,
+                     int32_t* starts, int64_t* slots, int32_t* positions, int32_t* new_free,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Writes rows of keys and values into the pages at their slots (-1 or any other
+ * slot outside the pool: the row is left out).  A page and head's scale is the
+ * least power of two, from 2^-126 on, that takes the largest magnitude written
+ * since the page was begun (its first row written) to the codes' range; where it
+ * grows, the rows before are rounded again to the new scale:
+ *   s = max(s_old, least), code = round(x / s), code' = round(code s_old / s),
+ * ties to even; s = 0 for a page of zeros.  s_old need not be a power of two.
+ * An infinity or NaN among a head's new elements of a page makes its scale NaN
+ * (until the page is begun again) and its new codes 0: rows that read the page
+ * give NaN.  The rows of one page follow each other in the call at increasing
+ * slots, and no page is written from two places of a call (else its contents are
+ * open; nothing is accessed out of range).  k, v: element e of head h of row r at
+ * r * row_stride + h * head_stride + e.  No memory is shared with the pages. */
+int fibq_cache8_write(const void* k, const void* v, int dtype, int64_t n_rows,
+                      int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride,
+                      int64_t v_head_stride, const int64_t* slots, int H, int d, int page,
+                      int64_t n_pages, int codes, void* k_pages, float* k_scales, void* v_pages,
+                      float* v_scales, void* stream);
+
+/* Workspace bytes of fibq_attn_cache8 (0 for an invalid problem, or if it needs none). */
+size_t fibq_attn_cache8_workspace_bytes(int64_t n_seqs, int64_t n_rows, int H, int G,
+                                        int64_t max_pages, int page, int d);
+
+/* Attention over the paged cache: for row i of the M rows of sequence g and query
+ * head h,
+ *   o = sum_t softmax_t(scale <q, K_t>) V_t over t < lens[g] - M + i + 1 if causal
+ *   (the rows are the sequence's last M tokens), else over t < lens[g] (cross
+ *   attention to states of another length).
+ * scale <= 0 selects 1/sqrt(d).  q: device [n_rows][H * G][d] of q_dtype; out:
+ * device float of the same shape.  table: device int32 [n_seqs][max_pages]; starts: device
+ * int32 [n_seqs + 1], or NULL for one row per sequence (n_rows = n_seqs).  A row
+ * that sees no token gives zeros; rows of a sequence whose length is outside
+ * [0, max_pages * page], or less than its rows if causal, are NaN and nothing of
+ * its cache is read.  A page id outside [0, n_pages) makes the rows that see its
+ * tokens NaN.  Rows that belong to no sequence are left as they are; a sequence
+ * whose starts are not 0 <= starts[g] <= starts[g + 1] <= n_rows has none, and rows
+ * that two sequences claim are open.  What
+ * lies behind a sequence's last token is never used, whatever it holds.  Scores
+ * are limited to +-2^126, so that finite queries and elements give finite rows.
+ * 1 <= G <= 16.  workspace: device, at least
+ * fibq_attn_cache8_workspace_bytes(...) bytes, 256-byte aligned, else
+ * FIBQ_EWORKSPACE; calls that overlap in time need one each. */
+int fibq_attn_cache8(const void* q, int q_dtype, const void* k_pages, const float* k_scales,
+                     const void* v_pages, const float* v_scales, int codes, const int32_t* table,
+                     const int32_t* lens, const int32_t* starts, int64_t n_seqs, int64_t n_rows,
+                     int H, int G, int64_t max_pages, int page, int64_t n_pages, int d,
+                     int causal, float scale, float* out, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -94,6 +94,20 @@ def lib():
             "fibq_evict": (c_i, [c_p, c_p, c_p, c_p, c_p, c_p, c_i64, c_i64, c_i, c_i64, c_i64,
                                  c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p, ctypes.c_size_t,
                                  c_p]),
+            "fibq_rope": (c_i, [c_p, c_p, c_i, c_i64, c_i, c_i, c_i, c_i64, c_i64, c_i64, c_i64,
+                                c_p, c_p, c_i, c_i, c_f, c_i, c_p, c_p, c_i64, c_i64, c_i64, c_i64,
+                                c_p]),
+            "fibq_page_resize_workspace_bytes": (ctypes.c_size_t, [c_i64]),
+            "fibq_page_resize": (c_i, [c_p, c_p, c_p, c_i64, c_i64, c_i, c_i64, c_p, c_i64, c_p,
+                                       c_i64, c_p, c_p, c_p, c_p, c_p, c_p, ctypes.c_size_t,
+                                       c_p]),
+            "fibq_cache8_write": (c_i, [c_p, c_p, c_i, c_i64, c_i64, c_i64, c_i64, c_i64, c_p,
+                                        c_i, c_i, c_i, c_i64, c_i, c_p, c_p, c_p, c_p, c_p]),
+            "fibq_attn_cache8_workspace_bytes": (ctypes.c_size_t, [c_i64, c_i64, c_i, c_i, c_i64,
+                                                                   c_i, c_i]),
+            "fibq_attn_cache8": (c_i, [c_p, c_i, c_p, c_p, c_p, c_p, c_i, c_p, c_p, c_p, c_i64,
+                                       c_i64, c_i, c_i, c_i64, c_i, c_i64, c_i, c_i, c_f, c_p,
+                                       c_p, ctypes.c_size_t, c_p]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -121,6 +135,10 @@ def _bind(L):
                             ("fibq_attn_tree", "fibq_attn_tree_workspace_bytes",
                              "fibq_attn_decode_accum", "fibq_attn_decode_accum_workspace_bytes",
                              "fibq_accept_draft", "fibq_evict", "fibq_evict_workspace_bytes")))
+    _binding.bind_paged(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in
+                          ("fibq_rope", "fibq_page_resize", "fibq_page_resize_workspace_bytes",
+                           "fibq_cache8_write", "fibq_attn_cache8",
+                           "fibq_attn_cache8_workspace_bytes")))
     _fast = _binding
     _bound = True
 
@@ -739,4 +757,333 @@ def evict(k_payload, k_norms, v_payload, v_norms, acc, lens, keep, recent, out=N
                           vno.data_ptr(), acco.data_ptr(), lenso.data_ptr(), index.data_ptr(),
                           workspace.data_ptr(), workspace.numel(), _stream())
     _check(st, "fibq_evict")
+    return out
+
+
+# ------------------------------------------------------- paged 8-bit cache ----
+# Keys and values in 8 bits with one scale per page and head: pages int8 or
+# float8_e4m3fn [n_pages, H, page, d], scales float32 [n_pages, H]; tables int32
+# [n_seqs, max_pages]; rows of all sequences one behind the other.
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def rope_freqs(rot, base=10000.0, scaling=None, factor=1.0, trained=0, low=1.0, high=32.0):
+    """Radians per position of each of the rot / 2 pairs (float64, host):
+    f_i = base^(-2 i / rot), and for positions beyond the ``trained`` ones
+
+    * ``scaling=None``: as they are;
+    * ``"linear"``: f_i / factor;
+    * ``"base"``: the base grows to base * factor^(rot / (rot - 2)), which leaves the
+      fastest pair as it is and divides the slowest by ``factor``;
+    * ``"ramp"``: w_i f_i + (1 - w_i) f_i / factor, where w_i = clamp((n_i - low) /
+      (high - low), 0, 1) and n_i = trained * f_i / 2 pi are the pair's turns over
+      the trained positions: pairs of many turns keep their speed."""
+    if rot < 2 or rot % 2:
+        raise ValueError(f"rot = {rot} must be even and at least 2")
+    if not (base > 0 and factor > 0 and math.isfinite(base) and math.isfinite(factor)):
+        raise ValueError("base and factor must be positive numbers")
+    i = np.arange(rot // 2, dtype=np.float64)
+    if scaling == "base":
+        if rot == 2:
+            raise ValueError('scaling "base" needs rot > 2')
+        base *= factor ** (rot / (rot - 2))
+    f = np.float64(base) ** (-2.0 * i / rot)
+    if scaling == "linear":
+        return f / factor
+    if scaling == "ramp":
+        if trained < 1 or not high > low:
+            raise ValueError('scaling "ramp" needs trained >= 1 and high > low')
+        w = np.clip((trained * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+        return w * f + (1.0 - w) * f / factor
+    if scaling not in (None, "base"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f
+
+
+def _head_rows(t, name, dtypes, shape):
+    """Rows of heads [n, H, d] with dense heads, at any row and head strides."""
+    _want(t, name, dtypes, shape, contiguous=False)
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name} must have contiguous heads")
+
+
+def _extent(t):
+    """First byte, and the byte behind the last, of a strided tensor."""
+    if t.numel() == 0:
+        return t.data_ptr(), t.data_ptr()
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+
+
+def _same_rows(a, b):
+    return a.data_ptr() == b.data_ptr() and a.stride() == b.stride()
+
+
+def _apart(a, b):
+    """Whether rows of heads have no memory in common: extents that do not meet, or
+    parts of rows of one matrix whose columns do not."""
+    (a0, a1), (b0, b1) = _extent(a), _extent(b)
+    if a1 <= b0 or b1 <= a0:
+        return True
+    row = a.stride(0) * a.element_size()
+    if row != b.stride(0) * b.element_size() or row == 0:
+        return False
+    wide = [((t.shape[1] - 1) * t.stride(1) + t.shape[2]) * t.element_size() for t in (a, b)]
+    at = (b0 - a0) % row
+    return wide[0] <= at and at + wide[1] <= row
+
+
+def _apart_from_itself(t, name):
+    n, H, d = t.shape
+    row, head = t.stride(0), t.stride(1)
+    if not ((head >= d or H == 1) and (row >= (H - 1) * head + d or n == 1)
+            or row >= d and head >= (n - 1) * row + d):
+        raise ValueError(f"{name} holds an element twice")
+
+
+def rope(q, k, positions, freqs, layout="half", scale=1.0, inverse=False, out=None):
+    """Rotary positions of queries and keys in one call.
+
+    q [n, Hq, d] and k [n, Hk, d] or None (float32, float16 or bfloat16; dense heads at
+    any strides, such as parts of one projection); positions int32 [n]; freqs float64
+    [rot / 2] on the device (``rope_freqs``), rot <= d: the first rot elements of each
+    head turn, the others are copied.  ``layout`` "half" pairs elements i and
+    i + rot / 2, "interleaved" 2 i and 2 i + 1.  ``scale`` multiplies the turned
+    elements; ``inverse`` turns back, which with the same scale is the gradient.
+    -> (q, k) turned, new and dense, or in ``out``, a pair; out=(q, k) works in place.
+    """
+    fast = _compiled(q)
+    if fast is not None:
+        done = fast.rope(q, k, positions, freqs,
+                         layout == "interleaved" if layout in ROPE_LAYOUTS else None, scale,
+                         inverse, out, _raw_stream(), _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
+    torch = _torch()
+    types = (torch.float32, torch.float16, torch.bfloat16)
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(ROPE_LAYOUTS)}")
+    _head_rows(q, "q", types, (None, None, None))
+    n, Hq, d = q.shape
+    if k is not None:
+        _head_rows(k, "k", (q.dtype,), (n, None, d))
+    _want(positions, "positions", (torch.int32,), (n,))
+    _want(freqs, "freqs", (torch.float64,), (None,))
+    if out is None:
+        out = tuple(None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                    for x in (q, k))
+    out = tuple(out)
+    if len(out) != 2 or (out[1] is None) != (k is None):
+        raise ValueError("out must hold an output for q and one for k, as they are given")
+    pairs = [("q", q, out[0])] + ([("k", k, out[1])] if k is not None else [])
+    for name, x, y in pairs:
+        _head_rows(y, f"{name} out", (q.dtype,), tuple(x.shape))
+        _apart_from_itself(y, f"{name} out")
+    _here(q, q=q, k=k, positions=positions, freqs=freqs, q_out=out[0], k_out=out[1])
+    for name, x, y in pairs:
+        for other, z, w in pairs:
+            if not (name == other and _same_rows(y, z)) and not _apart(y, z):
+                raise ValueError(f"{name} out overlaps {other}")
+            if name < other and not _apart(y, w):
+                raise ValueError(f"{name} out overlaps {other} out")
+        for other, t in (("positions", positions), ("freqs", freqs)):
+            (a0, a1), (b0, b1) = _extent(y), _extent(t)
+            if a0 < b1 and b0 < a1:
+                raise ValueError(f"{name} out overlaps {other}")
+    kk, ko = (k, out[1]) if k is not None else (q, out[0])
+    st = lib().fibq_rope(q.data_ptr(), None if k is None else k.data_ptr(), _dtype_code(q), n, Hq,
+                         0 if k is None else k.shape[1], d, *_strides(q), *_strides(kk),
+                         positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0],
+                         ROPE_LAYOUTS[layout], scale, int(bool(inverse)), out[0].data_ptr(),
+                         None if k is None else out[1].data_ptr(), *_strides(out[0]),
+                         *_strides(ko), _stream())
+    _check(st, "fibq_rope")
+    return out
+
+
+def _strides(t):
+    """Row and head strides as the library takes them: those of a single row or
+    head are open in torch and are given as if dense."""
+    n, H, d = t.shape
+    head = t.stride(1) if H > 1 else d
+    return (t.stride(0) if n > 1 else (H - 1) * head + d), head
+
+
+def page_resize_workspace_bytes(n_seqs):
+    return lib().fibq_page_resize_workspace_bytes(n_seqs)
+
+
+def page_resize(table, lens, grow, page, n_pages, free, n_free, n_rows, out=None, workspace=None):
+    """Block tables and slot maps from request lengths, on the device.
+
+    table int32 [n, max_pages] (in place); lens, grow int32 [n]: request g holds lens[g]
+    tokens and gets grow[g] new ones, or gives -grow[g] back; free int32 [F] (in place):
+    a stack of page ids, n_free int32 [1] of them free.  Pages given back go onto the
+    stack first, then requests take theirs from its top, first come, first served.
+    -> (new_lens [n], starts [n + 1], slots int64 [n_rows], positions int32 [n_rows],
+    new_free [1]), or those tensors in ``out``: row r of the new tokens of all requests,
+    one behind the other, has slot page id * page + offset and its position; a request
+    that cannot be served has new length -1, and its rows and those behind the last
+    slot and position -1.  In ``out``, new_lens may be ``lens`` and new_free ``n_free``;
+    nothing else may share memory.  ``slots`` are rows of a flat cache as well
+    (``token_ids`` of ``decode``).
+    """
+    fast = _compiled(lens)
+    if fast is not None:
+        done = fast.page_resize(table, lens, grow, page, n_pages, free, n_free, n_rows, out,
+                                workspace, _raw_stream(), _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
+    torch = _torch()
+    _want(table, "table", (torch.int32,), (None, None))
+    n, max_pages = table.shape
+    _want(lens, "lens", (torch.int32,), (n,))
+    _want(grow, "grow", (torch.int32,), (n,))
+    _want(free, "free", (torch.int32,), (None,))
+    _want(n_free, "n_free", (torch.int32,), (1,))
+    if not 0 <= n_rows < 1 << 31:
+        raise ValueError(f"n_rows = {n_rows} must lie in [0, 2^31)")
+    if out is None:
+        def new(m, dtype=torch.int32):
+            return torch.empty((m,), dtype=dtype, device=lens.device)
+        out = (new(n), new(n + 1), new(n_rows, torch.int64), new(n_rows), new(1))
+    out = tuple(out)
+    if len(out) != 5:
+        raise ValueError("out must hold five tensors")
+    names = ("new_lens", "starts", "slots", "positions", "new_free")
+    for name, t, m in zip(names, out, (n, n + 1, n_rows, n_rows, 1)):
+        _want(t, name, (torch.int64 if name == "slots" else torch.int32,), (m,))
+    workspace = _workspace(workspace, page_resize_workspace_bytes(n), lens.device)
+    ins = dict(table=table, lens=lens, grow=grow, free=free, n_free=n_free)
+    outs = dict(zip(names, out))
+    _here(lens, workspace=workspace, **ins, **outs)
+    may = {("new_lens", "lens"), ("new_free", "n_free")}
+    taken = dict(ins)
+    for x, a in ins.items():  # table and free are written
+        for y in ("table", "free"):
+            if x != y and _shared(a, ins[y]):
+                raise ValueError(f"{y} overlaps {x}")
+    for y, b in dict(outs, workspace=workspace).items():
+        for x, a in taken.items():
+            if _shared(a, b) and not ((y, x) in may and a.data_ptr() == b.data_ptr()):
+                raise ValueError(f"{y} overlaps {x}")
+        taken[y] = b
+    st = lib().fibq_page_resize(table.data_ptr(), lens.data_ptr(), grow.data_ptr(), n, max_pages,
+                                page, n_pages, free.data_ptr(), free.shape[0], n_free.data_ptr(),
+                                n_rows, *(t.data_ptr() for t in out), workspace.data_ptr(),
+                                workspace.numel(), _stream())
+    _check(st, "fibq_page_resize")
+    return out
+
+
+def _check_pages(k_pages, k_scales, v_pages, v_scales):
+    """The pools of a paged 8-bit cache; returns (n_pages, H, page, d, code)."""
+    torch = _torch()
+    codes = {torch.int8: 0, torch.float8_e4m3fn: 1}
+    _want(k_pages, "k_pages", tuple(codes), (None, None, None, None))
+    n_pages, H, page, d = k_pages.shape
+    _want(v_pages, "v_pages", (k_pages.dtype,), (n_pages, H, page, d))
+    _want(k_scales, "k_scales", (torch.float32,), (n_pages, H))
+    _want(v_scales, "v_scales", (torch.float32,), (n_pages, H))
+    return n_pages, H, page, d, codes[k_pages.dtype]
+
+
+def cache8_write(k, v, slots, k_pages, k_scales, v_pages, v_scales):
+    """Writes keys and values [n, H, d] (dense heads, any strides) into the pages of an
+    8-bit cache at slots int64 [n] (-1: left out), in place.
+
+    The scale of a page and head is the least power of two that takes everything
+    written since the page was begun to the codes' range; where it grows, the rows
+    before are rounded again.  Rows of one page follow each other at increasing slots.
+    A NaN or infinity makes the scale of its page and head NaN.
+    """
+    fast = _compiled(k)
+    if fast is not None:
+        done = fast.cache8_write(k, v, slots, k_pages, k_scales, v_pages, v_scales, _raw_stream(),
+                                 _torch()._C._cuda_getDevice())
+        if done is not None:
+            return
+    torch = _torch()
+    n_pages, H, page, d, code = _check_pages(k_pages, k_scales, v_pages, v_scales)
+    _head_rows(k, "k", (torch.float32, torch.float16, torch.bfloat16), (None, H, d))
+    n = k.shape[0]
+    _head_rows(v, "v", (k.dtype,), (n, H, d))
+    _want(slots, "slots", (torch.int64,), (n,))
+    ins = dict(k=k, v=v, slots=slots)
+    pools = dict(k_pages=k_pages, k_scales=k_scales, v_pages=v_pages, v_scales=v_scales)
+    _here(k, **ins, **pools)
+    taken = dict(ins)
+    for y, b in pools.items():
+        for x, a in taken.items():
+            (a0, a1), (b0, b1) = _extent(a), _extent(b)
+            if a0 < b1 and b0 < a1:
+                raise ValueError(f"{y} overlaps {x}")
+        taken[y] = b
+    st = lib().fibq_cache8_write(k.data_ptr(), v.data_ptr(), _dtype_code(k), n, *_strides(k),
+                                 *_strides(v), slots.data_ptr(), H, d, page, n_pages, code,
+                                 k_pages.data_ptr(), k_scales.data_ptr(), v_pages.data_ptr(),
+                                 v_scales.data_ptr(), _stream())
+    _check(st, "fibq_cache8_write")
+
+
+def attn_cache8_workspace_bytes(n_seqs, n_rows, H, G, max_pages, page, d):
+    return lib().fibq_attn_cache8_workspace_bytes(n_seqs, n_rows, H, G, max_pages, page, d)
+
+
+def attn_cache8(q, k_pages, k_scales, v_pages, v_scales, table, lens, starts=None, causal=True,
+                scale=0.0, workspace=None, out=None):
+    """Attention over the paged 8-bit cache.
+
+    q [n_rows, Hq, d], Hq = H * G; table int32 [n_seqs, max_pages], lens int32 [n_seqs];
+    starts int32 [n_seqs + 1]: sequence g has rows starts[g] .. starts[g + 1] - 1 (None:
+    one row each).  ``causal``: the rows are the sequence's last tokens, and each sees
+    those up to itself; else every row sees all lens[g] (cross attention).
+    -> out float32 [n_rows, Hq, d].  Rows of a sequence with a bad length are NaN, rows
+    of no sequence are not written, and rows that see nothing are zero.  ``workspace`` as
+    for ``attn_decode`` (``attn_cache8_workspace_bytes``).
+    """
+    fast = _compiled(q)
+    if fast is not None:
+        done = fast.attn_cache8(q, k_pages, k_scales, v_pages, v_scales, table, lens, starts,
+                                causal, scale, workspace, out, _raw_stream(),
+                                _torch()._C._cuda_getDevice())
+        if done is not None:
+            return done
+    torch = _torch()
+    n_pages, H, page, d, code = _check_pages(k_pages, k_scales, v_pages, v_scales)
+    _want(q, "q", (torch.float32, torch.float16, torch.bfloat16), (None, None, d))
+    n_rows, Hq, _ = q.shape
+    if H < 1 or Hq < 1 or Hq % H:
+        raise ValueError(f"q has {Hq} heads, which is no multiple of the cache's {H}")
+    _want(table, "table", (torch.int32,), (None, None))
+    n_seqs, max_pages = table.shape
+    _want(lens, "lens", (torch.int32,), (n_seqs,))
+    if starts is not None:
+        _want(starts, "starts", (torch.int32,), (n_seqs + 1,))
+    elif n_rows != n_seqs:
+        raise ValueError(f"q has {n_rows} rows for {n_seqs} sequences: starts must be given")
+    if out is None:
+        out = torch.empty((n_rows, Hq, d), dtype=torch.float32, device=q.device)
+    _want(out, "out", (torch.float32,), (n_rows, Hq, d))
+    workspace = _workspace(workspace, attn_cache8_workspace_bytes(n_seqs, n_rows, H, Hq // H,
+                                                                  max_pages, page, d), q.device)
+    ins = dict(q=q, k_pages=k_pages, k_scales=k_scales, v_pages=v_pages, v_scales=v_scales,
+               table=table, lens=lens)
+    if starts is not None:
+        ins["starts"] = starts
+    _here(q, out=out, workspace=workspace, **ins)
+    for x, a in ins.items():
+        if _shared(a, out):
+            raise ValueError(f"out overlaps {x}")
+        if _shared(a, workspace):
+            raise ValueError(f"workspace overlaps {x}")
+    if _shared(out, workspace):
+        raise ValueError("workspace overlaps out")
+    st = lib().fibq_attn_cache8(q.data_ptr(), _dtype_code(q), k_pages.data_ptr(),
+                                k_scales.data_ptr(), v_pages.data_ptr(), v_scales.data_ptr(), code,
+                                table.data_ptr(), lens.data_ptr(),
+                                None if starts is None else starts.data_ptr(), n_seqs, n_rows, H,
+                                Hq // H, max_pages, page, n_pages, d, int(bool(causal)), scale,
+                                out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "fibq_attn_cache8")
     return out

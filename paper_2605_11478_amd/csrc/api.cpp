@@ -490,4 +490,162 @@ int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t*
                                             stream));
 }
 
+// ------------------------------------------------------- paged 8-bit cache --
+static bool dtype_known(int dtype) {
+  return dtype == FIBQ_F32 || dtype == FIBQ_F16 || dtype == FIBQ_BF16;
+}
+static bool page_known(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
+static bool head_dim_known(int d) { return d == 64 || d == 128 || d == 256; }
+static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Rows of heads at these strides: no negative ones, none so long that an address overflows.
+static bool strides_known(int64_t row, int64_t head) {
+  return row >= 0 && head >= 0 && row < (1LL << 40) && head < (1LL << 40);
+}
+// ... and no element twice (outputs).
+static bool strides_apart(int64_t n, int heads, int d, int64_t row, int64_t head) {
+  return (head >= d && row >= (heads - 1) * head + d) || (row >= d && head >= (n - 1) * row + d);
+}
+
+int fibq_rope(const void* q, const void* k, int dtype, int64_t n_rows, int q_heads, int k_heads,
+              int d, int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride,
+              int64_t k_head_stride, const int32_t* positions, const double* freqs, int rot,
+              int layout, float scale, int inverse, void* q_out, void* k_out,
+              int64_t q_out_row_stride, int64_t q_out_head_stride, int64_t k_out_row_stride,
+              int64_t k_out_head_stride, void* stream) {
+  if (!dtype_known(dtype) || n_rows < 0 || n_rows >= (1LL << 31) || q_heads < 1 || k_heads < 0 ||
+      q_heads > 2048 || k_heads > 2048 || q_heads + k_heads > 2048)
+    return FIBQ_EINVAL;
+  if (d < 2 || d > 512 || d % 2 != 0 || rot < 2 || rot > d || rot % 2 != 0) return FIBQ_EINVAL;
+  if (layout != FIBQ_ROPE_HALF && layout != FIBQ_ROPE_INTERLEAVED) return FIBQ_EINVAL;
+  if (!std::isfinite(scale)) return FIBQ_EINVAL;
+  if (n_rows == 0) return FIBQ_OK;
+  if (!q || !q_out || !positions || !freqs || (k_heads > 0 && (!k || !k_out))) return FIBQ_EINVAL;
+  if (!strides_known(q_row_stride, q_head_stride) ||
+      !strides_known(q_out_row_stride, q_out_head_stride) ||
+      !strides_apart(n_rows, q_heads, d, q_out_row_stride, q_out_head_stride))
+    return FIBQ_EINVAL;
+  if (q_out == q && (q_row_stride != q_out_row_stride || q_head_stride != q_out_head_stride))
+    return FIBQ_EINVAL;
+  if (k_heads > 0) {
+    if (!strides_known(k_row_stride, k_head_stride) ||
+        !strides_known(k_out_row_stride, k_out_head_stride) ||
+        !strides_apart(n_rows, k_heads, d, k_out_row_stride, k_out_head_stride))
+      return FIBQ_EINVAL;
+    if (k_out == k && (k_row_stride != k_out_row_stride || k_head_stride != k_out_head_stride))
+      return FIBQ_EINVAL;
+    if (q_out == k || q_out == k_out || k_out == q) return FIBQ_EINVAL;
+  }
+  return hip_status(fibq::dev::launch_rope(
+      {q, k, dtype, n_rows, q_heads, k_heads, d, q_row_stride, q_head_stride, k_row_stride,
+       k_head_stride, positions, freqs, rot, layout, scale, inverse, q_out, k_out,
+       q_out_row_stride, q_out_head_stride, k_out_row_stride, k_out_head_stride},
+      stream));
+}
+
+size_t fibq_page_resize_workspace_bytes(int64_t n_seqs) {
+  return n_seqs < 0 || n_seqs > 65535 ? 0 : fibq::dev::resize_workspace_bytes(n_seqs);
+}
+
+int fibq_page_resize(int32_t* table, const int32_t* lens, const int32_t* grow, int64_t n_seqs,
+                     int64_t max_pages, int page, int64_t n_pages, int32_t* free_pages,
+                     int64_t free_cap, const int32_t* n_free, int64_t n_rows, int32_t* new_lens,
+                     int32_t* starts, int64_t* slots, int32_t* positions, int32_t* new_free,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (n_seqs < 0 || n_seqs > 65535 || page < 1 || page > 65536 || max_pages < 0 ||
+      max_pages >= (1LL << 30) || max_pages * page >= (1LL << 30) || n_pages < 0 ||
+      n_pages >= (1LL << 31) || free_cap < 0 || free_cap >= (1LL << 31) || n_rows < 0 ||
+      n_rows >= (1LL << 31))
+    return FIBQ_EINVAL;
+  if (!n_free || !starts || !new_free) return FIBQ_EINVAL;
+  if (n_seqs > 0 && (!lens || !grow || !new_lens)) return FIBQ_EINVAL;
+  if (n_seqs > 0 && max_pages > 0 && !table) return FIBQ_EINVAL;
+  if ((free_cap > 0 && !free_pages) || (n_rows > 0 && (!slots || !positions))) return FIBQ_EINVAL;
+  const void* in[] = {table, lens, grow, free_pages, n_free};
+  const void* o[] = {new_lens, starts, slots, positions, new_free};
+  for (const void*& y : o) {
+    if (!y) continue;
+    for (const void* x : in)
+      if (x == y && !(y == new_lens && y == lens) && !(y == new_free && y == n_free))
+        return FIBQ_EINVAL;
+    for (const void** x = o; x != &y; ++x)
+      if (*x == y) return FIBQ_EINVAL;
+  }
+  const int rc = check_workspace(workspace, workspace_bytes,
+                                 fibq::dev::resize_workspace_bytes(n_seqs));
+  if (rc != FIBQ_OK) return rc;
+  return hip_status(fibq::dev::launch_resize(
+      {table, lens, grow, n_seqs, max_pages, page, n_pages, free_pages, free_cap, n_free, n_rows,
+       new_lens, starts, slots, positions, new_free, static_cast<int32_t*>(workspace)},
+      stream));
+}
+
+int fibq_cache8_write(const void* k, const void* v, int dtype, int64_t n_rows,
+                      int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride,
+                      int64_t v_head_stride, const int64_t* slots, int H, int d, int page,
+                      int64_t n_pages, int codes, void* k_pages, float* k_scales, void* v_pages,
+                      float* v_scales, void* stream) {
+  if (!dtype_known(dtype) || n_rows < 0 || H < 1 || H > 1024 || d < 1 || !page_known(page) ||
+      n_pages < 1 || n_pages >= (1LL << 31) || (codes != FIBQ_INT8 && codes != FIBQ_E4M3))
+    return FIBQ_EINVAL;
+  if (!strides_known(k_row_stride, k_head_stride) || !strides_known(v_row_stride, v_head_stride))
+    return FIBQ_EINVAL;
+  if (n_rows >= (1LL << 31)) return FIBQ_EINVAL;
+  if (!head_dim_known(d)) return FIBQ_EUNSUPPORTED;
+  if (n_rows * H * d >= (1LL << 31)) return FIBQ_EINVAL;
+  if (n_rows == 0) return FIBQ_OK;
+  if (!k || !v || !slots || !k_pages || !k_scales || !v_pages || !v_scales) return FIBQ_EINVAL;
+  if (!aligned16(k_pages) || !aligned16(v_pages)) return FIBQ_EINVAL;
+  if (k_pages == v_pages || k_scales == v_scales) return FIBQ_EINVAL;
+  return hip_status(fibq::dev::launch_write({k, v, dtype, n_rows, k_row_stride, k_head_stride,
+                                             v_row_stride, v_head_stride, slots, H, d, page,
+                                             n_pages, codes, k_pages, k_scales, v_pages, v_scales},
+                                            stream));
+}
+
+// FIBQ_OK for sizes that fibq_attn_cache8 takes.
+static int page_attn_sizes(int64_t n_seqs, int64_t n_rows, int H, int G, int64_t max_pages,
+                           int page, int d) {
+  if (n_seqs < 0 || n_seqs > 65535 || n_rows < 0 || n_rows >= (1LL << 31) || H < 1 || H > 1024 ||
+      G < 1 || G > 16 || max_pages < 0 || max_pages >= (1LL << 30) || !page_known(page) ||
+      max_pages * page >= (1LL << 30) || d < 1)
+    return FIBQ_EINVAL;
+  if (!head_dim_known(d)) return FIBQ_EUNSUPPORTED;
+  return n_rows * H * G * d < (1LL << 31) ? FIBQ_OK : FIBQ_EINVAL;
+}
+
+size_t fibq_attn_cache8_workspace_bytes(int64_t n_seqs, int64_t n_rows, int H, int G,
+                                        int64_t max_pages, int page, int d) {
+  if (page_attn_sizes(n_seqs, n_rows, H, G, max_pages, page, d) != FIBQ_OK) return 0;
+  return fibq::dev::page_attn_workspace_bytes(n_seqs, n_rows, H, G, max_pages, page, d);
+}
+
+int fibq_attn_cache8(const void* q, int q_dtype, const void* k_pages, const float* k_scales,
+                     const void* v_pages, const float* v_scales, int codes, const int32_t* table,
+                     const int32_t* lens, const int32_t* starts, int64_t n_seqs, int64_t n_rows,
+                     int H, int G, int64_t max_pages, int page, int64_t n_pages, int d,
+                     int causal, float scale, float* out, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  int rc = page_attn_sizes(n_seqs, n_rows, H, G, max_pages, page, d);
+  if (rc == FIBQ_EINVAL) return rc;
+  if (!dtype_known(q_dtype) || (codes != FIBQ_INT8 && codes != FIBQ_E4M3) ||
+      !std::isfinite(scale) || n_pages < 1 || n_pages >= (1LL << 31) ||
+      (!starts && n_rows != n_seqs))
+    return FIBQ_EINVAL;
+  if (rc != FIBQ_OK) return rc;
+  if (n_seqs == 0 || n_rows == 0) return FIBQ_OK;
+  if (!q || !lens || !out || (max_pages > 0 && !table)) return FIBQ_EINVAL;
+  if (!k_pages || !k_scales || !v_pages || !v_scales) return FIBQ_EINVAL;
+  if (!aligned16(k_pages) || !aligned16(v_pages)) return FIBQ_EINVAL;
+  rc = check_workspace(workspace, workspace_bytes,
+                       fibq::dev::page_attn_workspace_bytes(n_seqs, n_rows, H, G, max_pages, page,
+                                                            d));
+  if (rc != FIBQ_OK) return rc;
+  if (scale <= 0.0f) scale = 1.0f / std::sqrt((float)d);
+  return hip_status(fibq::dev::launch_page_attn(
+      {q, q_dtype, k_pages, k_scales, v_pages, v_scales, codes, table, lens, starts, n_seqs,
+       n_rows, H, G, max_pages, page, n_pages, d, causal, scale, out, workspace},
+      stream));
+}
+
 }  // extern "C"

@@ -1,5 +1,5 @@
-// The per-call part of the Python binding for encode, decode, attention and the
-// serving operators:
+// The per-call part of the Python binding for encode, decode, attention, the
+// serving operators and the paged 8-bit cache:
 // argument checks, output allocation and the library call, without the Python
 // interpreter between them (14 us of checks around a 7 us kernel before, about
 // 2 us here).  Every function returns None, having done nothing, for any
@@ -512,6 +512,315 @@ PyObject* bind_serving(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   Py_RETURN_NONE;
 }
 
+// ------------------------------------------------------- paged 8-bit cache --
+decltype(&fibq_rope) g_rope;
+decltype(&fibq_page_resize) g_resize;
+decltype(&fibq_page_resize_workspace_bytes) g_resize_ws;
+decltype(&fibq_cache8_write) g_write8;
+decltype(&fibq_attn_cache8) g_attn8;
+decltype(&fibq_attn_cache8_workspace_bytes) g_attn8_ws;
+
+// Rows of heads [n, H, d] of type ty on dev, dense heads at any strides
+struct HeadRows {
+  const char *begin, *end;
+  int64_t n, H, d, row, head, size;
+};
+bool head_rows(const Tensor* t, at::ScalarType ty, at::Device dev, HeadRows* r) {
+  if (!t || t->scalar_type() != ty || t->dim() != 3 || t->device() != dev) return false;
+  r->n = t->size(0), r->H = t->size(1), r->d = t->size(2), r->size = t->element_size();
+  if (t->stride(2) != 1 && r->d > 1) return false;
+  r->head = r->H > 1 ? t->stride(1) : r->d;
+  r->row = r->n > 1 ? t->stride(0) : (r->H - 1) * r->head + r->d;
+  r->begin = r->end = static_cast<const char*>(ptr(*t));
+  if (t->numel() > 0) r->end += ((r->n - 1) * r->row + (r->H - 1) * r->head + r->d) * r->size;
+  return true;
+}
+// no memory in common: extents that do not meet, or columns of one matrix that do not
+bool apart(const HeadRows& a, const HeadRows& b) {
+  if (a.end <= b.begin || b.end <= a.begin) return true;
+  const int64_t row = a.row * a.size;
+  if (row != b.row * b.size || row == 0 || a.n < 2) return false;
+  const int64_t wide_a = ((a.H - 1) * a.head + a.d) * a.size,
+                wide_b = ((b.H - 1) * b.head + b.d) * b.size;
+  const int64_t at = ((b.begin - a.begin) % row + row) % row;
+  return wide_a <= at && at + wide_b <= row;
+}
+bool once(const HeadRows& a) {  // (no element twice)
+  return (a.head >= a.d && a.row >= (a.H - 1) * a.head + a.d) ||
+         (a.row >= a.d && a.head >= (a.n - 1) * a.row + a.d);
+}
+bool meets(const HeadRows& a, const Tensor* t) {
+  const char* p = static_cast<const char*>(ptr(*t));
+  return a.begin < p + t->nbytes() && p < a.end;
+}
+
+// rope(q, k, positions, freqs, layout, scale, inverse, out, stream, device) -> (q, k);
+// out: None or (q, k) themselves
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!g_rope || n_args != 10) FIBQ_NONE;
+  const Tensor *q = tensor(a[0]), *k = a[1] == Py_None ? nullptr : tensor(a[1]), *at_ = tensor(a[2]),
+               *freqs = tensor(a[3]);
+  int64_t st, index;
+  const bool has_k = a[1] != Py_None;
+  if (!q || (has_k && !k) || !at_ || !freqs || !PyFloat_CheckExact(a[5]) || !PyBool_Check(a[6]) ||
+      !PyBool_Check(a[4]) || !int_arg(a[8], &st) || !int_arg(a[9], &index) ||
+      q->device().index() != index || freqs->dim() != 1)
+    FIBQ_NONE;
+  const at::Device dev = q->device();
+  const int dt = dtype_code(*q);
+  HeadRows rq, rk{};
+  if (dt < 0 || !head_rows(q, q->scalar_type(), dev, &rq) ||
+      (has_k && (!head_rows(k, q->scalar_type(), dev, &rk) || rk.n != rq.n || rk.d != rq.d)) ||
+      !shaped(at_, at::kInt, {rq.n}) || !shaped(freqs, at::kDouble, {freqs->size(0)}) ||
+      at_->device() != dev || freqs->device() != dev || rq.H > 2048 || rk.H > 2048)
+    FIBQ_NONE;
+  const int64_t rot = 2 * freqs->size(0);
+  if (rq.d > 512 || rot < 2 || rot > rq.d) FIBQ_NONE;
+  const bool in_place = a[7] != Py_None;
+  if (in_place) {
+    if (!PyTuple_CheckExact(a[7]) || PyTuple_GET_SIZE(a[7]) != 2 || PyTuple_GET_ITEM(a[7], 0) != a[0] ||
+        PyTuple_GET_ITEM(a[7], 1) != a[1])
+      FIBQ_NONE;
+    if (!once(rq) || meets(rq, at_) || meets(rq, freqs)) FIBQ_NONE;
+    if (has_k && (!once(rk) || !apart(rq, rk) || meets(rk, at_) || meets(rk, freqs))) FIBQ_NONE;
+  }
+  const void *pq = ptr(*q), *pk = has_k ? ptr(*k) : nullptr;
+  const int32_t* pp = static_cast<const int32_t*>(ptr(*at_));
+  const double* pf = static_cast<const double*>(ptr(*freqs));
+  const at::ScalarType ty = q->scalar_type();
+  const float scale = (float)PyFloat_AS_DOUBLE(a[5]);
+  const bool interleaved = a[4] == Py_True, inverse = a[6] == Py_True;
+  Tensor qo, ko;
+  int64_t qs[2] = {rq.row, rq.head}, ks[2] = {rk.row, rk.head};
+  int rc;
+  {
+    NoGil no_gil;
+    void *to_q = const_cast<void*>(pq), *to_k = const_cast<void*>(pk);
+    if (!in_place) {
+      qo = empty(dev, ty, {rq.n, rq.H, rq.d});
+      to_q = qo.data_ptr(), qs[0] = rq.H * rq.d, qs[1] = rq.d;
+      if (has_k) {
+        ko = empty(dev, ty, {rk.n, rk.H, rk.d});
+        to_k = ko.data_ptr(), ks[0] = rk.H * rk.d, ks[1] = rk.d;
+      }
+    }
+    rc = g_rope(pq, pk, dt, rq.n, (int)rq.H, (int)rk.H, (int)rq.d, rq.row, rq.head, rk.row, rk.head,
+                pp, pf, (int)rot, interleaved ? FIBQ_ROPE_INTERLEAVED : FIBQ_ROPE_HALF, scale, inverse,
+                to_q, to_k, qs[0], qs[1], ks[0], ks[1], reinterpret_cast<void*>(st));
+  }
+  if (rc != FIBQ_OK) return raise_status(rc, "fibq_rope");
+  if (in_place) return Py_NewRef_(a[7]);
+  PyObject* r = PyTuple_New(2);
+  if (!r) return nullptr;
+  PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(qo));
+  PyTuple_SET_ITEM(r, 1, has_k ? THPVariable_Wrap(ko) : Py_NewRef_(Py_None));
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
+// page_resize(table, lens, grow, page, n_pages, free, n_free, n_rows, out, workspace,
+//             stream, device) -> out; out: a tuple of five tensors or None
+PyObject* page_resize(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!g_resize || n_args != 12) FIBQ_NONE;
+  const Tensor *table = tensor(a[0]), *stack = tensor(a[5]);
+  int64_t page, n_pages, n_rows, st, index;
+  if (!table || table->dim() != 2 || !stack || stack->dim() != 1 || !int_arg(a[3], &page) ||
+      !int_arg(a[4], &n_pages) || !int_arg(a[7], &n_rows) || !int_arg(a[10], &st) ||
+      !int_arg(a[11], &index) || table->device().index() != index || page < 1 || page > 65536 ||
+      n_rows < 0 || n_rows >= (1LL << 31))
+    FIBQ_NONE;
+  const at::Device dev = table->device();
+  const int64_t n = table->size(0), max_pages = table->size(1), cap = stack->size(0);
+  const Tensor* in[] = {given(a[0], at::kInt, {n, max_pages}, dev), given(a[5], at::kInt, {cap}, dev),
+                        given(a[1], at::kInt, {n}, dev), given(a[2], at::kInt, {n}, dev),
+                        given(a[6], at::kInt, {1}, dev)};
+  for (const Tensor* x : in)
+    if (!x) FIBQ_NONE;
+  for (int w = 0; w < 2; ++w)  // the table and the stack are written
+    for (int i = w + 1; i < 5; ++i)
+      if (shared(in[w], in[i])) FIBQ_NONE;
+  const int64_t sizes[5] = {n, n + 1, n_rows, n_rows, 1};
+  Tensor out[5], ws;
+  const int64_t need = (int64_t)g_resize_ws(n);
+  if (!workspace(a[9], need, dev, &ws)) FIBQ_NONE;
+  if (ws.defined())
+    for (const Tensor* x : in)
+      if (shared(x, &ws)) FIBQ_NONE;
+  if (a[8] != Py_None) {
+    if (!PyTuple_CheckExact(a[8]) || PyTuple_GET_SIZE(a[8]) != 5) FIBQ_NONE;
+    for (int i = 0; i < 5; ++i) {
+      const Tensor* t = given(PyTuple_GET_ITEM(a[8], i), i == 2 ? at::kLong : at::kInt, {sizes[i]}, dev);
+      if (!t) FIBQ_NONE;
+      const Tensor* same = i == 0 ? in[2] : i == 4 ? in[4] : nullptr;  // (may be this input)
+      for (const Tensor* x : in)
+        if (shared(x, t) && !(x == same && ptr(*x) == ptr(*t))) FIBQ_NONE;
+      for (int j = 0; j < i; ++j)
+        if (shared(&out[j], t)) FIBQ_NONE;
+      if (ws.defined() && shared(&ws, t)) FIBQ_NONE;
+      out[i] = *t;
+    }
+  }
+  const int32_t *pl = static_cast<const int32_t*>(ptr(*in[2])), *pg = static_cast<const int32_t*>(ptr(*in[3])),
+                *pn = static_cast<const int32_t*>(ptr(*in[4]));
+  int32_t *pt = static_cast<int32_t*>(table->data_ptr()), *pf = static_cast<int32_t*>(stack->data_ptr());
+  int rc;
+  {
+    NoGil no_gil;
+    if (!ws.defined()) ws = empty(dev, at::kByte, {need > 1 ? need : 1});
+    for (int i = 0; i < 5; ++i)
+      if (!out[i].defined()) out[i] = empty(dev, i == 2 ? at::kLong : at::kInt, {sizes[i]});
+    rc = g_resize(pt, pl, pg, n, max_pages, (int)page, n_pages, pf, cap, pn, n_rows,
+                  static_cast<int32_t*>(out[0].data_ptr()), static_cast<int32_t*>(out[1].data_ptr()),
+                  static_cast<int64_t*>(out[2].data_ptr()), static_cast<int32_t*>(out[3].data_ptr()),
+                  static_cast<int32_t*>(out[4].data_ptr()), ws.data_ptr(), (size_t)ws.numel(),
+                  reinterpret_cast<void*>(st));
+  }
+  if (rc != FIBQ_OK) return raise_status(rc, "fibq_page_resize");
+  if (a[8] != Py_None) return Py_NewRef_(a[8]);
+  PyObject* r = PyTuple_New(5);
+  if (!r) return nullptr;
+  for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
+// k_pages, k_scales, v_pages, v_scales at a[0] .. a[3], on the device `index`
+struct Pools {
+  const Tensor* t[4];
+  int64_t n_pages, H, page, d;
+  int codes;
+  at::Device dev = at::kCPU;
+};
+bool pools(PyObject* const* a, int64_t index, Pools* p) {
+  for (int i = 0; i < 4; ++i) p->t[i] = tensor(a[i]);
+  const Tensor* k = p->t[0];
+  if (!k || k->dim() != 4 || k->device().index() != index) return false;
+  p->n_pages = k->size(0), p->H = k->size(1), p->page = k->size(2), p->d = k->size(3);
+  p->dev = k->device();
+  const at::ScalarType ty = k->scalar_type();
+  if (ty != at::kChar && ty != at::kFloat8_e4m3fn) return false;
+  p->codes = ty == at::kChar ? FIBQ_INT8 : FIBQ_E4M3;
+  for (int i = 0; i < 4; ++i)
+    if (!p->t[i] || p->t[i]->device() != p->dev ||
+        !(i % 2 ? shaped(p->t[i], at::kFloat, {p->n_pages, p->H})
+                : shaped(p->t[i], ty, {p->n_pages, p->H, p->page, p->d})))
+      return false;
+  return p->H > 0 && p->H <= 1024 && p->page <= 128 && p->d <= 256;
+}
+
+// cache8_write(k, v, slots, k_pages, k_scales, v_pages, v_scales, stream, device) -> True
+PyObject* cache8_write(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!g_write8 || n_args != 9) FIBQ_NONE;
+  const Tensor *k = tensor(a[0]), *v = tensor(a[1]), *slots = tensor(a[2]);
+  int64_t st, index;
+  Pools p;
+  HeadRows rk, rv;
+  if (!k || !v || !slots || !int_arg(a[7], &st) || !int_arg(a[8], &index) || !pools(a + 3, index, &p))
+    FIBQ_NONE;
+  const int dt = dtype_code(*k);
+  if (dt < 0 || !head_rows(k, k->scalar_type(), p.dev, &rk) || !head_rows(v, k->scalar_type(), p.dev, &rv) ||
+      rv.n != rk.n || rk.H != p.H || rv.H != p.H || rk.d != p.d || rv.d != p.d ||
+      !shaped(slots, at::kLong, {rk.n}) || slots->device() != p.dev)
+    FIBQ_NONE;
+  for (int i = 0; i < 4; ++i) {
+    if (meets(rk, p.t[i]) || meets(rv, p.t[i]) || shared(slots, p.t[i])) FIBQ_NONE;
+    for (int j = 0; j < i; ++j)
+      if (shared(p.t[i], p.t[j])) FIBQ_NONE;
+  }
+  void* to[4];
+  for (int i = 0; i < 4; ++i) to[i] = p.t[i]->data_ptr();
+  const int64_t* ps = static_cast<const int64_t*>(ptr(*slots));
+  int rc;
+  {
+    NoGil no_gil;
+    rc = g_write8(rk.begin, rv.begin, dt, rk.n, rk.row, rk.head, rv.row, rv.head, ps, (int)p.H, (int)p.d,
+                  (int)p.page, p.n_pages, p.codes, to[0], static_cast<float*>(to[1]), to[2],
+                  static_cast<float*>(to[3]), reinterpret_cast<void*>(st));
+  }
+  if (rc != FIBQ_OK) return raise_status(rc, "fibq_cache8_write");
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// attn_cache8(q, k_pages, k_scales, v_pages, v_scales, table, lens, starts, causal, scale,
+//             workspace, out, stream, device) -> out
+PyObject* attn_cache8(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!g_attn8 || n_args != 14) FIBQ_NONE;
+  const Tensor *q = tensor(a[0]), *table = tensor(a[5]);
+  int64_t st, index;
+  Pools p;
+  if (!q || q->dim() != 3 || !q->is_contiguous() || !table || table->dim() != 2 || !PyBool_Check(a[8]) ||
+      !PyFloat_CheckExact(a[9]) || !int_arg(a[12], &st) || !int_arg(a[13], &index) ||
+      !pools(a + 1, index, &p))
+    FIBQ_NONE;
+  const int64_t n_rows = q->size(0), Hq = q->size(1), n = table->size(0), max_pages = table->size(1);
+  const int dt = dtype_code(*q);
+  if (dt < 0 || q->device() != p.dev || q->size(2) != p.d || Hq < 1 || Hq % p.H != 0 || Hq / p.H > 16 ||
+      max_pages >= (1LL << 30))
+    FIBQ_NONE;
+  const bool has_starts = a[7] != Py_None;
+  const Tensor *cells = given(a[5], at::kInt, {n, max_pages}, p.dev), *lens = given(a[6], at::kInt, {n}, p.dev),
+               *starts = has_starts ? given(a[7], at::kInt, {n + 1}, p.dev) : nullptr;
+  if (!cells || !lens || (has_starts ? !starts : n_rows != n)) FIBQ_NONE;
+  const int G = (int)(Hq / p.H);
+  const int64_t need =
+      (int64_t)g_attn8_ws(n, n_rows, (int)p.H, G, max_pages, (int)p.page, (int)p.d);
+  Tensor ws, out;
+  if (!workspace(a[10], need, p.dev, &ws)) FIBQ_NONE;
+  if (a[11] != Py_None) {
+    const Tensor* t = given(a[11], at::kFloat, {n_rows, Hq, p.d}, p.dev);
+    if (!t) FIBQ_NONE;
+    out = *t;
+  }
+  const Tensor* in[] = {q, p.t[0], p.t[1], p.t[2], p.t[3], cells, lens, starts};
+  for (const Tensor* x : in)
+    if (x && ((out.defined() && shared(x, &out)) || (ws.defined() && shared(x, &ws)))) FIBQ_NONE;
+  if (out.defined() && ws.defined() && shared(&out, &ws)) FIBQ_NONE;
+  const void *pq = ptr(*q), *kp = ptr(*p.t[0]), *vp = ptr(*p.t[2]);
+  const float *ks = static_cast<const float*>(ptr(*p.t[1])), *vs = static_cast<const float*>(ptr(*p.t[3]));
+  const int32_t *pt = static_cast<const int32_t*>(ptr(*cells)), *pl = static_cast<const int32_t*>(ptr(*lens)),
+                *ps = starts ? static_cast<const int32_t*>(ptr(*starts)) : nullptr;
+  const float scale = (float)PyFloat_AS_DOUBLE(a[9]);
+  const bool causal = a[8] == Py_True;
+  int rc;
+  {
+    NoGil no_gil;
+    if (!ws.defined()) ws = empty(p.dev, at::kByte, {need > 1 ? need : 1});
+    if (!out.defined()) out = empty(p.dev, at::kFloat, {n_rows, Hq, p.d});
+    rc = g_attn8(pq, dt, kp, ks, vp, vs, p.codes, pt, pl, ps, n, n_rows, (int)p.H, G, max_pages, (int)p.page,
+                 p.n_pages, (int)p.d, causal, scale, static_cast<float*>(out.data_ptr()), ws.data_ptr(),
+                 (size_t)ws.numel(), reinterpret_cast<void*>(st));
+  }
+  if (rc != FIBQ_OK) return raise_status(rc, "fibq_attn_cache8");
+  return keep(a[11], out);
+  END_HANDLE_TH_ERRORS
+}
+
+// bind_paged(rope, page_resize, its workspace_bytes, cache8_write, attn_cache8, its
+// workspace_bytes): addresses
+PyObject* bind_paged(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 6) {
+    PyErr_SetString(PyExc_TypeError, "bind_paged takes six addresses");
+    return nullptr;
+  }
+  void* p[6];
+  for (int i = 0; i < 6; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  g_rope = reinterpret_cast<decltype(g_rope)>(p[0]);
+  g_resize = reinterpret_cast<decltype(g_resize)>(p[1]);
+  g_resize_ws = reinterpret_cast<decltype(g_resize_ws)>(p[2]);
+  g_write8 = reinterpret_cast<decltype(g_write8)>(p[3]);
+  g_attn8 = reinterpret_cast<decltype(g_attn8)>(p[4]);
+  g_attn8_ws = reinterpret_cast<decltype(g_attn8_ws)>(p[5]);
+  Py_RETURN_NONE;
+}
+
 // bind(encode, decode, attn_decode, attn_workspace_bytes, payload_bytes,
 // check): addresses of the loaded library's entry points, and _check
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
@@ -544,6 +853,11 @@ PyMethodDef methods[] = {
     {"attn_accum", (PyCFunction)(void*)attn_accum, METH_FASTCALL, nullptr},
     {"accept", (PyCFunction)(void*)accept, METH_FASTCALL, nullptr},
     {"evict", (PyCFunction)(void*)evict, METH_FASTCALL, nullptr},
+    {"bind_paged", (PyCFunction)(void*)bind_paged, METH_FASTCALL, nullptr},
+    {"rope", (PyCFunction)(void*)rope, METH_FASTCALL, nullptr},
+    {"page_resize", (PyCFunction)(void*)page_resize, METH_FASTCALL, nullptr},
+    {"cache8_write", (PyCFunction)(void*)cache8_write, METH_FASTCALL, nullptr},
+    {"attn_cache8", (PyCFunction)(void*)attn_cache8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr,
                       nullptr, nullptr};

@@ -119,6 +119,78 @@ int launch_evict(const uint8_t* kp, const uint16_t* kn, const uint8_t* vp, const
                  int keep, int recent, int64_t T_out, uint8_t* kpo, uint16_t* kno, uint8_t* vpo,
                  uint16_t* vno, float* acco, int32_t* new_lens, int32_t* index, void* ws,
                  void* stream);
+// One call of each operator of the paged 8-bit cache.  Strides in elements.
+struct Rope {
+  const void *q, *k;  // k may be null (k_heads = 0)
+  int dtype;
+  int64_t n_rows;
+  int q_heads, k_heads, d;
+  int64_t q_row, q_head, k_row, k_head;
+  const int32_t* positions;
+  const double* freqs;
+  int rot, layout;
+  float scale;
+  int inverse;
+  void *q_out, *k_out;
+  int64_t qo_row, qo_head, ko_row, ko_head;
+};
+int launch_rope(const Rope& a, void* stream);
+
+struct Resize {
+  int32_t* table;
+  const int32_t *lens, *grow;
+  int64_t n, max_pages;
+  int page;
+  int64_t n_pages;
+  int32_t* free_pages;
+  int64_t free_cap;
+  const int32_t* n_free;
+  int64_t n_rows;
+  int32_t *new_lens, *starts;
+  int64_t* slots;
+  int32_t *positions, *new_free;
+  int32_t* top;  // workspace: where each request's new pages begin on the stack
+};
+size_t resize_workspace_bytes(int64_t n);
+int launch_resize(const Resize& a, void* stream);
+
+struct Write {
+  const void *k, *v;
+  int dtype;
+  int64_t n_rows, k_row, k_head, v_row, v_head;
+  const int64_t* slots;
+  int H, d, page;
+  int64_t n_pages;
+  int codes;
+  void* k_pages;
+  float* k_scales;
+  void* v_pages;
+  float* v_scales;
+};
+int launch_write(const Write& a, void* stream);
+
+struct PageAttn {
+  const void* q;
+  int q_dtype;
+  const void* k_pages;
+  const float* k_scales;
+  const void* v_pages;
+  const float* v_scales;
+  int codes;
+  const int32_t *table, *lens, *starts;  // starts null: one row per sequence
+  int64_t n_seqs, n_rows;
+  int H, G;
+  int64_t max_pages;
+  int page;
+  int64_t n_pages;
+  int d, causal;
+  float scale;
+  float* out;
+  void* ws;
+};
+size_t page_attn_workspace_bytes(int64_t n_seqs, int64_t n_rows, int H, int G, int64_t max_pages,
+                                 int page, int d);
+int launch_page_attn(const PageAttn& a, void* stream);
 }  // namespace dev
 
 }  // namespace fibq
