@@ -1,11 +1,10 @@
 // Attention over the paged 8-bit cache (fibq_attn_cache8).
 //
 // A work item is one head of one sequence and a tile of up to 16 R query rows (whole
-// tokens of it, G rows each).  Workgroups take equal shares of all items' tokens, so
-// one may hold several short items or a part of a long one; parts leave a record each
-// (reference, sum, exponent, accumulators), and a second launch joins the records of
-// every item that was cut.  In a workgroup each of the four wavefronts takes a quarter
-// of the tokens, 32 at a time:
+// tokens of it, G rows each).  Long items are cut into equal parts of at most P tokens;
+// P follows from the lengths on the device, so that the parts fill the card once and are
+// alike however unequal the sequences are.  A workgroup takes one part; its wavefronts
+// take a share of the part's tokens each, 32 at a time:
 //
 //   S^T[t][r] = K[t][:] . Q[r][:]     v_mfma_f32_16x16x32_f16, A = codes as binary16
 //                                     (exact), B = queries, scaled by a power of two per
@@ -17,9 +16,10 @@
 // Four tokens of S^T that a lane holds are consecutive, so its weights are the A operand
 // of the second product as they are: the tokens of a lane group are 4 of each half tile,
 // and V is read in that order.  Nothing goes through LDS until the wavefronts' states are
-// joined.  `ref` (the largest score so far, in a row) and `e` (the largest weight's
-// exponent) move only when a score exceeds ref by more than kLag or a weight leaves its
-// range, so the common path has no exchange between lanes.
+// joined.  `ref` (a score near the row's largest so far) and `e` (the exponent of its
+// largest weight) move only when a weight leaves its range, so the common path has no
+// exchange between lanes.  Parts of an item that was cut leave a state each, which a
+// second launch joins.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -36,165 +36,123 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
-constexpr float kLag = 8.0f;       // log2 by which a score may exceed its row's reference
-constexpr float kTop = 0x1p15f;    // weights stay below (binary16)
-constexpr int kTopBits = 7;        // exponent of a row's largest weight when e is set
-constexpr float kLimit = 0x1p126f; // of scores
-constexpr int64_t kItem = 64;      // an item costs about as much as this many tokens
-constexpr int64_t kChunk = 512;    // tokens of a workgroup, at least
+constexpr float kLag = 0x1p8f;      // exp2 of what a score may exceed its row's reference by
+constexpr float kTop = 0x1p15f;     // weights stay below (binary16)
+constexpr int kTopBits = 7;         // exponent of a row's largest weight when e is set
+constexpr float kLimit = 0x1p126f;  // of scores
+constexpr float kNone = -0x1p127f;  // reference of a row that has seen nothing
 
 struct Args {
   PageAttn a;
   int tile_tokens;  // query tokens of an item
   int shift;        // log2 of the page
-  int n_wg;         // workgroups, at most
-  int cut;          // items may be cut
+  int least_part;   // tokens of a part, at least
+  float target;     // parts that fill the card
   float scale2;     // scale log2(e)
 };
 
 // ------------------------------------------------------------------- work --
 struct Seq {
-  int64_t begin, rows, len;  // len 0 if bad
+  int begin, rows, len;  // len 0 if bad
   bool bad, causal;
-  int64_t tiles, head;  // items and weight of one head
+  int tiles;
 };
-__device__ __forceinline__ Seq sequence(const Args& p, int64_t g) {
+__device__ __forceinline__ Seq sequence(const Args& p, int g) {
   Seq s{};
   const PageAttn& a = p.a;
-  const int64_t b = a.starts ? a.starts[g] : g, e = a.starts ? a.starts[g + 1] : g + 1;
+  const int b = a.starts ? a.starts[g] : g, e = a.starts ? a.starts[g + 1] : g + 1;
+  const int len = a.lens[g];
   if (b < 0 || e < b || e > a.n_rows) return s;
-  const int64_t len = a.lens[g];
   s.begin = b;
   s.rows = e - b;
-  s.bad = len < 0 || len > a.max_pages << p.shift || (a.causal && s.rows > len);
+  s.bad = len < 0 || len > (int)(a.max_pages << p.shift) || (a.causal && s.rows > len);
   s.causal = a.causal && !s.bad;
   s.len = s.bad ? 0 : len;
-  s.tiles = (int64_t)((uint32_t)(s.rows + p.tile_tokens - 1) / (uint32_t)p.tile_tokens);
-  s.head = s.causal ? s.tiles * (s.len - s.rows + kItem) +
-                          p.tile_tokens * (s.tiles * (s.tiles - 1) / 2) + s.rows
-                    : s.tiles * (s.len + kItem);
-  if (s.rows == 0) s.head = 0;
-  return s;
-}
-// weight of the tiles before tile t of a head
-__device__ __forceinline__ int64_t before_tile(const Args& p, const Seq& s, int64_t t) {
-  return s.causal ? t * (s.len - s.rows + kItem) + p.tile_tokens * (t * (t + 1) / 2)
-                  : t * (s.len + kItem);
-}
-__device__ __forceinline__ int64_t tile_tokens_seen(const Args& p, const Seq& s, int64_t t) {
-  return s.causal ? s.len - s.rows + min(s.rows, (t + 1) * p.tile_tokens) : s.len;
-}
-
-// The share of workgroup w: [lo, hi) of the weights of all items, and the sequence
-// that holds lo with the weight before it.  Called by all threads of kThreads.
-struct Share {
-  int64_t lo, hi, seq, before, each, more;
-  int n_wg;
-  __device__ __forceinline__ int64_t begin(int64_t w) const { return each * w + min(w, more); }
-};
-__device__ __forceinline__ Share share(const Args& p, int w, int64_t* lds) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t n = p.a.n_seqs;
-  int64_t total = 0, mine = 0, upto = 0;
-  for (int64_t g0 = 0; g0 < n; g0 += kThreads) {
-    const int64_t g = g0 + tid;
-    mine = g < n ? sequence(p, g).head * p.a.H : 0;
-    upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t y = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += y;
-    }
-    if (lane == 63) lds[wave] = upto;
-    __syncthreads();
-    for (int v = 0; v < kWaves; ++v) {
-      if (v < wave) upto += lds[v];
-      total += lds[v];
-    }
-    __syncthreads();
-  }
-  Share s;
-  s.n_wg = (int)max((int64_t)1, min((int64_t)p.n_wg, total / kChunk));
-  s.each = total / s.n_wg;
-  s.more = total - s.each * s.n_wg;
-  s.lo = w < s.n_wg ? s.begin(w) : total;
-  s.hi = w < s.n_wg ? s.begin(w + 1) : total;
-  if (tid == 0) lds[0] = n, lds[1] = 0;
-  __syncthreads();
-  if (s.lo >= s.hi) {
-    s.seq = n;
-    s.before = 0;
-    return s;
-  }
-  int64_t carry = 0;
-  for (int64_t g0 = 0; g0 < n; g0 += kThreads) {  // (one round: as summed above)
-    if (n > kThreads) {
-      const int64_t g = g0 + tid;
-      mine = g < n ? sequence(p, g).head * p.a.H : 0;
-      upto = mine;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(upto, o, 64);
-        if (lane >= o) upto += y;
-      }
-      if (lane == 63) lds[2 + wave] = upto;
-      __syncthreads();
-      int64_t sum = 0;
-      for (int v = 0; v < kWaves; ++v) {
-        if (v < wave) upto += lds[2 + v];
-        sum += lds[2 + v];
-      }
-      upto += carry;
-      carry += sum;
-    }
-    if (upto - mine <= s.lo && s.lo < upto) {
-      lds[0] = g0 + tid;
-      lds[1] = upto - mine;
-    }
-    __syncthreads();
-    if (lds[0] < n) break;
-  }
-  s.seq = lds[0];
-  s.before = lds[1];
-  __syncthreads();
+  s.tiles = a.starts ? (int)((uint32_t)(s.rows + p.tile_tokens - 1) / (uint32_t)p.tile_tokens) : 1;
   return s;
 }
 
-// One item's part: tokens [from, to) of what its rows see.
+// One part of an item: tokens [from, to) of the `seen` that its rows see.
 struct Part {
   Seq s;
-  int64_t g, tile, seen, from, to;
-  int h;
-  bool begins, ends;
+  int g, h, tile, part, parts;
+  int i0, n_tokens;  // its query tokens
+  int seen, from, to;
+  int stride;  // from one part of an item to the next
 };
-// The item at weight x of a share, up to weight hi.  Returns the weight behind it.
-__device__ __forceinline__ int64_t part_at(const Args& p, const Seq& s, int64_t g, int64_t before,
-                                           int64_t x, int64_t hi, Part* r) {
-  const int64_t local = x - before;
+// Part w of all, in every thread of the workgroup.  Parts are in the order of sequences,
+// tiles from the last (a causal sequence's longest), parts, heads.  False: there is none.
+template <int W>
+__device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, float* lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = (int)p.a.n_seqs;
+  Seq s{};
+  float tokens = 0.0f;
+  for (int g = tid; g < n; g += 64 * W) {
+    s = sequence(p, g);
+    tokens += (float)s.tiles * (float)s.len;
+  }
+  tokens = wave_sum(tokens);
+  if (lane == 0) lds[wave] = tokens;
+  __syncthreads();
+  tokens = 0.0f;
+#pragma unroll
+  for (int v = 0; v < W; ++v) tokens += lds[v];
+  // (a little more than the exact quotient, so that rounding never makes a part too many)
+  const float share = tokens * (float)p.a.H * 1.001f / p.target;
+  const int part = (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
+  int* at = (int*)lds + W;  // {sequence, parts before it}, sums of the wavefronts
+  __syncthreads();
+  if (tid == 0) at[0] = -1;
+  int before = 0;
+  for (int g0 = 0; g0 < n; g0 += 64 * W) {
+    const int g = g0 + tid;
+    if (n > 64 * W) s = g < n ? sequence(p, g) : Seq{};
+    const int parts = max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part));
+    const int mine = g < n ? s.tiles * parts * p.a.H : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 63) at[2 + wave] = upto;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+      if (v < wave) upto += at[2 + v];
+      all += at[2 + v];
+    }
+    if (w < before + upto && w >= before + upto - mine) {
+      at[0] = g;
+      at[1] = before + upto - mine;
+    }
+    __syncthreads();
+    before += all;
+    if (w < before) break;
+  }
+  const int g = at[0];
+  if (g < 0) return false;
+  s = sequence(p, g);
+  uint32_t i = (uint32_t)(w - at[1]);
+  const uint32_t H = (uint32_t)p.a.H;
   r->s = s;
   r->g = g;
-  r->h = (int)(local / s.head);
-  const int64_t in_head = local - r->h * s.head;
-  int64_t lo = 0, up = s.tiles - 1;  // the last tile that begins at or before in_head
-  while (lo < up) {
-    const int64_t mid = (lo + up + 1) / 2;
-    if (before_tile(p, s, mid) <= in_head)
-      lo = mid;
-    else
-      up = mid - 1;
-  }
-  r->tile = lo;
-  r->seen = tile_tokens_seen(p, s, lo);
-  const int64_t off = in_head - before_tile(p, s, lo), all = r->seen + kItem;
-  const int64_t end = min(all, off + (hi - x));
-  r->begins = off == 0;
-  r->ends = end == all;
-  auto token = [](int64_t o) { return o <= kItem ? (int64_t)0 : (o - kItem) & ~(int64_t)31; };
-  r->from = token(off);
-  r->to = r->ends ? r->seen : token(end);
-  return x + (end - off);
+  r->stride = p.a.H;
+  r->parts = max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part));
+  if (i >= (uint32_t)s.tiles * (uint32_t)r->parts * H) return false;  // (counts that overflowed)
+  r->h = (int)(i % H);
+  i /= H;
+  r->part = (int)(i % (uint32_t)r->parts);
+  r->tile = s.tiles - 1 - (int)(i / (uint32_t)r->parts);
+  r->i0 = r->tile * p.tile_tokens;
+  r->n_tokens = min(p.tile_tokens, s.rows - r->i0);
+  r->seen = s.causal ? s.len - s.rows + r->i0 + r->n_tokens : s.len;
+  const int size = ((int)((uint32_t)(r->seen + r->parts - 1) / (uint32_t)r->parts) + 31) & ~31;
+  r->from = min(r->part * size, r->seen);
+  r->to = min(r->from + size, r->seen);
+  return true;
 }
 
 // ---------------------------------------------------------------- records --
@@ -237,14 +195,6 @@ __device__ __forceinline__ float limited(float x) {
 }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* x) {
-  T y[8];
-  __builtin_memcpy(y, p, sizeof(y));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = to_float(y[e]);
-}
-
 // ------------------------------------------------------------- main kernel --
 template <typename T, int CODES, int D, int R>
 struct Wave {
@@ -253,8 +203,8 @@ struct Wave {
   static constexpr int CB = D / 16;                  // bytes of a lane's V row
 
   h8 q[R][2 * KJ][QP];
-  int qe[R];        // a row's queries are q 2^qe
-  int vis[R];       // tokens that a row sees
+  int qe[R];                     // a row's queries are q 2^qe
+  int vis[R];                    // tokens that a row sees
   float ref[R], sum[R], top[R];  // top: largest weight so far, in units of 2^e
   int e[R];
   f4 acc[R][CB];
@@ -264,7 +214,7 @@ struct Wave {
   uint32_t v[8][CB / 4];
 
   // pages of the current range, one a lane
-  int64_t page0;
+  int page0;
   int id;
   float ks, vs;
   uint64_t bad;
@@ -277,18 +227,18 @@ struct Wave {
 
   const Args& p;
   const int lane, row16, group;
-  int64_t g;
+  int g;
   int h;
   int pages;  // of the sequence
 
   __device__ __forceinline__ explicit Wave(const Args& p_)
       : p(p_), lane(threadIdx.x & 63), row16(lane & 15), group(lane >> 4) {}
 
-  __device__ __forceinline__ void load_pages(int64_t first) {
+  __device__ __forceinline__ void load_pages(int first) {
     page0 = first;
-    const int64_t at = first + lane;
+    const int at = first + lane;
     const PageAttn& a = p.a;
-    id = at < pages ? a.table[g * a.max_pages + at] : -1;
+    id = at < pages ? a.table[(int64_t)g * a.max_pages + at] : -1;
     const bool known = id >= 0 && id < a.n_pages;
     if (!known) id = 0;
     const int64_t ph = (int64_t)id * a.H + h;
@@ -297,7 +247,7 @@ struct Wave {
     bad = __ballot(!known || !(fabsf(ks) < INFINITY) || !(fabsf(vs) < INFINITY));
   }
   __device__ __forceinline__ Half half(int t) {
-    const int l = __builtin_amdgcn_readfirstlane((int)((t >> p.shift) - page0));
+    const int l = __builtin_amdgcn_readfirstlane((t >> p.shift) - page0);
     const int64_t ph = (int64_t)__builtin_amdgcn_readlane(id, l) * p.a.H + h;
     const int64_t at = ((ph << p.shift) + (t & ((1 << p.shift) - 1))) * D;
     return {(const uint8_t*)p.a.k_pages + at, (const uint8_t*)p.a.v_pages + at,
@@ -323,53 +273,47 @@ struct Wave {
                          CB);
   }
 
-  __device__ __forceinline__ void begin(const Part& r, int n_rows) {
+  __device__ __forceinline__ void begin(const Part& r) {
     const PageAttn& a = p.a;
-    g = r.g;
-    h = r.h;
-    pages = (int)((r.s.len + (1 << p.shift) - 1) >> p.shift);
-    const int64_t i0 = r.tile * p.tile_tokens;
+    const int n_rows = r.n_tokens * a.G;
 #pragma unroll
     for (int s = 0; s < R; ++s) {
       const int rr = s * 16 + row16;
       const bool used = rr < n_rows;
-      const int i = used ? rr / a.G : 0, hq = used ? rr - i * a.G : 0;
-      vis[s] = !used ? 0 : (int)(r.s.causal ? r.s.len - r.s.rows + i0 + i + 1 : r.s.len);
-      const T* x = (const T*)a.q + (((r.s.begin + i0 + i) * a.H + h) * a.G + hq) * D;
-      float y[2 * KJ][8];
-      float big = 0.0f;
-      lost[s] = false;
+      const int i = used ? (int)((uint32_t)rr / (uint32_t)a.G) : 0, hq = used ? rr - i * a.G : 0;
+      vis[s] = !used ? 0 : r.s.causal ? r.s.len - r.s.rows + r.i0 + i + 1 : r.s.len;
+      const T* x = (const T*)a.q + (((int64_t)(r.s.begin + r.i0 + i) * a.H + r.h) * a.G + hq) * D;
+      T y[2 * KJ][8];
 #pragma unroll
-      for (int c = 0; c < 2 * KJ; ++c) {
-        load8(x + (c / 2) * 64 + group * 16 + (c % 2) * 8, y[c]);
+      for (int c = 0; c < 2 * KJ; ++c)
+        __builtin_memcpy(y[c], x + (c / 2) * 64 + group * 16 + (c % 2) * 8, sizeof(y[c]));
+      float big = 0.0f;
+      int l = 0;
+#pragma unroll
+      for (int c = 0; c < 2 * KJ; ++c)
 #pragma unroll
         for (int i8 = 0; i8 < 8; ++i8) {
-          if (!used) y[c][i8] = 0.0f;
-          if (!(fabsf(y[c][i8]) < INFINITY)) {
-            lost[s] = true;
-            y[c][i8] = 0.0f;
-          }
-          big = fmaxf(big, fabsf(y[c][i8]));
+          const float z = fabsf(to_float(y[c][i8]));
+          l |= !(z < INFINITY);
+          big = fmaxf(big, z);
         }
-      }
       big = fmaxf(big, __shfl_xor(big, 16, 64));
       big = fmaxf(big, __shfl_xor(big, 32, 64));
-      int l = lost[s];
       l |= __shfl_xor(l, 16, 64);
       l |= __shfl_xor(l, 32, 64);
       lost[s] = l;
       int ex = 0;
-      if (big > 0.0f) frexpf(big, &ex);
+      if (big > 0.0f && !l) frexpf(big, &ex);
       qe[s] = ex - 15;  // the largest is in [2^14, 2^15)
 #pragma unroll
       for (int c = 0; c < 2 * KJ; ++c)
 #pragma unroll
         for (int i8 = 0; i8 < 8; ++i8) {
-          const float z = ldexpf(y[c][i8], -qe[s]);
+          const float z = used && !l ? ldexpf(to_float(y[c][i8]), -qe[s]) : 0.0f;
           q[s][c][0][i8] = (_Float16)z;
           if constexpr (QP == 2) q[s][c][1][i8] = (_Float16)(z - (float)q[s][c][0][i8]);
         }
-      ref[s] = -INFINITY;
+      ref[s] = kNone;
       sum[s] = 0.0f;
       top[s] = 0.0f;
       e[s] = 0;
@@ -389,12 +333,11 @@ struct Wave {
       big[u] = fmaxf(big[u], __shfl_xor(big[u], 32, 64));
     }
     const float to = fmaxf(ref[r], fmaxf(big[0], big[1]));
-    const bool live = to > -INFINITY;
-    const float a = live ? exp2_(ref[r] - to) : 1.0f;
+    const float a = exp2_(ref[r] - to);
     float w = fmaxf(top[r], __shfl_xor(top[r], 16, 64));
     w = fmaxf(w, __shfl_xor(w, 32, 64));
     w = ldexpf(w * a, e[r]);
-    if (live) w = fmaxf(w, fmaxf(exp2_(big[0] - to) * fabsf(v0), exp2_(big[1] - to) * fabsf(v1)));
+    w = fmaxf(w, fmaxf(exp2_(big[0] - to) * fabsf(v0), exp2_(big[1] - to) * fabsf(v1)));
     int ew = e[r];
     if (w > 0.0f) {
       frexpf(w, &ew);
@@ -413,27 +356,13 @@ struct Wave {
     }
   }
 
-  // Weights of a tile, their sum in units of the reference, and the largest magnitude.
-  __device__ __forceinline__ void weights(int r, const f4* s, const float* v, float* w, float* all,
-                                          float* largest) const {
-    const float base = ref[r] > -INFINITY ? ref[r] : 0.0f;
-    *all = *largest = 0.0f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float c = limited(ldexpf(v[u], -e[r]));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = exp2_(s[u][i] - base);
-        *all += x;
-        w[4 * u + i] = x * c;
-        *largest = fmaxf(*largest, fabsf(w[4 * u + i]));
-      }
-    }
-  }
-
   // Tokens [from, to) of the item, from a multiple of 32.
-  __device__ __forceinline__ void run(int from, int to, int least, int most) {
+  __device__ __forceinline__ void run(const Part& r_, int from, int to) {
     if (from >= to) return;
+    const int least = r_.s.causal ? r_.s.len - r_.s.rows + r_.i0 + 1 : r_.s.len, most = r_.seen;
+    g = r_.g;
+    h = r_.h;
+    pages = (r_.s.len + (1 << p.shift) - 1) >> p.shift;
     load_pages(from >> p.shift);
     Half t[2] = {half(from), half(min(from + 16, to - 1) & ~15)};
     load_k(t);
@@ -483,16 +412,27 @@ struct Wave {
             for (int i = 0; i < 4; ++i)
               if (t0 + u * 16 + group * 4 + i >= vis[r]) s[r][u][i] = -INFINITY;
           }
-          big = fmaxf(big, fmaxf(fmaxf(s[r][u][0], s[r][u][1]), fmaxf(s[r][u][2], s[r][u][3])));
         }
-        if (__any(big > ref[r] + kLag)) move(r, s[r], vs[0], vs[1]);
         float w[8], more, largest;
-        weights(r, s[r], vs, w, &more, &largest);
-        sum[r] += more;
-        if (__any(largest >= kTop)) {  // (what was added to the sum moves with it)
+        for (int pass = 0; pass < 2; ++pass) {
+          float most_p = 0.0f;
+          more = largest = 0.0f;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float c = limited(ldexpf(vs[u], -e[r]));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = exp2_(s[r][u][i] - ref[r]);
+              most_p = fmaxf(most_p, x);
+              more += x;
+              w[4 * u + i] = x * c;
+              largest = fmaxf(largest, fabsf(w[4 * u + i]));
+            }
+          }
+          if (!__any(most_p > kLag || largest >= kTop)) break;
           move(r, s[r], vs[0], vs[1]);
-          weights(r, s[r], vs, w, &more, &largest);
         }
+        sum[r] += more;
         top[r] = fmaxf(top[r], largest);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -574,205 +514,162 @@ struct Joined {
   float ref, exp;
 };
 __device__ __forceinline__ float factor(float ref, float exp, const Joined& j) {
-  return ref > -INFINITY ? exp2_(ref - j.ref + (exp - j.exp)) : 0.0f;
-}
-__device__ __forceinline__ float weight(float ref, const Joined& j) {
-  return ref > -INFINITY ? exp2_(ref - j.ref) : 0.0f;
+  return ref > kNone ? exp2_(ref - j.ref + (exp - j.exp)) : 0.0f;
 }
 // acc / sum 2^exp; zero where nothing was seen
 __device__ __forceinline__ float finished(float acc, float sum, float exp) {
   return sum == 0.0f ? 0.0f : ldexpf(acc / sum, (int)exp);
 }
 
-template <typename T, int CODES, int D, int R>
-__global__ __launch_bounds__(kThreads) void main_kernel(Args p) {
-  __shared__ State<D, R> states[kWaves];
-  __shared__ int64_t lds[2 + kWaves];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // neighbours in the list of items share keys and values: one XCD's L2 serves them
-  const int per = p.n_wg / 8, b = blockIdx.x;
-  const int w = p.n_wg % 8 == 0 ? (b % 8) * per + b / 8 : b;
-  const Share sh = share(p, w, lds);
-  int64_t x = sh.lo, g = sh.seq, before = sh.before;
-  if (g >= p.a.n_seqs) return;
-  Seq s = sequence(p, g);
-  while (x < sh.hi) {
-    while (x >= before + s.head * p.a.H) {
-      before += s.head * p.a.H;
-      s = sequence(p, ++g);
-    }
-    Part r;
-    const int64_t after = part_at(p, s, g, before, x, p.cut ? sh.hi : INT64_MAX, &r);
-    x = after;
-    const bool skip = !p.cut && !r.begins;  // (an uncut item is whole where it begins)
-    if (skip) {
-      // the item began in the share before: its rest is that share's
-      const int64_t off = before + r.h * s.head + before_tile(p, s, r.tile);
-      x = off + r.seen + kItem;
-      continue;
-    }
-    const int64_t i0 = r.tile * p.tile_tokens;
-    const int n_rows = (int)min((int64_t)p.tile_tokens, s.rows - i0) * p.a.G;
-    const int64_t row0 = s.begin + i0;
-    Wave<T, CODES, D, R> wv(p);
-    wv.begin(r, n_rows);
-    const int tiles = (int)((r.to - r.from + 31) >> 5), each = (tiles + kWaves - 1) / kWaves;
-    const int from = (int)r.from + min(tiles, wave * each) * 32;
-    const int to = (int)min(r.to, r.from + (int64_t)min(tiles, (wave + 1) * each) * 32);
-    const int least = (int)(s.causal ? s.len - s.rows + i0 + 1 : s.len);
-    wv.run(from, to, least, (int)r.seen);
-    wv.store(&states[wave]);
-    __syncthreads();
-    State<D, R>* record =
-        (State<D, R>*)p.a.ws + 2 * (int64_t)w + (r.begins ? 1 : 0);
-    constexpr int kPer = D / 64;  // columns of a lane
-    for (int rr = wave; rr < n_rows; rr += kWaves) {
-      Joined j{-INFINITY, -INFINITY};
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) j.ref = fmaxf(j.ref, states[v].ref[rr]);
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v)
-        if (states[v].ref[rr] > -INFINITY)
-          j.exp = fmaxf(j.exp, ceilf(states[v].ref[rr] - j.ref) + states[v].exp[rr]);
-      if (j.exp == -INFINITY) j.exp = 0.0f;
-      float sum = 0.0f, acc[kPer];
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        const float ref = states[v].ref[rr], f = factor(ref, states[v].exp[rr], j);
-        sum += states[v].sum[rr] * weight(ref, j);
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) acc[c] += states[v].acc[rr][lane * kPer + c] * f;
-      }
-      if (r.begins && r.ends) {
-        const int i = rr / p.a.G, hq = rr - i * p.a.G;
-        float* out = p.a.out + (((row0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) out[c] = s.bad ? NAN : finished(acc[c], sum, j.exp);
-      } else {
-        if (lane == 0) {
-          record->ref[rr] = j.ref;
-          record->sum[rr] = sum;
-          record->exp[rr] = j.exp;
-        }
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) record->acc[rr][lane * kPer + c] = acc[c];
-      }
-    }
-    __syncthreads();
-  }
-}
 
-// Joins the records of the item that share w begins and does not end: its own second
-// one and the first ones of the shares behind it, up to the one that ends the item.  A
-// wavefront takes a row.
-template <int D, int R>
-__global__ __launch_bounds__(kThreads) void merge_kernel(Args p) {
-  __shared__ int64_t lds[2 + kWaves];
-  const int lane = threadIdx.x & 63, w = blockIdx.x;
+template <typename T, int CODES, int D, int R, int W>
+__global__ __launch_bounds__(64 * W, (R == 1 && D < 256 ? 16 : D < 256 ? 8 : 4) / 4) void main_kernel(Args p) {
+  __shared__ State<D, R> states[W];
+  const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Share sh = share(p, w, lds);
-  if (sh.lo >= sh.hi || w + 1 >= sh.n_wg) return;
-  int64_t g = sh.seq, before = sh.before;
-  Seq s = sequence(p, g);
-  while (sh.hi - 1 >= before + s.head * p.a.H) {
-    before += s.head * p.a.H;
-    s = sequence(p, ++g);
-  }
   Part r;
-  part_at(p, s, g, before, sh.hi - 1, sh.hi, &r);  // the last item of the share
-  const int64_t begin = before + r.h * s.head + before_tile(p, s, r.tile);
-  const int64_t end = begin + r.seen + kItem;
-  if (begin < sh.lo || end <= sh.hi) return;
-  int count = 2;
-  while (sh.begin(w + count) < end) ++count;
-  const State<D, R>* rec = (const State<D, R>*)p.a.ws;
-  auto at = [&](int i) { return rec + 2 * (int64_t)(w + i) + (i == 0); };
-  const int64_t i0 = r.tile * p.tile_tokens;
-  const int n_rows = (int)min((int64_t)p.tile_tokens, s.rows - i0) * p.a.G;
-  constexpr int kPer = D / 64;
-  for (int rr = blockIdx.y * kWaves + wave; rr < n_rows; rr += gridDim.y * kWaves) {
-    Joined j{-INFINITY, -INFINITY};
-    for (int i = lane; i < count; i += 64) j.ref = fmaxf(j.ref, at(i)->ref[rr]);
-    j.ref = wave_max(j.ref);
-    for (int i = lane; i < count; i += 64)
-      if (at(i)->ref[rr] > -INFINITY)
-        j.exp = fmaxf(j.exp, ceilf(at(i)->ref[rr] - j.ref) + at(i)->exp[rr]);
-    j.exp = wave_max(j.exp);
-    if (j.exp == -INFINITY) j.exp = 0.0f;
+  if (!part_at<W>(p, blockIdx.x, &r, (float*)states)) return;
+  __syncthreads();
+  Wave<T, CODES, D, R> wv(p);
+  wv.begin(r);
+  const int tiles = (r.to - r.from + 31) >> 5, each = (tiles + W - 1) / W;
+  const int from = r.from + min(tiles, wave * each) * 32;
+  wv.run(r, from, min(r.to, r.from + min(tiles, (wave + 1) * each) * 32));
+  wv.store(&states[wave]);
+  __syncthreads();
+  State<D, R>* record = (State<D, R>*)p.a.ws + blockIdx.x;
+  constexpr int kPer = D / 64;  // columns of a lane
+  const int n_rows = r.n_tokens * p.a.G;
+  for (int rr = wave; rr < n_rows; rr += W) {
+    Joined j{kNone, -0x1p30f};
+#pragma unroll
+    for (int v = 0; v < W; ++v) j.ref = fmaxf(j.ref, states[v].ref[rr]);
+#pragma unroll
+    for (int v = 0; v < W; ++v)
+      if (states[v].ref[rr] > kNone)
+        j.exp = fmaxf(j.exp, ceilf(states[v].ref[rr] - j.ref) + states[v].exp[rr]);
     float sum = 0.0f, acc[kPer];
 #pragma unroll
     for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
-    for (int i0 = 0; i0 < count; i0 += 64) {
-      const int n = min(64, count - i0);
-      float f = 0.0f;
-      if (lane < n) {
-        const State<D, R>* x = at(i0 + lane);
-        f = factor(x->ref[rr], x->exp[rr], j);
-        sum += x->sum[rr] * weight(x->ref[rr], j);
-      }
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
-        const float* x = at(i0 + i)->acc[rr] + lane * kPer;
-        const float fi = __shfl(f, i, 64);
 #pragma unroll
-        for (int c = 0; c < kPer; ++c) acc[c] += x[c] * fi;
-      }
+    for (int v = 0; v < W; ++v) {
+      const float ref = states[v].ref[rr], f = factor(ref, states[v].exp[rr], j);
+      sum += states[v].sum[rr] * exp2_(ref - j.ref);
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) acc[c] += states[v].acc[rr][lane * kPer + c] * f;
     }
-    sum = wave_sum(sum);
-    const int i = rr / p.a.G, hq = rr - i * p.a.G;
-    float* out = p.a.out + (((s.begin + i0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
+    if (r.parts == 1) {
+      const int i = rr / p.a.G, hq = rr - i * p.a.G;
+      float* out = p.a.out +
+                   (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
 #pragma unroll
-    for (int c = 0; c < kPer; ++c) out[c] = s.bad ? NAN : finished(acc[c], sum, j.exp);
+      for (int c = 0; c < kPer; ++c) out[c] = r.s.bad ? NAN : finished(acc[c], sum, j.exp);
+    } else {
+      if (lane == 0) {
+        record->ref[rr] = j.ref;
+        record->sum[rr] = sum;
+        record->exp[rr] = j.exp;
+      }
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) record->acc[rr][lane * kPer + c] = acc[c];
+    }
   }
+}
+
+// Joins the states of an item that was cut; the workgroup of its first part does it, a
+// wavefront for each row.
+template <int D, int R>
+__global__ __launch_bounds__(256) void merge_kernel(Args p) {
+  __shared__ float lds[10];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Part r;
+  if (!part_at<4>(p, blockIdx.x, &r, lds) || r.parts == 1 || r.part != 0) return;
+  const State<D, R>* rec = (const State<D, R>*)p.a.ws + blockIdx.x;
+  const int rr = blockIdx.y * 4 + wave;
+  if (rr >= r.n_tokens * p.a.G) return;
+  constexpr int kPer = D / 64;
+  Joined j{kNone, -0x1p30f};
+  for (int i = lane; i < r.parts; i += 64) j.ref = fmaxf(j.ref, rec[(int64_t)i * r.stride].ref[rr]);
+  j.ref = wave_max(j.ref);
+  for (int i = lane; i < r.parts; i += 64) {
+    const State<D, R>& x = rec[(int64_t)i * r.stride];
+    if (x.ref[rr] > kNone) j.exp = fmaxf(j.exp, ceilf(x.ref[rr] - j.ref) + x.exp[rr]);
+  }
+  j.exp = wave_max(j.exp);
+  float sum = 0.0f, acc[kPer];
+#pragma unroll
+  for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
+  for (int i0 = 0; i0 < r.parts; i0 += 64) {
+    const int n = min(64, r.parts - i0);
+    float f = 0.0f;
+    if (lane < n) {
+      const State<D, R>& x = rec[(int64_t)(i0 + lane) * r.stride];
+      f = factor(x.ref[rr], x.exp[rr], j);
+      sum += x.sum[rr] * exp2_(x.ref[rr] - j.ref);
+    }
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float* x = rec[(int64_t)(i0 + i) * r.stride].acc[rr] + lane * kPer;
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) acc[c] += x[c] * fi;
+    }
+  }
+  sum = wave_sum(sum);
+  const int i = rr / p.a.G, hq = rr - i * p.a.G;
+  float* out = p.a.out + (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D +
+               lane * kPer;
+#pragma unroll
+  for (int c = 0; c < kPer; ++c) out[c] = finished(acc[c], sum, j.exp);
 }
 
 // ---------------------------------------------------------------- dispatch --
 constexpr int kCu = 256;
 
 struct Plan {
-  int R, n_wg;
+  int R, parts, least;  // row tiles of 16 R; parts, at most; tokens of a part, at least
+  float target;
   bool cut;
   size_t bytes;
 };
-// Row tiles of 16 R: the large one where sequences have rows for it.
 Plan plan(int64_t n_seqs, int64_t n_rows, int H, int G, int64_t max_pages, int page, int d) {
   Plan p{};
-  const int large = d == 256 ? 2 : 4;
-  p.R = n_rows * G >= 24 * std::max<int64_t>(1, n_seqs) ? large : 1;
-  const int64_t room = max_pages * page;
-  const int64_t tile = 16 * p.R / G, items = (n_rows / tile + std::min(n_seqs, n_rows)) * H;
-  const int64_t most = p.R > 1 ? kCu : d == 64 ? 4 * kCu : d == 128 ? 3 * kCu : 2 * kCu;
-  p.n_wg = (int)std::max<int64_t>(1, std::min(most, items * (room + kItem) / kChunk));
-  if (p.n_wg > 8) p.n_wg = (p.n_wg + 7) / 8 * 8;
-  p.cut = room > kChunk && p.n_wg > 1;
-  p.bytes = p.cut ? (size_t)p.n_wg * 2 * 16 * p.R * (d + 3) * 4 : 0;
+  p.R = n_rows * G >= 24 * std::max<int64_t>(1, n_seqs) ? 2 : 1;
+  const int64_t room = max_pages * page, tile = 16 * p.R / G;
+  const int64_t items = (n_rows / tile + std::min(n_seqs, n_rows)) * H;
+  const int64_t target = p.R == 2 ? 2 * kCu : d == 256 ? kCu : 2 * kCu;
+  p.least = 512;
+  if (items >= kCu && room <= 4096) p.least = 4096;
+  p.target = (float)target;
+  p.cut = room > p.least;
+  p.parts = (int)(items + (p.cut ? target : 0));
+  p.bytes = p.cut ? (size_t)p.parts * 16 * p.R * (d + 3) * 4 : 0;
   return p;
 }
 
 template <typename T, int CODES, int D, int R>
-int launch(const Args& p, hipStream_t st) {
-  main_kernel<T, CODES, D, R><<<p.n_wg, kThreads, 0, st>>>(p);
+int launch(const Args& p, const Plan& pl, hipStream_t st) {
+  constexpr int W = R == 1 ? 8 : 4;
+  main_kernel<T, CODES, D, R, W><<<pl.parts, 64 * W, 0, st>>>(p);
   int rc = (int)hipGetLastError();
-  if (rc != 0 || !p.cut) return rc;
+  if (rc != 0 || !pl.cut) return rc;
   const int rows = std::min(16 * R, p.tile_tokens * p.a.G);
-  merge_kernel<D, R><<<dim3(p.n_wg, (rows + kWaves - 1) / kWaves), kThreads, 0, st>>>(p);
+  merge_kernel<D, R><<<dim3(pl.parts, (rows + 3) / 4), 256, 0, st>>>(p);
   return (int)hipGetLastError();
 }
 template <typename T, int CODES>
-int launch_d(const Args& p, int R, hipStream_t st) {
+int launch_d(const Args& p, const Plan& pl, hipStream_t st) {
   switch (p.a.d) {
-    case 64: return R == 1 ? launch<T, CODES, 64, 1>(p, st) : launch<T, CODES, 64, 4>(p, st);
-    case 128: return R == 1 ? launch<T, CODES, 128, 1>(p, st) : launch<T, CODES, 128, 4>(p, st);
-    default: return R == 1 ? launch<T, CODES, 256, 1>(p, st) : launch<T, CODES, 256, 2>(p, st);
+    case 64: return pl.R == 1 ? launch<T, CODES, 64, 1>(p, pl, st) : launch<T, CODES, 64, 2>(p, pl, st);
+    case 128: return pl.R == 1 ? launch<T, CODES, 128, 1>(p, pl, st) : launch<T, CODES, 128, 2>(p, pl, st);
+    default: return pl.R == 1 ? launch<T, CODES, 256, 1>(p, pl, st) : launch<T, CODES, 256, 2>(p, pl, st);
   }
 }
 template <typename T>
-int launch_codes(const Args& p, int R, hipStream_t st) {
-  return p.a.codes == FIBQ_INT8 ? launch_d<T, FIBQ_INT8>(p, R, st)
-                                : launch_d<T, FIBQ_E4M3>(p, R, st);
+int launch_codes(const Args& p, const Plan& pl, hipStream_t st) {
+  return p.a.codes == FIBQ_INT8 ? launch_d<T, FIBQ_INT8>(p, pl, st)
+                                : launch_d<T, FIBQ_E4M3>(p, pl, st);
 }
 
 }  // namespace pa
@@ -785,12 +682,12 @@ size_t page_attn_workspace_bytes(int64_t n_seqs, int64_t n_rows, int H, int G, i
 int launch_page_attn(const PageAttn& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   const pa::Plan pl = pa::plan(a.n_seqs, a.n_rows, a.H, a.G, a.max_pages, a.page, a.d);
-  const pa::Args p{a,       16 * pl.R / a.G, __builtin_ctz(a.page),
-                   pl.n_wg, pl.cut,          a.scale * 1.44269504088896341f};
+  const pa::Args p{a,        16 * pl.R / a.G, __builtin_ctz(a.page),
+                   pl.least, pl.target,       a.scale * 1.44269504088896341f};
   switch (a.q_dtype) {
-    case FIBQ_F32: return pa::launch_codes<float>(p, pl.R, st);
-    case FIBQ_F16: return pa::launch_codes<f16_t>(p, pl.R, st);
-    default: return pa::launch_codes<bf16_t>(p, pl.R, st);
+    case FIBQ_F32: return pa::launch_codes<float>(p, pl, st);
+    case FIBQ_F16: return pa::launch_codes<f16_t>(p, pl, st);
+    default: return pa::launch_codes<bf16_t>(p, pl, st);
   }
 }
 
