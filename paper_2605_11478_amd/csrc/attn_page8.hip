@@ -34,12 +34,13 @@ namespace pa {
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLag = 0x1p8f;      // exp2 of what a score may exceed its row's reference by
 constexpr float kTop = 0x1p15f;     // weights stay below (binary16)
 constexpr int kTopBits = 7;         // exponent of a row's largest weight when e is set
-constexpr float kLimit = 0x1p126f;  // of scores
+constexpr float kLimit = 0x1p94f;   // of a score's factors: scores stay below 2^126, codes' products being below 2^32
 constexpr float kNone = -0x1p127f;  // reference of a row that has seen nothing
 
 struct Args {
@@ -49,6 +50,9 @@ struct Args {
   int least_part;   // tokens of a part, at least
   float target;     // parts that fill the card
   float scale2;     // scale log2(e)
+  int rows;         // query rows of an item, at most
+  int cut;          // items may be cut
+  int parts;        // at most
 };
 
 // ------------------------------------------------------------------- work --
@@ -57,6 +61,11 @@ struct Seq {
   bool bad, causal;
   int tiles;
 };
+// the same value in every lane, in a scalar register
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Seq uni(const Seq& s) {
+  return {uni(s.begin), uni(s.rows), uni(s.len), (bool)uni(s.bad), (bool)uni(s.causal), uni(s.tiles)};
+}
 __device__ __forceinline__ Seq sequence(const Args& p, int g) {
   Seq s{};
   const PageAttn& a = p.a;
@@ -78,69 +87,73 @@ struct Part {
   int g, h, tile, part, parts;
   int i0, n_tokens;  // its query tokens
   int seen, from, to;
-  int stride;  // from one part of an item to the next
 };
 // Part w of all, in every thread of the workgroup.  Parts are in the order of sequences,
 // tiles from the last (a causal sequence's longest), parts, heads.  False: there is none.
-template <int W>
-__device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, float* lds) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+__device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, W = blockDim.x >> 6;
   const int n = (int)p.a.n_seqs;
-  Seq s{};
-  float tokens = 0.0f;
-  for (int g = tid; g < n; g += 64 * W) {
-    s = sequence(p, g);
-    tokens += (float)s.tiles * (float)s.len;
-  }
-  tokens = wave_sum(tokens);
-  if (lane == 0) lds[wave] = tokens;
-  __syncthreads();
-  tokens = 0.0f;
-#pragma unroll
-  for (int v = 0; v < W; ++v) tokens += lds[v];
-  // (a little more than the exact quotient, so that rounding never makes a part too many)
-  const float share = tokens * (float)p.a.H * 1.001f / p.target;
-  const int part = (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
-  int* at = (int*)lds + W;  // {sequence, parts before it}, sums of the wavefronts
-  __syncthreads();
-  if (tid == 0) at[0] = -1;
-  int before = 0;
-  for (int g0 = 0; g0 < n; g0 += 64 * W) {
-    const int g = g0 + tid;
-    if (n > 64 * W) s = g < n ? sequence(p, g) : Seq{};
-    const int parts = max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part));
-    const int mine = g < n ? s.tiles * parts * p.a.H : 0;
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += y;
-    }
-    if (lane == 63) at[2 + wave] = upto;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int v = 0; v < W; ++v) {
-      if (v < wave) upto += at[2 + v];
-      all += at[2 + v];
-    }
-    if (w < before + upto && w >= before + upto - mine) {
-      at[0] = g;
-      at[1] = before + upto - mine;
-    }
-    __syncthreads();
-    before += all;
-    if (w < before) break;
-  }
-  const int g = at[0];
-  if (g < 0) return false;
-  s = sequence(p, g);
-  uint32_t i = (uint32_t)(w - at[1]);
   const uint32_t H = (uint32_t)p.a.H;
+  int g, first = 0, part = 0;
+  if (!p.cut && !p.a.starts) {  // one item, one part for each sequence and head
+    g = (int)((uint32_t)w / H);
+    first = g * (int)H;
+  } else {
+    Seq s{};
+    float tokens = 0.0f;
+    for (int at = tid; at < n; at += 64 * W) {
+      s = sequence(p, at);
+      tokens += (float)s.tiles * (float)s.len;
+    }
+    tokens = wave_sum(tokens);
+    if (lane == 0) lds[wave] = __float_as_int(tokens);
+    __syncthreads();
+    tokens = 0.0f;
+    for (int v = 0; v < W; ++v) tokens += __int_as_float(lds[v]);
+    // (a little more than the exact quotient, so that rounding never makes a part too many)
+    const float share = tokens * (float)p.a.H * 1.001f / p.target;
+    part = (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
+    int* found = lds + W;  // sequence, parts before it
+    int* sums = found + 2;
+    __syncthreads();
+    if (tid == 0) found[0] = -1;
+    int before = 0;
+    for (int g0 = 0; g0 < n; g0 += 64 * W) {
+      const int at = g0 + tid;
+      if (n > 64 * W) s = at < n ? sequence(p, at) : Seq{};
+      const int parts = max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part));
+      const int mine = at < n ? s.tiles * parts * p.a.H : 0;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += y;
+      }
+      if (lane == 63) sums[wave] = upto;
+      __syncthreads();
+      int all = 0;
+      for (int v = 0; v < W; ++v) {
+        if (v < wave) upto += sums[v];
+        all += sums[v];
+      }
+      if (w < before + upto && w >= before + upto - mine) {
+        found[0] = at;
+        found[1] = before + upto - mine;
+      }
+      __syncthreads();
+      before += all;
+      if (w < before) break;
+    }
+    g = uni(found[0]);
+    if (g < 0) return false;
+    first = uni(found[1]);
+    part = uni(part);
+  }
+  const Seq s = uni(sequence(p, g));
+  uint32_t i = (uint32_t)(w - first);
   r->s = s;
   r->g = g;
-  r->stride = p.a.H;
-  r->parts = max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part));
+  r->parts = part ? max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part)) : 1;
   if (i >= (uint32_t)s.tiles * (uint32_t)r->parts * H) return false;  // (counts that overflowed)
   r->h = (int)(i % H);
   i /= H;
@@ -154,14 +167,34 @@ __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, float* ld
   r->to = min(r->from + size, r->seen);
   return true;
 }
+constexpr int part_lds(int W) { return 2 * W + 2; }
 
 // ---------------------------------------------------------------- records --
-// A state of an item's rows: references, sums, exponents and accumulators.
-template <int D, int R>
+// A state of an item's rows: references, sums, exponents, and accumulators [rows][D].
+__host__ __device__ constexpr int state_head(int rows) { return (3 * rows + 3) & ~3; }
+__host__ __device__ constexpr int state_floats(int rows, int d) { return state_head(rows) + rows * d; }
+template <int D>
 struct State {
-  float ref[16 * R], sum[16 * R], exp[16 * R];
-  float acc[16 * R][D];
+  float* at;
+  int rows;
+  __device__ __forceinline__ float& ref(int r) const { return at[r]; }
+  __device__ __forceinline__ float& sum(int r) const { return at[rows + r]; }
+  __device__ __forceinline__ float& exp(int r) const { return at[2 * rows + r]; }
+  __device__ __forceinline__ float* acc(int r) const { return at + state_head(rows) + r * D; }
 };
+template <int D>
+__device__ __forceinline__ State<D> state(void* base, int64_t i, int rows) {
+  return {(float*)base + i * state_floats(rows, D), rows};
+}
+
+// What the second launch joins, one for each part: the parts of the item that begins
+// there if it was cut (else 0), its rows, its first query row and its head.
+struct Join {
+  int parts, n_rows, row, h;
+};
+__device__ __forceinline__ Join* joins(const Args& p, int d) {
+  return (Join*)((float*)p.a.ws + (int64_t)p.parts * state_floats(p.rows, d));
+}
 
 // -------------------------------------------------------------- operators --
 template <int CODES>
@@ -225,6 +258,8 @@ struct Wave {
     bool bad;
   };
 
+  Half t[2];
+
   const Args& p;
   const int lane, row16, group;
   int g;
@@ -234,13 +269,16 @@ struct Wave {
   __device__ __forceinline__ explicit Wave(const Args& p_)
       : p(p_), lane(threadIdx.x & 63), row16(lane & 15), group(lane >> 4) {}
 
-  __device__ __forceinline__ void load_pages(int first) {
+  // Ids of the 64 pages from `first` on, one a lane (-1 behind the last), and their scales.
+  __device__ __forceinline__ int page_of(int first) {
     page0 = first;
     const int at = first + lane;
+    return at < pages ? p.a.table[(int64_t)g * p.a.max_pages + at] : -1;
+  }
+  __device__ __forceinline__ void scales_of(int ids) {
     const PageAttn& a = p.a;
-    id = at < pages ? a.table[(int64_t)g * a.max_pages + at] : -1;
-    const bool known = id >= 0 && id < a.n_pages;
-    if (!known) id = 0;
+    const bool known = ids >= 0 && ids < a.n_pages;
+    id = known ? ids : 0;
     const int64_t ph = (int64_t)id * a.H + h;
     ks = a.k_scales[ph] * p.scale2;
     vs = a.v_scales[ph];
@@ -273,9 +311,15 @@ struct Wave {
                          CB);
   }
 
-  __device__ __forceinline__ void begin(const Part& r) {
+  // The part's first loads, each as soon as its address is known, then its queries.
+  __device__ __forceinline__ void begin(const Part& r, int from, int to) {
     const PageAttn& a = p.a;
+    g = r.g;
+    h = r.h;
+    pages = (r.s.len + (1 << p.shift) - 1) >> p.shift;
+    const int first = page_of(from >> p.shift);
     const int n_rows = r.n_tokens * a.G;
+    T y[R][2 * KJ][8];
 #pragma unroll
     for (int s = 0; s < R; ++s) {
       const int rr = s * 16 + row16;
@@ -283,17 +327,25 @@ struct Wave {
       const int i = used ? (int)((uint32_t)rr / (uint32_t)a.G) : 0, hq = used ? rr - i * a.G : 0;
       vis[s] = !used ? 0 : r.s.causal ? r.s.len - r.s.rows + r.i0 + i + 1 : r.s.len;
       const T* x = (const T*)a.q + (((int64_t)(r.s.begin + r.i0 + i) * a.H + r.h) * a.G + hq) * D;
-      T y[2 * KJ][8];
 #pragma unroll
       for (int c = 0; c < 2 * KJ; ++c)
-        __builtin_memcpy(y[c], x + (c / 2) * 64 + group * 16 + (c % 2) * 8, sizeof(y[c]));
+        __builtin_memcpy(y[s][c], x + (c / 2) * 64 + group * 16 + (c % 2) * 8, sizeof(y[s][c]));
+    }
+    scales_of(first);
+    t[0] = half(from);
+    t[1] = half(min(from + 16, to - 1) & ~15);
+    load_k(t);
+    load_v(t);
+#pragma unroll
+    for (int s = 0; s < R; ++s) {
+      const bool used = s * 16 + row16 < n_rows;
       float big = 0.0f;
       int l = 0;
 #pragma unroll
       for (int c = 0; c < 2 * KJ; ++c)
 #pragma unroll
         for (int i8 = 0; i8 < 8; ++i8) {
-          const float z = fabsf(to_float(y[c][i8]));
+          const float z = fabsf(to_float(y[s][c][i8]));
           l |= !(z < INFINITY);
           big = fmaxf(big, z);
         }
@@ -303,32 +355,37 @@ struct Wave {
       l |= __shfl_xor(l, 32, 64);
       lost[s] = l;
       int ex = 0;
-      if (big > 0.0f && !l) frexpf(big, &ex);
+      if (big > 0.0f && !l) ex = __builtin_amdgcn_frexp_expf(big);
       qe[s] = ex - 15;  // the largest is in [2^14, 2^15)
 #pragma unroll
       for (int c = 0; c < 2 * KJ; ++c)
 #pragma unroll
         for (int i8 = 0; i8 < 8; ++i8) {
-          const float z = used && !l ? ldexpf(to_float(y[c][i8]), -qe[s]) : 0.0f;
+          const float z = used && !l ? ldexpf(to_float(y[s][c][i8]), -qe[s]) : 0.0f;
           q[s][c][0][i8] = (_Float16)z;
           if constexpr (QP == 2) q[s][c][1][i8] = (_Float16)(z - (float)q[s][c][0][i8]);
         }
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int s = 0; s < R; ++s) {
       ref[s] = kNone;
       sum[s] = 0.0f;
       top[s] = 0.0f;
       e[s] = 0;
+      lost[s] = false;
 #pragma unroll
       for (int c = 0; c < CB; ++c) acc[s][c] = f4{0, 0, 0, 0};
     }
   }
 
   // A row's reference becomes its largest score, and its weights' exponent that of the
-  // largest weight.  s: scores, -inf where masked.
-  __device__ __forceinline__ void move(int r, const f4* s, float v0, float v1) {
-    float big[2];
+  // largest weight.  b0, b1: the lane's largest scores in the two halves of the tile.
+  __device__ __forceinline__ void move(int r, float b0, float b1, float v0, float v1) {
+    float big[2] = {b0, b1};
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      big[u] = fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3]));
       big[u] = fmaxf(big[u], __shfl_xor(big[u], 16, 64));
       big[u] = fmaxf(big[u], __shfl_xor(big[u], 32, 64));
     }
@@ -339,10 +396,7 @@ struct Wave {
     w = ldexpf(w * a, e[r]);
     w = fmaxf(w, fmaxf(exp2_(big[0] - to) * fabsf(v0), exp2_(big[1] - to) * fabsf(v1)));
     int ew = e[r];
-    if (w > 0.0f) {
-      frexpf(w, &ew);
-      ew = max(ew - 1 - kTopBits, -100);
-    }
+    if (w > 0.0f) ew = max(__builtin_amdgcn_frexp_expf(w) - 1 - kTopBits, -100);
     const float by = ldexpf(a, e[r] - ew);
     sum[r] *= a;
     top[r] = ldexpf(w, -ew);
@@ -358,15 +412,8 @@ struct Wave {
 
   // Tokens [from, to) of the item, from a multiple of 32.
   __device__ __forceinline__ void run(const Part& r_, int from, int to) {
-    if (from >= to) return;
+    const int last = (to - 1) & ~31;
     const int least = r_.s.causal ? r_.s.len - r_.s.rows + r_.i0 + 1 : r_.s.len, most = r_.seen;
-    g = r_.g;
-    h = r_.h;
-    pages = (r_.s.len + (1 << p.shift) - 1) >> p.shift;
-    load_pages(from >> p.shift);
-    Half t[2] = {half(from), half(min(from + 16, to - 1) & ~15)};
-    load_k(t);
-    load_v(t);
     for (int t0 = from; t0 < to; t0 += 32) {
       f4 s[R][2];
 #pragma unroll
@@ -386,58 +433,71 @@ struct Wave {
               s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, q[r][2 * j + 1][i], s[r][u], 0, 0, 0);
             }
         }
-      // the next tile's keys are on their way from here on, its values from the end
+      // The next tile's keys are on their way from here on, its values from the end.  (The
+      // last tile's own again: a branch around the loads would make each wait one for all.)
       const float ks[2] = {t[0].ks, t[1].ks}, vs[2] = {t[0].vs, t[1].vs};
       const bool lost_page[2] = {t[0].bad, t[1].bad};
-      const int next = t0 + 32;
-      if (next < to) {
-        if ((next >> p.shift) - page0 >= 63) load_pages(next >> p.shift);
-        t[0] = half(next);
-        t[1] = half(min(next + 16, to - 1) & ~15);
-        load_k(t);
-      }
-      const bool masked = t0 + 32 > least;
+      const int next = min(t0 + 32, last);
+      if ((next >> p.shift) - page0 >= 63) scales_of(page_of(next >> p.shift));
+      t[0] = half(next);
+      t[1] = half(min(next + 16, to - 1) & ~15);
+      load_k(t);
+      const bool masked = t0 + 32 > least || lost_page[0] || lost_page[1];
       h8 hi[R], lo[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        float big = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const float f = limited(ldexpf(ks[u], qe[r]));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[r][u][i] = limited(s[r][u][i] * f);
-          if (lost_page[u]) s[r][u] = f4{NAN, NAN, NAN, NAN};
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (t0 + u * 16 + group * 4 + i >= vis[r]) s[r][u][i] = -INFINITY;
-          }
-        }
+        const float f[2] = {limited(ldexpf(ks[0], qe[r])), limited(ldexpf(ks[1], qe[r]))};
         float w[8], more, largest;
-        for (int pass = 0; pass < 2; ++pass) {
-          float most_p = 0.0f;
-          more = largest = 0.0f;
+        auto hide = [&](float* x) {  // what a row does not see, and what is no number
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (lost_page[i / 4]) x[i] = NAN;
+            if (t0 + (i / 4) * 16 + group * 4 + i % 4 >= vis[r]) x[i] = -INFINITY;
+          }
+        };
+        auto weigh = [&]() {  // whether all weights are in their range
+          float x[8], top_p[2];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s[r][i / 4][i % 4], f[i / 4], -ref[r]);
+          if (masked) hide(x);
+          more = 0.0f;
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const float c = limited(ldexpf(vs[u], -e[r]));
+            top_p[u] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float x = exp2_(s[r][u][i] - ref[r]);
-              most_p = fmaxf(most_p, x);
-              more += x;
-              w[4 * u + i] = x * c;
-              largest = fmaxf(largest, fabsf(w[4 * u + i]));
+            for (int i = 4 * u; i < 4 * u + 4; ++i) {
+              x[i] = exp2_(x[i]);
+              top_p[u] = fmaxf(top_p[u], x[i]);
+              more += x[i];
+              w[i] = x[i] * c;
             }
+            largest = u ? fmaxf(largest, top_p[u] * fabsf(c)) : top_p[u] * fabsf(c);
           }
-          if (!__any(most_p > kLag || largest >= kTop)) break;
-          move(r, s[r], vs[0], vs[1]);
+          return !__any(fmaxf(top_p[0], top_p[1]) > kLag || largest >= kTop);
+        };
+        if (!weigh()) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] = s[r][i / 4][i % 4];
+            asm volatile("" : "+v"(x[i]));  // (nothing of this before the branch)
+            x[i] *= f[i / 4];
+          }
+          if (masked) hide(x);
+          move(r, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+               fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])), vs[0], vs[1]);
+          weigh();
         }
         sum[r] += more;
         top[r] = fmaxf(top[r], largest);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          hi[r][i] = (_Float16)w[i];
-          lo[r][i] = (_Float16)(w[i] - (float)hi[r][i]);
+        for (int i = 0; i < 8; i += 2) {
+          const h2 x = __builtin_convertvector(f2{w[i], w[i + 1]}, h2);
+          const h2 y = __builtin_convertvector(f2{__builtin_fmaf((float)x[0], -1.0f, w[i]),
+                                                  __builtin_fmaf((float)x[1], -1.0f, w[i + 1])}, h2);
+          hi[r][i] = x[0], hi[r][i + 1] = x[1];
+          lo[r][i] = y[0], lo[r][i + 1] = y[1];
         }
       }
       if (t0 + 32 > most) {  // what lies behind the last token may hold anything
@@ -468,7 +528,7 @@ struct Wave {
             }
           }
         }
-      if (next < to) load_v(t);
+      load_v(t);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -491,20 +551,23 @@ struct Wave {
     return h8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
   }
 
-  __device__ __forceinline__ void store(State<D, R>* to) const {
+  __device__ __forceinline__ void store(const State<D>& to) const {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (group == 0) {
-        to->ref[r * 16 + row16] = ref[r];
-        to->sum[r * 16 + row16] = lost[r] && sum[r] > 0.0f ? NAN : sum[r];
-        to->exp[r * 16 + row16] = (float)e[r];
+      if (group == 0 && r * 16 + row16 < to.rows) {
+        to.ref(r * 16 + row16) = ref[r];
+        to.sum(r * 16 + row16) = lost[r] && sum[r] > 0.0f ? NAN : sum[r];
+        to.exp(r * 16 + row16) = (float)e[r];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) {
+        const int rr = r * 16 + group * 4 + i;
+        if (rr >= to.rows) break;
 #pragma unroll
         for (int c = 0; c < CB; c += 4)
-          *(f4*)&to->acc[r * 16 + group * 4 + i][row16 * CB + c] =
+          *(f4*)(to.acc(rr) + row16 * CB + c) =
               f4{acc[r][c][i], acc[r][c + 1][i], acc[r][c + 2][i], acc[r][c + 3][i]};
+      }
     }
   }
 };
@@ -522,41 +585,62 @@ __device__ __forceinline__ float finished(float acc, float sum, float exp) {
 }
 
 
-template <typename T, int CODES, int D, int R, int W>
-__global__ __launch_bounds__(64 * W, (R == 1 && D < 256 ? 16 : D < 256 ? 8 : 4) / 4) void main_kernel(Args p) {
-  __shared__ State<D, R> states[W];
-  const int lane = threadIdx.x & 63;
+// Wavefronts that a SIMD holds at once, by registers.
+__host__ __device__ constexpr int waves_of_simd(int R, int D) {
+  return R == 1 ? (D == 64 ? 4 : D == 128 ? 3 : 2) : D == 64 ? 3 : D == 128 ? 2 : 1;
+}
+
+template <typename T, int CODES, int D, int R>
+__global__ __launch_bounds__(R == 1 && D == 64 ? 512 : 256, waves_of_simd(R, D))
+void main_kernel(Args p) {
+  extern __shared__ __align__(16) float states[];
+  const int lane = threadIdx.x & 63, W = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Part r;
-  if (!part_at<W>(p, blockIdx.x, &r, (float*)states)) return;
-  __syncthreads();
+  Part r{};
+  const bool live = part_at(p, blockIdx.x, &r, (int*)states);
+  if (p.cut && threadIdx.x == 0)
+    joins(p, D)[blockIdx.x] = Join{live && r.part == 0 && r.parts > 1 ? r.parts : 0, r.n_tokens * p.a.G,
+                                   r.s.begin + r.i0, r.h};
+  if (!live) return;
   Wave<T, CODES, D, R> wv(p);
-  wv.begin(r);
-  const int tiles = (r.to - r.from + 31) >> 5, each = (tiles + W - 1) / W;
+  const int tiles = (r.to - r.from + 31) >> 5, each = (int)((uint32_t)(tiles + W - 1) / (uint32_t)W);
   const int from = r.from + min(tiles, wave * each) * 32;
-  wv.run(r, from, min(r.to, r.from + min(tiles, (wave + 1) * each) * 32));
-  wv.store(&states[wave]);
+  const int to = min(r.to, r.from + min(tiles, (wave + 1) * each) * 32);
+  wv.clear();
+  if (from < to) {
+    wv.begin(r, from, to);
+    wv.run(r, from, to);
+  }
+  __syncthreads();  // (part_at's words have been read)
+  wv.store(state<D>(states, wave, p.rows));
   __syncthreads();
-  State<D, R>* record = (State<D, R>*)p.a.ws + blockIdx.x;
+  const State<D> record = state<D>(p.a.ws, blockIdx.x, p.rows);
   constexpr int kPer = D / 64;  // columns of a lane
   const int n_rows = r.n_tokens * p.a.G;
   for (int rr = wave; rr < n_rows; rr += W) {
+    // (of 8 states, the last one's again behind it: reads that wait for nothing)
     Joined j{kNone, -0x1p30f};
+    float refs[8], exps[8], sum = 0.0f, acc[kPer];
 #pragma unroll
-    for (int v = 0; v < W; ++v) j.ref = fmaxf(j.ref, states[v].ref[rr]);
+    for (int v = 0; v < 8; ++v) {
+      const State<D> x = state<D>(states, min(v, W - 1), p.rows);
+      refs[v] = x.ref(rr);
+      exps[v] = x.exp(rr);
+      j.ref = fmaxf(j.ref, refs[v]);
+    }
 #pragma unroll
-    for (int v = 0; v < W; ++v)
-      if (states[v].ref[rr] > kNone)
-        j.exp = fmaxf(j.exp, ceilf(states[v].ref[rr] - j.ref) + states[v].exp[rr]);
-    float sum = 0.0f, acc[kPer];
+    for (int v = 0; v < 8; ++v)
+      if (refs[v] > kNone) j.exp = fmaxf(j.exp, ceilf(refs[v] - j.ref) + exps[v]);
 #pragma unroll
     for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
 #pragma unroll
-    for (int v = 0; v < W; ++v) {
-      const float ref = states[v].ref[rr], f = factor(ref, states[v].exp[rr], j);
-      sum += states[v].sum[rr] * exp2_(ref - j.ref);
+    for (int v = 0; v < 8; ++v) {
+      if (v >= W) break;
+      const State<D> x = state<D>(states, v, p.rows);
+      const float f = factor(refs[v], exps[v], j);
+      sum += x.sum(rr) * exp2_(refs[v] - j.ref);
 #pragma unroll
-      for (int c = 0; c < kPer; ++c) acc[c] += states[v].acc[rr][lane * kPer + c] * f;
+      for (int c = 0; c < kPer; ++c) acc[c] += x.acc(rr)[lane * kPer + c] * f;
     }
     if (r.parts == 1) {
       const int i = rr / p.a.G, hq = rr - i * p.a.G;
@@ -566,102 +650,153 @@ __global__ __launch_bounds__(64 * W, (R == 1 && D < 256 ? 16 : D < 256 ? 8 : 4) 
       for (int c = 0; c < kPer; ++c) out[c] = r.s.bad ? NAN : finished(acc[c], sum, j.exp);
     } else {
       if (lane == 0) {
-        record->ref[rr] = j.ref;
-        record->sum[rr] = sum;
-        record->exp[rr] = j.exp;
+        record.ref(rr) = j.ref;
+        record.sum(rr) = sum;
+        record.exp(rr) = j.exp;
       }
 #pragma unroll
-      for (int c = 0; c < kPer; ++c) record->acc[rr][lane * kPer + c] = acc[c];
+      for (int c = 0; c < kPer; ++c) record.acc(rr)[lane * kPer + c] = acc[c];
     }
   }
 }
 
-// Joins the states of an item that was cut; the workgroup of its first part does it, a
-// wavefront for each row.
-template <int D, int R>
+// Joins the states of the items that were cut: a wavefront for each row or, where items
+// have few rows and many parts, four (WIDE).  What it reads has just been written by
+// other XCDs, so each read takes long: many are on their way at once.
+template <int D, int WIDE>
 __global__ __launch_bounds__(256) void merge_kernel(Args p) {
-  __shared__ float lds[10];
+  constexpr int kPer = D / 64, kBatch = 8;
+  __shared__ float joined[4][3 + D];
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Part r;
-  if (!part_at<4>(p, blockIdx.x, &r, lds) || r.parts == 1 || r.part != 0) return;
-  const State<D, R>* rec = (const State<D, R>*)p.a.ws + blockIdx.x;
-  const int rr = blockIdx.y * 4 + wave;
-  if (rr >= r.n_tokens * p.a.G) return;
-  constexpr int kPer = D / 64;
-  Joined j{kNone, -0x1p30f};
-  for (int i = lane; i < r.parts; i += 64) j.ref = fmaxf(j.ref, rec[(int64_t)i * r.stride].ref[rr]);
-  j.ref = wave_max(j.ref);
-  for (int i = lane; i < r.parts; i += 64) {
-    const State<D, R>& x = rec[(int64_t)i * r.stride];
-    if (x.ref[rr] > kNone) j.exp = fmaxf(j.exp, ceilf(x.ref[rr] - j.ref) + x.exp[rr]);
-  }
-  j.exp = wave_max(j.exp);
-  float sum = 0.0f, acc[kPer];
+  const int wave = uni((int)(threadIdx.x >> 6)), mine = WIDE > 1 ? wave : 0;
+  const Join* list = joins(p, D);
+  for (int w0 = blockIdx.x; w0 < p.parts; w0 += 64 * gridDim.x) {
+    const int wl = w0 + lane * gridDim.x;
+    uint64_t todo = __ballot(wl < p.parts && list[min(wl, p.parts - 1)].parts > 0);
+    for (; todo; todo &= todo - 1) {
+      const int w = w0 + (__ffsll((unsigned long long)todo) - 1) * gridDim.x;
+      const int parts = uni(list[w].parts), n_rows = uni(list[w].n_rows), row = uni(list[w].row),
+                h = uni(list[w].h);
+      const int rows_apart = gridDim.y * (4 / WIDE);
+      for (int rr = blockIdx.y * (4 / WIDE) + (WIDE > 1 ? 0 : wave); rr < n_rows; rr += rows_apart) {
+        Joined j{kNone, -0x1p30f};
+        float sum = 0.0f, acc[kPer];
 #pragma unroll
-  for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
-  for (int i0 = 0; i0 < r.parts; i0 += 64) {
-    const int n = min(64, r.parts - i0);
-    float f = 0.0f;
-    if (lane < n) {
-      const State<D, R>& x = rec[(int64_t)(i0 + lane) * r.stride];
-      f = factor(x.ref[rr], x.exp[rr], j);
-      sum += x.sum[rr] * exp2_(x.ref[rr] - j.ref);
+        for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
+        // parts of this wavefront: mine, mine + WIDE, ..., kBatch at a time
+        for (int i0 = mine; i0 < parts; i0 += WIDE * kBatch) {
+          float x[kBatch][kPer];
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const int i = min(i0 + b * WIDE, parts - 1);
+            const State<D> s = state<D>(p.a.ws, w + (int64_t)i * p.a.H, p.rows);
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) x[b][c] = s.acc(rr)[lane * kPer + c];
+          }
+          const int i = i0 + lane % kBatch * WIDE;
+          const State<D> s = state<D>(p.a.ws, w + (int64_t)min(i, parts - 1) * p.a.H, p.rows);
+          const float ref = i < parts ? s.ref(rr) : kNone, exp = s.exp(rr), all = s.sum(rr);
+          const Joined old = j;
+          j.ref = fmaxf(j.ref, wave_max(ref));
+          j.exp = wave_max(fmaxf(ref > kNone ? ceilf(ref - j.ref) + exp : -0x1p30f,
+                                 old.ref > kNone ? ceilf(old.ref - j.ref) + old.exp : -0x1p30f));
+          const float f = factor(ref, exp, j), f0 = factor(old.ref, old.exp, j);
+          sum = sum * exp2_(old.ref - j.ref) +
+                wave_sum(lane < kBatch && i < parts ? all * exp2_(ref - j.ref) : 0.0f);
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) acc[c] *= f0;
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const float fb = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), b));
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) acc[c] += x[b][c] * fb;
+          }
+        }
+        if (WIDE > 1) {
+          __syncthreads();  // (the row before has been read)
+          if (lane == 0) joined[wave][0] = j.ref, joined[wave][1] = j.exp, joined[wave][2] = sum;
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) joined[wave][3 + lane * kPer + c] = acc[c];
+          __syncthreads();
+          if (wave != 0) continue;
+          float top = -0x1p30f;
+#pragma unroll
+          for (int v = 1; v < 4; ++v) j.ref = fmaxf(j.ref, joined[v][0]);
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (joined[v][0] > kNone) top = fmaxf(top, ceilf(joined[v][0] - j.ref) + joined[v][1]);
+          j.exp = top;
+          sum = 0.0f;
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float f = factor(joined[v][0], joined[v][1], j);
+            sum += joined[v][2] * exp2_(joined[v][0] - j.ref);
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) acc[c] += joined[v][3 + lane * kPer + c] * f;
+          }
+        }
+        const int i = (int)((uint32_t)rr / (uint32_t)p.a.G), hq = rr - i * p.a.G;
+        float* out = p.a.out + (((int64_t)(row + i) * p.a.H + h) * p.a.G + hq) * D + lane * kPer;
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) out[c] = finished(acc[c], sum, j.exp);
+      }
     }
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-      const float* x = rec[(int64_t)(i0 + i) * r.stride].acc[rr] + lane * kPer;
-      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) acc[c] += x[c] * fi;
-    }
   }
-  sum = wave_sum(sum);
-  const int i = rr / p.a.G, hq = rr - i * p.a.G;
-  float* out = p.a.out + (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D +
-               lane * kPer;
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) out[c] = finished(acc[c], sum, j.exp);
 }
 
 // ---------------------------------------------------------------- dispatch --
 constexpr int kCu = 256;
 
 struct Plan {
-  int R, parts, least;  // row tiles of 16 R; parts, at most; tokens of a part, at least
+  int R, rows, waves;   // row tiles of 16 R; rows of an item, at most; wavefronts of a workgroup
+  int parts, joins;     // parts, at most; workgroups that join
+  int least;            // tokens of a part, at least
   float target;
   bool cut;
   size_t bytes;
 };
-Plan plan(int64_t n_seqs, int64_t n_rows, int H, int G, int64_t max_pages, int page, int d) {
+Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pages, int page, int d) {
   Plan p{};
   p.R = n_rows * G >= 24 * std::max<int64_t>(1, n_seqs) ? 2 : 1;
   const int64_t room = max_pages * page, tile = 16 * p.R / G;
-  const int64_t items = (n_rows / tile + std::min(n_seqs, n_rows)) * H;
-  const int64_t target = p.R == 2 ? 2 * kCu : d == 256 ? kCu : 2 * kCu;
-  p.least = 512;
-  if (items >= kCu && room <= 4096) p.least = 4096;
+  p.rows = one ? G : (int)tile * G;
+  const int64_t items = (one ? n_rows : n_rows / tile + std::min(n_seqs, n_rows)) * H;
+  p.cut = room > (items >= kCu ? 4096 : 2048);
+  // wavefronts that a compute unit holds at once
+  const int64_t held = 4 * waves_of_simd(p.R, d);
+  // workgroups for each compute unit: parts, or items that are not cut
+  int64_t k = std::min<int64_t>(4, (items + kCu / 2 - 1) / (kCu / 2));
+  // (an item's last part is half empty on the average)
+  int64_t target = std::max(k * kCu - items / 2, items / 2);
+  if (p.R == 2) target = kCu * held / 4;
+  p.waves = p.R == 1 && d == 64 ? 8 : 4;
+  if (p.R == 1)
+    while (p.waves > 2 && (p.cut ? k : (items + kCu - 1) / kCu) * p.waves > held) p.waves /= 2;
+  p.least = !p.cut ? (int)room : items >= kCu ? 2048 : items >= kCu / 2 ? 1024 : 512;
   p.target = (float)target;
-  p.cut = room > p.least;
   p.parts = (int)(items + (p.cut ? target : 0));
-  p.bytes = p.cut ? (size_t)p.parts * 16 * p.R * (d + 3) * 4 : 0;
+  p.joins = std::min(p.parts, p.R == 1 ? 251 : 509);
+  p.bytes = p.cut ? (size_t)p.parts * (state_floats(p.rows, d) * 4 + sizeof(Join)) : 0;
   return p;
 }
 
 template <typename T, int CODES, int D, int R>
 int launch(const Args& p, const Plan& pl, hipStream_t st) {
-  constexpr int W = R == 1 ? 8 : 4;
-  main_kernel<T, CODES, D, R, W><<<pl.parts, 64 * W, 0, st>>>(p);
+  const size_t lds = std::max((size_t)pl.waves * state_floats(pl.rows, D), (size_t)part_lds(pl.waves)) * 4;
+  main_kernel<T, CODES, D, R><<<pl.parts, 64 * pl.waves, lds, st>>>(p);
   int rc = (int)hipGetLastError();
   if (rc != 0 || !pl.cut) return rc;
-  const int rows = std::min(16 * R, p.tile_tokens * p.a.G);
-  merge_kernel<D, R><<<dim3(pl.parts, (rows + 3) / 4), 256, 0, st>>>(p);
+  constexpr int kWide = R == 1 ? 4 : 1;
+  merge_kernel<D, kWide><<<dim3(pl.joins, kWide > 1 ? pl.rows : 1), 256, 0, st>>>(p);
   return (int)hipGetLastError();
 }
 template <typename T, int CODES>
 int launch_d(const Args& p, const Plan& pl, hipStream_t st) {
   switch (p.a.d) {
-    case 64: return pl.R == 1 ? launch<T, CODES, 64, 1>(p, pl, st) : launch<T, CODES, 64, 2>(p, pl, st);
+    case 64:
+      return pl.R == 1 ? launch<T, CODES, 64, 1>(p, pl, st) : launch<T, CODES, 64, 2>(p, pl, st);
     case 128: return pl.R == 1 ? launch<T, CODES, 128, 1>(p, pl, st) : launch<T, CODES, 128, 2>(p, pl, st);
     default: return pl.R == 1 ? launch<T, CODES, 256, 1>(p, pl, st) : launch<T, CODES, 256, 2>(p, pl, st);
   }
@@ -676,14 +811,19 @@ int launch_codes(const Args& p, const Plan& pl, hipStream_t st) {
 
 size_t page_attn_workspace_bytes(int64_t n_seqs, int64_t n_rows, int H, int G, int64_t max_pages,
                                  int page, int d) {
-  return pa::plan(n_seqs, n_rows, H, G, max_pages, page, d).bytes;
+  // (as many as the call needs with starts or without)
+  size_t most = pa::plan(n_seqs, n_rows, false, H, G, max_pages, page, d).bytes;
+  if (n_seqs == n_rows)
+    most = std::max(most, pa::plan(n_seqs, n_rows, true, H, G, max_pages, page, d).bytes);
+  return most;
 }
 
 int launch_page_attn(const PageAttn& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const pa::Plan pl = pa::plan(a.n_seqs, a.n_rows, a.H, a.G, a.max_pages, a.page, a.d);
+  const pa::Plan pl = pa::plan(a.n_seqs, a.n_rows, !a.starts, a.H, a.G, a.max_pages, a.page, a.d);
   const pa::Args p{a,        16 * pl.R / a.G, __builtin_ctz(a.page),
-                   pl.least, pl.target,       a.scale * 1.44269504088896341f};
+                   pl.least, pl.target,       a.scale * 1.44269504088896341f,
+                   pl.rows,  pl.cut,          pl.parts};
   switch (a.q_dtype) {
     case FIBQ_F32: return pa::launch_codes<float>(p, pl, st);
     case FIBQ_F16: return pa::launch_codes<f16_t>(p, pl, st);
