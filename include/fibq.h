@@ -446,7 +446,7 @@ size_t fibq_page_resize_workspace_bytes(int64_t n_seqs);
  * A slot is a row of a cache of n_pages * page rows; fibq_decode takes slots as
  * token_ids.  new_lens may be lens, and new_free n_free; outputs overlap nothing
  * otherwise.  lens, grow, table and free_pages are not written by others while
- * the call runs.  1 <= page <= 65536 here; free_cap < 2^31, n_rows < 2^31. */
+ * the call runs.  1 <= page <= 65536 here; free_cap < 2^30, n_rows < 2^31. */
 int fibq_page_resize(int32_t* table, const int32_t* lens, const int32_t* grow, int64_t n_seqs,
                      int64_t max_pages, int page, int64_t n_pages, int32_t* free_pages,
                      int64_t free_cap, const int32_t* n_free, int64_t n_rows, int32_t* new_lens,

@@ -554,7 +554,7 @@ int fibq_page_resize(int32_t* table, const int32_t* lens, const int32_t* grow, i
                      void* workspace, size_t workspace_bytes, void* stream) {
   if (n_seqs < 0 || n_seqs > 65535 || page < 1 || page > 65536 || max_pages < 0 ||
       max_pages >= (1LL << 30) || max_pages * page >= (1LL << 30) || n_pages < 0 ||
-      n_pages >= (1LL << 31) || free_cap < 0 || free_cap >= (1LL << 31) || n_rows < 0 ||
+      n_pages >= (1LL << 31) || free_cap < 0 || free_cap >= (1LL << 30) || n_rows < 0 ||
       n_rows >= (1LL << 31))
     return FIBQ_EINVAL;
   if (!n_free || !starts || !new_free) return FIBQ_EINVAL;

@@ -61,48 +61,65 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
     turn[i] = make_float2(cs * a.scale, (a.inverse ? -sn : sn) * a.scale);
   }
   __syncthreads();
+  // A thread has one piece of V elements of every head that it visits, so a row's angles
+  // stay in its registers; kHeads loads are on their way at once.
+  constexpr int kHeads = HALF ? 2 : 4;
   const int heads = a.q_heads + a.k_heads;
   const int turned = HALF ? half / V : a.rot / V;
   const int per_head = turned + (a.d - a.rot) / V;  // (rows are copied behind the turned part)
-  const int items = rows * heads * per_head;
-  for (int i = tid; i < items; i += kRopeThreads) {
-    const int h = i / per_head, c = i - h * per_head;
-    const int r = h / heads, head = h - r * heads;
-    const bool is_k = head >= a.q_heads;
-    const int64_t row = row0 + r;
-    const T* x = is_k ? (const T*)a.k + row * a.k_row + (head - a.q_heads) * a.k_head
-                      : (const T*)a.q + row * a.q_row + head * a.q_head;
-    T* y = is_k ? (T*)a.k_out + row * a.ko_row + (head - a.q_heads) * a.ko_head
-                : (T*)a.q_out + row * a.qo_row + head * a.qo_head;
-    const float2* t = turn + r * half;
-    if (c >= turned) {
-      const int at = a.rot + (c - turned) * V;
-      store<T, V>(y + at, load<T, V>(x + at));
-    } else if (HALF) {
-      const int at = c * V;
-      const Vec<T, V> x0 = load<T, V>(x + at), x1 = load<T, V>(x + at + half);
-      Vec<T, V> y0, y1;
+  for (int c0 = 0; c0 < per_head; c0 += kRopeThreads) {
+    const int pieces = min(per_head - c0, kRopeThreads), at_once = kRopeThreads / pieces;
+    const int slot = tid / pieces, c = c0 + tid - slot * pieces;
+    if (slot >= at_once) continue;
+    const bool turns = c < turned;
+    const int at = turns ? c * V : a.rot + (c - turned) * V;
+    for (int r = 0; r < rows; ++r) {
+      constexpr int kAngles = HALF ? V : V / 2;
+      float2 w[kAngles];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float2 w = t[at + e];
-        const float u = from(x0.e[e]), v = from(x1.e[e]);
-        y0.e[e] = (T)(u * w.x - v * w.y);
-        y1.e[e] = (T)(v * w.x + u * w.y);
-      }
-      store<T, V>(y + at, y0);
-      store<T, V>(y + at + half, y1);
-    } else {
-      const int at = c * V;
-      const Vec<T, V> x0 = load<T, V>(x + at);
-      Vec<T, V> y0;
+      for (int e = 0; e < kAngles; ++e)
+        w[e] = turns ? turn[r * half + (HALF ? at : at / 2) + e] : make_float2(1.0f, 0.0f);
+      const int64_t row = row0 + r;
+      const T *q = (const T*)a.q + row * a.q_row, *k = (const T*)a.k + row * a.k_row;
+      T *qo = (T*)a.q_out + row * a.qo_row, *ko = (T*)a.k_out + row * a.ko_row;
+      for (int h0 = slot; h0 < heads; h0 += kHeads * at_once) {
+        Vec<T, V> x0[kHeads], x1[HALF ? kHeads : 1];
 #pragma unroll
-      for (int e = 0; e < V; e += 2) {
-        const float2 w = t[(at + e) / 2];
-        const float u = from(x0.e[e]), v = from(x0.e[e + 1]);
-        y0.e[e] = (T)(u * w.x - v * w.y);
-        y0.e[e + 1] = (T)(v * w.x + u * w.y);
+        for (int u = 0; u < kHeads; ++u) {
+          const int h = min(h0 + u * at_once, heads - 1);
+          const T* x = (h < a.q_heads ? q + h * a.q_head : k + (h - a.q_heads) * a.k_head) + at;
+          x0[u] = load<T, V>(x);
+          if constexpr (HALF) x1[u] = turns ? load<T, V>(x + half) : x0[u];
+        }
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u) {
+          const int h = h0 + u * at_once;
+          if (h >= heads) break;
+          T* y = (h < a.q_heads ? qo + h * a.qo_head : ko + (h - a.q_heads) * a.ko_head) + at;
+          if (!turns) {
+            store<T, V>(y, x0[u]);
+          } else if constexpr (HALF) {
+            Vec<T, V> y0, y1;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const float p = from(x0[u].e[e]), q2 = from(x1[u].e[e]);
+              y0.e[e] = (T)(p * w[e].x - q2 * w[e].y);
+              y1.e[e] = (T)(q2 * w[e].x + p * w[e].y);
+            }
+            store<T, V>(y, y0);
+            store<T, V>(y + half, y1);
+          } else {
+            Vec<T, V> y0;
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+              const float p = from(x0[u].e[e]), q2 = from(x0[u].e[e + 1]);
+              y0.e[e] = (T)(p * w[e / 2].x - q2 * w[e / 2].y);
+              y0.e[e + 1] = (T)(q2 * w[e / 2].x + p * w[e / 2].y);
+            }
+            store<T, V>(y, y0);
+          }
+        }
       }
-      store<T, V>(y + at, y0);
     }
   }
 }
@@ -129,54 +146,69 @@ int rope_typed(const Rope& a, hipStream_t st) {
 }
 
 // ------------------------------------------------------------ page_resize --
-// Three prefix sums over the requests: rows, pages given back, pages taken.
-// One workgroup runs them; the places of the pages given back come first,
-// since what it may hand out depends on their number.
+// Three prefix sums over the requests: rows, pages given back, pages taken.  One
+// workgroup runs them; pages given back are placed first, since what it may hand out
+// depends on their number.  Sums stop at 2^31 - 1, which is more than any bound here.
 constexpr int kScan = 1024;
+constexpr int kStaged = 4096;  // requests whose results stay in LDS for the rows' search
 
-struct Sums {
-  int64_t v;  // inclusive prefix of this thread's value
-  int64_t total;
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
+
+struct Sum {
+  uint32_t upto, all;  // of the threads up to and with this one, of all threads
 };
-__device__ __forceinline__ Sums scan(int64_t v, int64_t* wave_sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t x = v;
+// `lds`: kScan / 64 words that no other sum of the same round uses
+__device__ __forceinline__ uint32_t scan_wave(uint32_t v, uint32_t* lds) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
+    const uint32_t y = __shfl_up(v, o, 64);
+    if (lane >= o) v = plus(v, y);
   }
-  __syncthreads();  // (the sums of the call before have been read)
-  if (lane == 63) wave_sums[wave] = x;
-  __syncthreads();
-  int64_t before = 0, total = 0;
+  if (lane == 63) lds[threadIdx.x >> 6] = v;
+  return v;
+}
+__device__ __forceinline__ Sum scan_all(uint32_t v, const uint32_t* lds) {
+  const int wave = threadIdx.x >> 6;
+  Sum s{v, 0};
 #pragma unroll
   for (int w = 0; w < kScan / 64; ++w) {
-    const int64_t s = wave_sums[w];
-    before += w < wave ? s : 0;
-    total += s;
+    if (w < wave) s.upto = plus(s.upto, lds[w]);
+    s.all = plus(s.all, lds[w]);
   }
-  return {x + before, total};
-}
-__device__ __forceinline__ int64_t pages_of(int64_t tokens, int page) {
-  return (tokens + page - 1) / page;
+  return s;
 }
 
 struct Request {
-  int64_t len, after, rows;
+  int len, grow, have, want;  // pages; both 0 if the request is not well-formed
+  uint32_t ends;              // rows of all requests up to and with it
   bool good;
 };
-// request g; `ends`: the rows of all requests up to and with it
-__device__ __forceinline__ Request request(const Resize& a, int64_t g, int64_t len, int64_t grow,
-                                           int64_t ends) {
-  const int64_t room = a.max_pages * a.page;
-  Request r{len, len + grow, grow > 0 ? grow : 0, false};
-  r.good = len >= 0 && len <= room && r.after >= 0 && r.after <= room && ends <= a.n_rows;
+__device__ __forceinline__ uint32_t pages_of(uint32_t tokens, uint32_t page) {
+  return (tokens + page - 1) / page;
+}
+__device__ __forceinline__ Request request(const Resize& a, int64_t g, uint32_t rows_before,
+                                           uint32_t* lds, uint32_t* all) {
+  const bool live = g < a.n;
+  Request r{live ? a.lens[g] : -1, live ? a.grow[g] : 0, 0, 0, 0, false};
+  const uint32_t rows = r.grow > 0 ? (uint32_t)r.grow : 0;
+  const uint32_t v = scan_wave(rows, lds);
+  __syncthreads();
+  const Sum s = scan_all(v, lds);
+  r.ends = plus(rows_before, s.upto);
+  *all = s.all;
+  const int64_t room = a.max_pages * a.page, after = (int64_t)r.len + r.grow;
+  r.good = r.len >= 0 && r.len <= room && after >= 0 && after <= room && (int64_t)r.ends <= a.n_rows;
+  if (r.good) {
+    r.have = (int)pages_of((uint32_t)r.len, (uint32_t)a.page);
+    r.want = (int)pages_of((uint32_t)after, (uint32_t)a.page);
+  }
   return r;
 }
 
-// A row's slot and position.  starts, new_lens and top are the scan's.
-__device__ __forceinline__ void place_row(const Resize& a, int64_t r, const int32_t* starts) {
+// A row's slot and position from the scan's results.
+__device__ __forceinline__ void place_row(const Resize& a, int r, const int32_t* starts,
+                                          const int32_t* new_lens, const int32_t* top) {
   int64_t slot = -1;
   int32_t position = -1;
   int lo = 0, hi = (int)a.n;  // the first request whose rows end behind r
@@ -188,20 +220,22 @@ __device__ __forceinline__ void place_row(const Resize& a, int64_t r, const int3
       lo = mid + 1;
   }
   if (lo < a.n) {
-    const int64_t after = a.new_lens[lo];
+    const int after = new_lens[lo];
     if (after >= 0) {
-      const int64_t rows = starts[lo + 1] - starts[lo], at = after - (starts[lo + 1] - r);
-      const int64_t have = pages_of(after - rows, a.page), p = at / a.page;
+      const int rows = starts[lo + 1] - starts[lo], at = after - (starts[lo + 1] - r);
+      const uint32_t page = (uint32_t)a.page;
+      const int have = (int)pages_of((uint32_t)(after - rows), page), p = (int)((uint32_t)at / page);
+      const int in = at - p * a.page;
       int32_t* cell = a.table + (int64_t)lo * a.max_pages + p;
       int32_t id;
       if (p < have) {
         id = *cell;
       } else {
-        id = a.free_pages[a.top[lo] - (p - have)];
-        if (at % a.page == 0) *cell = id;
+        id = a.free_pages[top[lo] - (p - have)];
+        if (in == 0) *cell = id;
       }
-      if (id >= 0 && id < a.n_pages) slot = (int64_t)id * a.page + at % a.page;
-      position = (int32_t)at;
+      if (id >= 0 && id < a.n_pages) slot = (int64_t)id * a.page + in;
+      position = at;
     }
   }
   a.slots[r] = slot;
@@ -209,75 +243,100 @@ __device__ __forceinline__ void place_row(const Resize& a, int64_t r, const int3
 }
 
 __global__ __launch_bounds__(kScan) void resize_kernel(Resize a, int place) {
-  __shared__ int64_t wave_sums[kScan / 64];
+  constexpr int kW = kScan / 64;
+  __shared__ uint32_t sums[3][kW];
+  __shared__ int taken_most;
+  extern __shared__ int32_t staged[];  // starts, new lengths, tops (if rows are placed here)
+  int32_t *l_starts = staged, *l_lens = staged + a.n + 1, *l_top = l_lens + a.n;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int64_t cap = a.free_cap;
-  const int64_t free0 = min(max((int64_t)*a.n_free, (int64_t)0), cap);
+  const uint32_t cap = (uint32_t)a.free_cap;
+  const uint32_t free0 = min((uint32_t)max(*a.n_free, 0), cap);
+  if (tid == 0) taken_most = 0;
+  Request r{};
+  Sum back{}, need{};
+  uint32_t rows_before = 0, back_before = 0;
   // pages given back, onto the stack in order
-  int64_t rows0 = 0, back0 = 0;
   for (int64_t g0 = 0; g0 < a.n; g0 += kScan) {
-    const int64_t g = g0 + tid;
-    const bool live = g < a.n;
-    const int64_t len = live ? a.lens[g] : 0, grow = live ? a.grow[g] : 0;
-    const Sums rows = scan(grow > 0 ? grow : 0, wave_sums);
-    const Request r = request(a, g, len, grow, rows0 + rows.v);
-    const int64_t want = r.good ? pages_of(r.after, a.page) : 0;
-    const int64_t back = r.good ? max(pages_of(r.len, a.page) - want, (int64_t)0) : 0;
-    const Sums backs = scan(back, wave_sums);
-    const int64_t to = free0 + back0 + backs.v - back;
-    for (uint64_t todo = __ballot(back > 0); todo; todo &= todo - 1) {
+    uint32_t rows;
+    r = request(a, g0 + tid, rows_before, sums[0], &rows);
+    const uint32_t b = (uint32_t)max(r.have - r.want, 0), n = (uint32_t)max(r.want - r.have, 0);
+    const uint32_t vb = scan_wave(b, sums[1]), vn = scan_wave(n, sums[2]);
+    __syncthreads();
+    back = scan_all(vb, sums[1]);
+    need = scan_all(vn, sums[2]);
+    const uint32_t to = plus(plus(free0, back_before), back.upto - b);
+    for (uint64_t todo = __ballot(b > 0); todo; todo &= todo - 1) {
       const int l = __ffsll((unsigned long long)todo) - 1;  // a lane's pages, by all lanes
-      const int64_t n = __shfl(back, l, 64), at = __shfl(to, l, 64);
-      const int32_t* from = a.table + (g0 + (tid & ~63) + l) * a.max_pages + __shfl(want, l, 64);
-      for (int64_t i = lane; i < n && at + i < cap; i += 64) a.free_pages[at + i] = from[i];
+      const uint32_t m = __shfl(b, l, 64), at = __shfl(to, l, 64);
+      const int32_t* from =
+          a.table + (g0 + (tid & ~63) + l) * a.max_pages + __shfl(r.want, l, 64);
+      for (uint32_t i = lane; i < m && at + i < cap; i += 64) a.free_pages[at + i] = from[i];
     }
-    rows0 += rows.total;
-    back0 += backs.total;
+    rows_before = plus(rows_before, rows);
+    back_before = plus(back_before, back.all);
   }
-  const int64_t free1 = min(free0 + back0, cap);
+  const uint32_t free1 = min(plus(free0, back_before), cap);
   // pages taken from its top, first come, first served
-  int64_t need0 = 0, taken = 0;
-  rows0 = 0;
+  uint32_t need_before = 0;
+  rows_before = 0;
+  int taken = 0;
   for (int64_t g0 = 0; g0 < a.n; g0 += kScan) {
-    const int64_t g = g0 + tid;
-    const bool live = g < a.n;
-    const int64_t len = live ? a.lens[g] : 0, grow = live ? a.grow[g] : 0;
-    const Sums rows = scan(grow > 0 ? grow : 0, wave_sums);
-    const Request r = request(a, g, len, grow, rows0 + rows.v);
-    const int64_t need =
-        r.good ? max(pages_of(r.after, a.page) - pages_of(r.len, a.page), (int64_t)0) : 0;
-    const Sums needs = scan(need, wave_sums);
-    const int64_t upto = need0 + needs.v;
-    const bool granted = r.good && (need == 0 || upto <= free1);
-    if (granted && need > 0) taken = upto;
-    if (live) {
-      a.new_lens[g] = granted ? (int32_t)r.after : -1;
-      a.starts[g + 1] = (int32_t)min(rows0 + rows.v, a.n_rows);
-      a.top[g] = granted ? (int32_t)(free1 - 1 - (upto - need)) : 0;
+    uint32_t rows = 0;
+    if (a.n > kScan) {  // (else as computed above)
+      __syncthreads();
+      r = request(a, g0 + tid, rows_before, sums[0], &rows);
+      const uint32_t vn = scan_wave((uint32_t)max(r.want - r.have, 0), sums[2]);
+      __syncthreads();
+      need = scan_all(vn, sums[2]);
     }
-    rows0 += rows.total;
-    need0 += needs.total;
+    const int64_t g = g0 + tid;
+    const uint32_t upto = plus(need_before, need.upto);
+    const int mine = max(r.want - r.have, 0);
+    const bool granted = r.good && (mine == 0 || upto <= free1);
+    if (granted && mine > 0) taken = (int)upto;
+    if (g < a.n) {
+      const int after = granted ? r.len + r.grow : -1;
+      const int end = (int)min((int64_t)r.ends, a.n_rows);
+      const int top = granted ? (int)(free1 - 1 - (upto - (uint32_t)mine)) : 0;
+      a.new_lens[g] = after;
+      a.starts[g + 1] = end;
+      if (place) {
+        l_starts[g + 1] = end;
+        l_lens[g] = after;
+        l_top[g] = top;
+      } else {
+        a.top[g] = top;
+      }
+    }
+    rows_before = plus(rows_before, rows);
+    need_before = plus(need_before, need.all);
   }
   // (granted requests that need pages are the first of those that do)
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) taken = max(taken, __shfl_xor(taken, o, 64));
-  __syncthreads();
-  if (lane == 0) wave_sums[tid >> 6] = taken;
-  __syncthreads();
+  __syncthreads();  // (taken_most is set, and pages given back are on the stack)
+  if (lane == 0 && taken > 0) atomicMax(&taken_most, taken);
   if (tid == 0) {
-    for (int w = 0; w < kScan / 64; ++w) taken = max(taken, wave_sums[w]);
     a.starts[0] = 0;
-    *a.new_free = (int32_t)(free1 - taken);
+    if (place) l_starts[0] = 0;
   }
-  if (!place) return;
   __threadfence_block();
   __syncthreads();
-  for (int64_t r = tid; r < a.n_rows; r += kScan) place_row(a, r, a.starts);
+  if (tid == 0) *a.new_free = (int)free1 - taken_most;
+  if (!place) return;
+  for (int q = tid; q < (int)a.n_rows; q += kScan) place_row(a, q, l_starts, l_lens, l_top);
 }
 
-__global__ __launch_bounds__(256) void place_kernel(Resize a) {
-  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (r < a.n_rows) place_row(a, r, a.starts);
+__global__ __launch_bounds__(256) void place_kernel(Resize a, int stage) {
+  extern __shared__ int32_t staged[];
+  const int32_t* starts = a.starts;
+  if (stage) {  // (the search's dozen reads from LDS)
+    for (int i = threadIdx.x; i <= (int)a.n; i += 256) staged[i] = a.starts[i];
+    __syncthreads();
+    starts = staged;
+  }
+  for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.n_rows; r += 256 * (int64_t)gridDim.x)
+    place_row(a, (int)r, starts, a.new_lens, a.top);
 }
 
 // ----------------------------------------------------------- cache8_write --
@@ -298,15 +357,15 @@ __device__ __forceinline__ float least_scale(uint32_t amax_bits, int codes) {
   return ldexpf(1.0f, max(e, -126));
 }
 
-struct Quotient {  // x / s, by the exact reciprocal where s is a power of two
+// x / s rounded to float: the remainder of x r corrects it once, r = 1 / s rounded
+// (Markstein's theorem; x r itself is exact where s is a power of two).
+struct Quotient {
   float s, r;
-  bool exact;
-  __device__ __forceinline__ explicit Quotient(float s_) : s(s_) {
-    const uint32_t u = __float_as_uint(s_);
-    exact = (u & 0x807fffffu) == 0 && u >= 0x00800000u && u < 0x7f000000u;
-    r = exact ? 1.0f / s_ : 0.0f;
+  __device__ __forceinline__ explicit Quotient(float s_) : s(s_), r(1.0f / s_) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    const float q = x * r;
+    return copysignf(__builtin_fmaf(__builtin_fmaf(-q, s, x), r, q), q);  // (of -0 as well)
   }
-  __device__ __forceinline__ float operator()(float x) const { return exact ? x * r : x / s; }
 };
 __device__ __forceinline__ uint32_t code4(const float* x, int codes) {
   uint32_t w = 0;
@@ -331,13 +390,10 @@ __device__ __forceinline__ void value4(uint32_t w, int codes, float* x) {
   }
 }
 
-__device__ __forceinline__ bool joins(const Write& a, int64_t before, int64_t s) {
-  return before >= 0 && s > before && s / a.page == before / a.page;
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void write_kernel(Write a, int chunk) {
-  constexpr int V = 8;
+// Rows of a run are read once, into registers, where they fit (kHeld pieces a thread).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void write_kernel(Write a, int shift, int chunk) {
+  constexpr int V = 8, kRow = D / V, kHeld = 4;
   __shared__ uint32_t wave_max[4];
   const int tid = threadIdx.x, lane = tid & 63, n_threads = blockDim.x;
   const int h = blockIdx.y;
@@ -346,31 +402,65 @@ __global__ __launch_bounds__(256) void write_kernel(Write a, int chunk) {
   const int64_t x_row = is_v ? a.v_row : a.k_row;
   uint8_t* pages = (uint8_t*)(is_v ? a.v_pages : a.k_pages);
   float* scales = is_v ? a.v_scales : a.k_scales;
-  const int64_t base = (int64_t)blockIdx.x * chunk, limit = a.n_pages * a.page;
-  auto slot = [&](int64_t r) -> int64_t {
-    if (r < 0 || r >= a.n_rows) return -1;
-    const int64_t s = a.slots[r];
-    return s >= 0 && s < limit ? s : -1;
-  };
-  const int64_t mine = lane < chunk ? slot(base + lane) : -1;
-  const bool begins = mine >= 0 && !joins(a, slot(base + lane - 1), mine);
-  const int per_row = a.d / V;
-  for (uint64_t todo = __ballot(begins); todo; todo &= todo - 1) {
+  const int64_t base = (int64_t)blockIdx.x * chunk, limit = a.n_pages << shift;
+  // Slots of the chunk's rows and of those that a run may go on over, the row before
+  // the chunk first: lane l of word w has row base - 1 + 63 w + l.
+  constexpr int kWords = 4;
+  int64_t slot[kWords];
+  uint64_t joins[kWords], known[kWords];  // bit l: of lane l; a row joins the one before it
+#pragma unroll
+  for (int w = 0; w < kWords; ++w) {
+    const int64_t r = base - 1 + 63 * w + lane;
+    const bool used = 63 * w < chunk + (1 << shift);
+    const int64_t s = used && r >= 0 && r < a.n_rows ? a.slots[r] : -1;
+    slot[w] = s >= 0 && s < limit ? s : -1;
+  }
+#pragma unroll
+  for (int w = 0; w < kWords; ++w) {
+    const int64_t before = __shfl_up(slot[w], 1, 64);
+    known[w] = __ballot(slot[w] >= 0);
+    joins[w] = __ballot(lane > 0 && before >= 0 && slot[w] > before &&
+                        slot[w] >> shift == before >> shift);
+  }
+  // (lane 63 of a word is lane 0 of the next, so bits 1 .. 63 are 63 rows a word)
+  for (uint64_t todo = known[0] & ~joins[0] & (chunk < 63 ? (2ull << chunk) - 2 : ~1ull); todo;
+       todo &= todo - 1) {
     const int l = __ffsll((unsigned long long)todo) - 1;
-    const int64_t r0 = base + l, s0 = __shfl(mine, l, 64);
+    const int64_t r0 = base - 1 + l, s0 = __shfl(slot[0], l, 64);
     int rows = 1;  // of the run: at most a page's, since its slots increase
-    for (bool more = true; more;) {
-      const int64_t r = r0 + rows + lane, s = slot(r);
-      const uint64_t ends = ~__ballot(s >= 0 && joins(a, slot(r - 1), s));
-      rows += ends ? __ffsll((unsigned long long)ends) - 1 : 64;
-      more = ends == 0;
+    int64_t s1 = s0;
+    {
+      int w = 0, at = l;
+#pragma unroll
+      for (int u = 0; u < kWords; ++u) {
+        if (u != w) continue;
+        const uint64_t on = at < 63 ? joins[u] >> (at + 1) : 0;  // bits of the rows behind
+        const int most = 63 - at, n = min(most, ~on ? __ffsll((unsigned long long)~on) - 1 : 64);
+        rows += n;
+        s1 = __shfl(slot[u], at + n, 64);
+        if (n == most) w = u + 1, at = 0;
+      }
     }
-    const int64_t p = s0 / a.page;
-    const int first = (int)(s0 - p * a.page);
+    const int64_t p = s0 >> shift;
+    const int first = (int)(s0 - (p << shift));
+    const bool dense = s1 - s0 == rows - 1;
+    const int pieces = rows * kRow;
+    const T* x0 = x + r0 * x_row;
+    float* scale = scales + p * a.H + h;
+    const float old = first ? *scale : 0.0f;
+    Vec<T, V> held[kHeld];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      const int i = min(tid + u * n_threads, pieces - 1);
+      held[u] = load<T, V>(x0 + (i / kRow) * x_row + i % kRow * V);
+    }
     uint32_t top = 0;
-    for (int i = tid; i < rows * per_row; i += n_threads) {
-      const int r = i / per_row;
-      const Vec<T, V> y = load<T, V>(x + (r0 + r) * x_row + (i - r * per_row) * V);
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(from(held[u].e[e])) & 0x7fffffffu);
+    for (int i = tid + kHeld * n_threads; i < pieces; i += n_threads) {
+      const Vec<T, V> y = load<T, V>(x0 + (i / kRow) * x_row + i % kRow * V);
 #pragma unroll
       for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(from(y.e[e])) & 0x7fffffffu);
     }
@@ -382,14 +472,13 @@ __global__ __launch_bounds__(256) void write_kernel(Write a, int chunk) {
       __syncthreads();
       for (int w = 0; w < n_threads / 64; ++w) top = max(top, wave_max[w]);
     }
-    float* scale = scales + p * a.H + h;
-    const float old = first ? *scale : 0.0f, least = least_scale(top, a.codes);
+    const float least = least_scale(top, a.codes);
     const bool lost = old != old || least != least;
     const float s = lost ? __uint_as_float(0x7fc00000u) : fmaxf(old, least);
-    uint8_t* page = pages + (p * a.H + h) * (int64_t)a.page * a.d;
+    uint8_t* page = pages + ((p * a.H + h) << shift) * D;
     const Quotient over(s);
     if (s > old)  // (not if s is no number)
-      for (int i = tid; i < first * per_row; i += n_threads) {
+      for (int i = tid; i < first * kRow; i += n_threads) {
         uint32_t w[2];
         __builtin_memcpy(w, page + i * V, 8);
 #pragma unroll
@@ -402,9 +491,7 @@ __global__ __launch_bounds__(256) void write_kernel(Write a, int chunk) {
         }
         __builtin_memcpy(page + i * V, w, 8);
       }
-    for (int i = tid; i < rows * per_row; i += n_threads) {
-      const int r = i / per_row, at = (i - r * per_row) * V;
-      const Vec<T, V> y = load<T, V>(x + (r0 + r) * x_row + at);
+    auto put = [&](int i, const Vec<T, V>& y) {
       uint32_t w[2] = {0, 0};
       if (s > 0.0f) {  // (codes 0 where the scale is 0 or no number)
 #pragma unroll
@@ -415,9 +502,15 @@ __global__ __launch_bounds__(256) void write_kernel(Write a, int chunk) {
           w[u] = code4(z, a.codes);
         }
       }
-      const int64_t to = a.slots[r0 + r] - p * a.page;
-      __builtin_memcpy(page + to * a.d + at, w, 8);
-    }
+      const int r = i / kRow;
+      const int to = dense ? first + r : (int)(a.slots[r0 + r] - (p << shift));
+      __builtin_memcpy(page + to * D + i % kRow * V, w, 8);
+    };
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+      if (tid + u * n_threads < pieces) put(tid + u * n_threads, held[u]);
+    for (int i = tid + kHeld * n_threads; i < pieces; i += n_threads)
+      put(i, load<T, V>(x0 + (i / kRow) * x_row + i % kRow * V));
     if (n_threads > 64) __syncthreads();  // every thread has read the old scale
     if (tid == 0) *scale = s;
   }
@@ -425,10 +518,17 @@ __global__ __launch_bounds__(256) void write_kernel(Write a, int chunk) {
 
 template <typename T>
 int write_typed(const Write& a, hipStream_t st) {
-  int chunk = (int)std::min<int64_t>(std::min(a.page, 64),
-                                     std::max<int64_t>(1, a.n_rows * a.H * 2 / 4096));
+  // few rows: a workgroup of one wavefront each; else those of about a page
+  const int chunk = (int)std::min<int64_t>(std::min(a.page, 63),
+                                           std::max<int64_t>(1, a.n_rows * a.H * 2 / 4096));
   const int64_t x = (a.n_rows + chunk - 1) / chunk;
-  write_kernel<T><<<dim3((unsigned)x, a.H, 2), chunk == 1 ? 64 : 256, 0, st>>>(a, chunk);
+  const dim3 grid((unsigned)x, a.H, 2);
+  const int threads = chunk == 1 ? 64 : 256, shift = __builtin_ctz(a.page);
+  switch (a.d) {
+    case 64: write_kernel<T, 64><<<grid, threads, 0, st>>>(a, shift, chunk); break;
+    case 128: write_kernel<T, 128><<<grid, threads, 0, st>>>(a, shift, chunk); break;
+    default: write_kernel<T, 256><<<grid, threads, 0, st>>>(a, shift, chunk); break;
+  }
   return (int)hipGetLastError();
 }
 
@@ -445,14 +545,16 @@ int launch_rope(const Rope& a, void* stream) {
 
 size_t resize_workspace_bytes(int64_t n) { return (size_t)n * 4; }
 
-// Up to 4096 rows the scan's workgroup places them as well.
+// Up to 4096 rows of as many requests the scan's workgroup places them as well.
 int launch_resize(const Resize& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool one = a.n_rows <= 4096;
-  pg::resize_kernel<<<1, pg::kScan, 0, st>>>(a, one);
+  const bool one = a.n_rows <= 4096 && a.n <= pg::kStaged;
+  pg::resize_kernel<<<1, pg::kScan, one ? (3 * a.n + 1) * 4 : 0, st>>>(a, one);
   int rc = (int)hipGetLastError();
-  if (rc != 0 || one) return rc;
-  pg::place_kernel<<<(unsigned)((a.n_rows + 255) / 256), 256, 0, st>>>(a);
+  if (rc != 0 || one || a.n_rows == 0) return rc;
+  const bool stage = a.n < pg::kStaged;
+  const int64_t grid = std::min<int64_t>((a.n_rows + 255) / 256, 4096);
+  pg::place_kernel<<<(unsigned)grid, 256, stage ? (a.n + 1) * 4 : 0, st>>>(a, stage);
   return (int)hipGetLastError();
 }
 
