@@ -41,6 +41,7 @@ constexpr float kLag = 0x1p8f;      // exp2 of what a score may exceed its row's
 constexpr float kTop = 0x1p15f;     // weights stay below (binary16)
 constexpr int kTopBits = 7;         // exponent of a row's largest weight when e is set
 constexpr float kLimit = 0x1p94f;   // of a score's factors: scores stay below 2^126, codes' products being below 2^32
+constexpr float kMost = 0x1p126f;   // of a weight's factor: never infinite, so that 0 stays 0
 constexpr float kNone = -0x1p127f;  // reference of a row that has seen nothing
 
 struct Args {
@@ -223,6 +224,16 @@ __device__ __forceinline__ h8 halves<FIBQ_INT8>(uint32_t lo, uint32_t hi) {
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// w less half HALF of x, in one instruction (exact: the half is w rounded)
+template <int HALF>
+__device__ __forceinline__ float rest(h2 x, float w) {
+  float r;
+  if constexpr (HALF == 0)
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(x), "v"(w));
+  else
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(x), "v"(w));
+  return r;
+}
 __device__ __forceinline__ float limited(float x) {
   return __builtin_amdgcn_fmed3f(x, -kLimit, kLimit);
 }
@@ -235,7 +246,10 @@ struct Wave {
   static constexpr int KJ = D / 64;                  // 16-byte pieces of a lane's K row
   static constexpr int CB = D / 16;                  // bytes of a lane's V row
 
-  h8 q[R][2 * KJ][QP];
+  static constexpr bool kShared = R > 1;             // queries in LDS, for all wavefronts
+
+  h8 q[kShared ? 1 : R][2 * KJ][QP];
+  const h8* lq;                  // [R][2 KJ][QP][64]
   int qe[R];                     // a row's queries are q 2^qe
   int vis[R];                    // tokens that a row sees
   float ref[R], sum[R], top[R];  // top: largest weight so far, in units of 2^e
@@ -311,60 +325,116 @@ struct Wave {
                          CB);
   }
 
-  // The part's first loads, each as soon as its address is known, then its queries.
-  __device__ __forceinline__ void begin(const Part& r, int from, int to) {
+  // Row rr's queries, and its tokens' number if it is none of the item's.
+  __device__ __forceinline__ const T* row_of(const Part& r, int rr, int* i) const {
     const PageAttn& a = p.a;
+    const bool used = rr < r.n_tokens * a.G;
+    *i = used ? (int)((uint32_t)rr / (uint32_t)a.G) : 0;
+    const int hq = used ? rr - *i * a.G : 0;
+    return (const T*)a.q + (((int64_t)(r.s.begin + r.i0 + *i) * a.H + r.h) * a.G + hq) * D;
+  }
+  // x 2^-e in QP binary16 parts
+  __device__ __forceinline__ void parts_of(const T* y, bool used, int e, h8* to, int stride) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float z = used ? ldexpf(to_float(y[i]), -e) : 0.0f;
+      to[0][i] = (_Float16)z;
+      if constexpr (QP == 2) to[stride][i] = (_Float16)(z - (float)to[0][i]);
+    }
+  }
+  __device__ __forceinline__ void look(const T* y, float* big, int* lost_) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float z = fabsf(to_float(y[i]));
+      *lost_ |= !(z < INFINITY);
+      *big = fmaxf(*big, z);
+    }
+  }
+  // the largest is in [2^14, 2^15) then
+  __device__ __forceinline__ int exponent(float big, int lost_) const {
+    return (big > 0.0f && !lost_ ? __builtin_amdgcn_frexp_expf(big) : 0) - 15;
+  }
+
+  // Queries of the item into LDS as the operand that each lane takes, 8 threads to a row.
+  // Behind them the rows' exponents and whether they are no numbers.
+  __device__ __forceinline__ void share_queries(const Part& r, h8* to) {
+    for (int rr = threadIdx.x >> 3; rr < 16 * R; rr += blockDim.x >> 3) share_row(r, rr, to);
+  }
+  __device__ __forceinline__ void share_row(const Part& r, int rr, h8* to) {
+    const int s = threadIdx.x & 7;
+    int i;
+    const T* x = row_of(r, rr, &i) + s * KJ * 8;
+    T y[KJ][8];
+    float big = 0.0f;
+    int l = 0;
+#pragma unroll
+    for (int m = 0; m < KJ; ++m) __builtin_memcpy(y[m], x + m * 8, sizeof(y[m]));
+#pragma unroll
+    for (int m = 0; m < KJ; ++m) look(y[m], &big, &l);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      big = fmaxf(big, __shfl_xor(big, o, 64));
+      l |= __shfl_xor(l, o, 64);
+    }
+    const int e = exponent(big, l);
+    const bool used = rr < r.n_tokens * p.a.G && !l;
+#pragma unroll
+    for (int m = 0; m < KJ; ++m) {
+      const int d8 = s * KJ + m, j = d8 >> 3, kg = (d8 & 7) >> 1;
+      h8 part[QP];
+      parts_of(y[m], used, e, part, 1);
+#pragma unroll
+      for (int u = 0; u < QP; ++u)
+        to[(((rr >> 4) * 2 * KJ + 2 * j + (d8 & 1)) * QP + u) * 64 + kg * 16 + (rr & 15)] = part[u];
+    }
+    int* rows = (int*)(to + R * 2 * KJ * QP * 64);
+    if (s == 0) rows[rr] = e, rows[16 * R + rr] = l;
+  }
+
+  // The part's first loads, each as soon as its address is known, then its queries.
+  __device__ __forceinline__ void begin(const Part& r, int from, int to, const h8* shared) {
     g = r.g;
     h = r.h;
     pages = (r.s.len + (1 << p.shift) - 1) >> p.shift;
     const int first = page_of(from >> p.shift);
-    const int n_rows = r.n_tokens * a.G;
-    T y[R][2 * KJ][8];
+    const int n_rows = r.n_tokens * p.a.G;
+    T y[kShared ? 1 : 2 * KJ][8];
 #pragma unroll
     for (int s = 0; s < R; ++s) {
-      const int rr = s * 16 + row16;
-      const bool used = rr < n_rows;
-      const int i = used ? (int)((uint32_t)rr / (uint32_t)a.G) : 0, hq = used ? rr - i * a.G : 0;
-      vis[s] = !used ? 0 : r.s.causal ? r.s.len - r.s.rows + r.i0 + i + 1 : r.s.len;
-      const T* x = (const T*)a.q + (((int64_t)(r.s.begin + r.i0 + i) * a.H + r.h) * a.G + hq) * D;
+      int i;
+      const T* x = row_of(r, s * 16 + row16, &i);
+      vis[s] = s * 16 + row16 >= n_rows ? 0 : r.s.causal ? r.s.len - r.s.rows + r.i0 + i + 1 : r.s.len;
+      if constexpr (!kShared)
 #pragma unroll
-      for (int c = 0; c < 2 * KJ; ++c)
-        __builtin_memcpy(y[s][c], x + (c / 2) * 64 + group * 16 + (c % 2) * 8, sizeof(y[s][c]));
+        for (int c = 0; c < 2 * KJ; ++c)
+          __builtin_memcpy(y[c], x + (c / 2) * 64 + group * 16 + (c % 2) * 8, sizeof(y[c]));
     }
     scales_of(first);
     t[0] = half(from);
     t[1] = half(min(from + 16, to - 1) & ~15);
     load_k(t);
     load_v(t);
+    if constexpr (kShared) {
+      lq = shared + lane;
+      const int* rows = (const int*)(shared + R * 2 * KJ * QP * 64);
 #pragma unroll
-    for (int s = 0; s < R; ++s) {
-      const bool used = s * 16 + row16 < n_rows;
+      for (int s = 0; s < R; ++s) {
+        qe[s] = rows[s * 16 + row16];
+        lost[s] = rows[16 * R + s * 16 + row16];
+      }
+    } else {
       float big = 0.0f;
       int l = 0;
 #pragma unroll
-      for (int c = 0; c < 2 * KJ; ++c)
-#pragma unroll
-        for (int i8 = 0; i8 < 8; ++i8) {
-          const float z = fabsf(to_float(y[s][c][i8]));
-          l |= !(z < INFINITY);
-          big = fmaxf(big, z);
-        }
+      for (int c = 0; c < 2 * KJ; ++c) look(y[c], &big, &l);
       big = fmaxf(big, __shfl_xor(big, 16, 64));
       big = fmaxf(big, __shfl_xor(big, 32, 64));
       l |= __shfl_xor(l, 16, 64);
       l |= __shfl_xor(l, 32, 64);
-      lost[s] = l;
-      int ex = 0;
-      if (big > 0.0f && !l) ex = __builtin_amdgcn_frexp_expf(big);
-      qe[s] = ex - 15;  // the largest is in [2^14, 2^15)
+      lost[0] = l;
+      qe[0] = exponent(big, l);
 #pragma unroll
-      for (int c = 0; c < 2 * KJ; ++c)
-#pragma unroll
-        for (int i8 = 0; i8 < 8; ++i8) {
-          const float z = used && !l ? ldexpf(to_float(y[s][c][i8]), -qe[s]) : 0.0f;
-          q[s][c][0][i8] = (_Float16)z;
-          if constexpr (QP == 2) q[s][c][1][i8] = (_Float16)(z - (float)q[s][c][0][i8]);
-        }
+      for (int c = 0; c < 2 * KJ; ++c) parts_of(y[c], row16 < n_rows && !l, qe[0], q[0][c], 1);
     }
   }
   __device__ __forceinline__ void clear() {
@@ -421,18 +491,25 @@ struct Wave {
 #pragma unroll
         for (int r = 0; r < R; ++r) s[r][u] = f4{0, 0, 0, 0};
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int j = 0; j < KJ; ++j) {
+        h8 x[2][2];
 #pragma unroll
-        for (int j = 0; j < KJ; ++j) {
-          const h8 a = halves<CODES>(k[u][j].x, k[u][j].y), b = halves<CODES>(k[u][j].z, k[u][j].w);
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int i = QP - 1; i >= 0; --i) {
-              s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[r][2 * j][i], s[r][u], 0, 0, 0);
-              s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, q[r][2 * j + 1][i], s[r][u], 0, 0, 0);
-            }
+        for (int u = 0; u < 2; ++u) {
+          x[u][0] = halves<CODES>(k[u][j].x, k[u][j].y);
+          x[u][1] = halves<CODES>(k[u][j].z, k[u][j].w);
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int i = QP - 1; i >= 0; --i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const h8 y = kShared ? lq[((r * 2 * KJ + 2 * j + c) * QP + i) * 64] : q[kShared ? 0 : r][2 * j + c][i];
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+                s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[u][c], y, s[r][u], 0, 0, 0);
+            }
+      }
       // The next tile's keys are on their way from here on, its values from the end.  (The
       // last tile's own again: a branch around the loads would make each wait one for all.)
       const float ks[2] = {t[0].ks, t[1].ks}, vs[2] = {t[0].vs, t[1].vs};
@@ -463,7 +540,7 @@ struct Wave {
           more = 0.0f;
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const float c = limited(ldexpf(vs[u], -e[r]));
+            const float c = __builtin_amdgcn_fmed3f(ldexpf(vs[u], -e[r]), -kMost, kMost);
             top_p[u] = 0.0f;
 #pragma unroll
             for (int i = 4 * u; i < 4 * u + 4; ++i) {
@@ -494,8 +571,7 @@ struct Wave {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
           const h2 x = __builtin_convertvector(f2{w[i], w[i + 1]}, h2);
-          const h2 y = __builtin_convertvector(f2{__builtin_fmaf((float)x[0], -1.0f, w[i]),
-                                                  __builtin_fmaf((float)x[1], -1.0f, w[i + 1])}, h2);
+          const h2 y = __builtin_convertvector(f2{rest<0>(x, w[i]), rest<1>(x, w[i + 1])}, h2);
           hi[r][i] = x[0], hi[r][i + 1] = x[1];
           lo[r][i] = y[0], lo[r][i + 1] = y[1];
         }
@@ -551,23 +627,21 @@ struct Wave {
     return h8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
   }
 
-  __device__ __forceinline__ void store(const State<D>& to) const {
+  // rows 16 r .. 16 r + 15
+  __device__ __forceinline__ void store(int r, const State<D>& to) const {
+    if (group == 0 && row16 < to.rows) {
+      to.ref(row16) = ref[r];
+      to.sum(row16) = lost[r] && sum[r] > 0.0f ? NAN : sum[r];
+      to.exp(row16) = (float)e[r];
+    }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (group == 0 && r * 16 + row16 < to.rows) {
-        to.ref(r * 16 + row16) = ref[r];
-        to.sum(r * 16 + row16) = lost[r] && sum[r] > 0.0f ? NAN : sum[r];
-        to.exp(r * 16 + row16) = (float)e[r];
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int rr = group * 4 + i;
+      if (rr >= to.rows) break;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int rr = r * 16 + group * 4 + i;
-        if (rr >= to.rows) break;
-#pragma unroll
-        for (int c = 0; c < CB; c += 4)
-          *(f4*)(to.acc(rr) + row16 * CB + c) =
-              f4{acc[r][c][i], acc[r][c + 1][i], acc[r][c + 2][i], acc[r][c + 3][i]};
-      }
+      for (int c = 0; c < CB; c += 4)
+        *(f4*)(to.acc(rr) + row16 * CB + c) =
+            f4{acc[r][c][i], acc[r][c + 1][i], acc[r][c + 2][i], acc[r][c + 3][i]};
     }
   }
 };
@@ -585,13 +659,66 @@ __device__ __forceinline__ float finished(float acc, float sum, float exp) {
 }
 
 
+// Row rr of an item from the W states of the workgroup's wavefronts: the result, or the
+// part's state.
+template <int D, int MOST>
+__device__ __forceinline__ void finish_row(const Args& p, const Part& r, int rr, int rr16,
+                                           const State<D>& states, const State<D>& record, int W,
+                                           int lane) {
+  constexpr int kPer = D / 64;  // columns of a lane
+  // (of MOST states, the last one's again behind it: reads that wait for nothing)
+  Joined j{kNone, -0x1p30f};
+  float refs[MOST], exps[MOST], sum = 0.0f, acc[kPer];
+#pragma unroll
+  for (int v = 0; v < MOST; ++v) {
+    const State<D> x = state<D>(states.at, min(v, W - 1), states.rows);
+    refs[v] = x.ref(rr16);
+    exps[v] = x.exp(rr16);
+    j.ref = fmaxf(j.ref, refs[v]);
+  }
+#pragma unroll
+  for (int v = 0; v < MOST; ++v)
+    if (refs[v] > kNone) j.exp = fmaxf(j.exp, ceilf(refs[v] - j.ref) + exps[v]);
+#pragma unroll
+  for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
+#pragma unroll
+  for (int v = 0; v < MOST; ++v) {
+    if (v >= W) break;
+    const State<D> x = state<D>(states.at, v, states.rows);
+    const float f = factor(refs[v], exps[v], j);
+    sum += x.sum(rr16) * exp2_(refs[v] - j.ref);
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) acc[c] += x.acc(rr16)[lane * kPer + c] * f;
+  }
+  if (r.parts == 1) {
+    const int i = rr / p.a.G, hq = rr - i * p.a.G;
+    float* out = p.a.out +
+                 (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) out[c] = r.s.bad ? NAN : finished(acc[c], sum, j.exp);
+  } else {
+    if (lane == 0) {
+      record.ref(rr) = j.ref;
+      record.sum(rr) = sum;
+      record.exp(rr) = j.exp;
+    }
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) record.acc(rr)[lane * kPer + c] = acc[c];
+  }
+}
+
 // Wavefronts that a SIMD holds at once, by registers.
 __host__ __device__ constexpr int waves_of_simd(int R, int D) {
   return R == 1 ? (D == 64 ? 4 : D == 128 ? 3 : 2) : D == 64 ? 3 : D == 128 ? 2 : 1;
 }
 
+// Wavefronts of a workgroup, at most.
+__host__ __device__ constexpr int most_waves(int R, int D) {
+  return R == 1 && D == 64 ? 8 : 4;
+}
+
 template <typename T, int CODES, int D, int R>
-__global__ __launch_bounds__(R == 1 && D == 64 ? 512 : 256, waves_of_simd(R, D))
+__global__ __launch_bounds__(64 * most_waves(R, D), waves_of_simd(R, D))
 void main_kernel(Args p) {
   extern __shared__ __align__(16) float states[];
   const int lane = threadIdx.x & 63, W = blockDim.x >> 6;
@@ -607,56 +734,24 @@ void main_kernel(Args p) {
   const int from = r.from + min(tiles, wave * each) * 32;
   const int to = min(r.to, r.from + min(tiles, (wave + 1) * each) * 32);
   wv.clear();
+  h8* queries = (h8*)(states + 64);  // (behind part_at's words)
+  if constexpr (R > 1) {
+    wv.share_queries(r, queries);
+    __syncthreads();
+  }
   if (from < to) {
-    wv.begin(r, from, to);
+    wv.begin(r, from, to, queries);
     wv.run(r, from, to);
   }
-  __syncthreads();  // (part_at's words have been read)
-  wv.store(state<D>(states, wave, p.rows));
-  __syncthreads();
   const State<D> record = state<D>(p.a.ws, blockIdx.x, p.rows);
-  constexpr int kPer = D / 64;  // columns of a lane
-  const int n_rows = r.n_tokens * p.a.G;
-  for (int rr = wave; rr < n_rows; rr += W) {
-    // (of 8 states, the last one's again behind it: reads that wait for nothing)
-    Joined j{kNone, -0x1p30f};
-    float refs[8], exps[8], sum = 0.0f, acc[kPer];
+  const int n_rows = r.n_tokens * p.a.G, rows16 = min(p.rows, 16);
 #pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      const State<D> x = state<D>(states, min(v, W - 1), p.rows);
-      refs[v] = x.ref(rr);
-      exps[v] = x.exp(rr);
-      j.ref = fmaxf(j.ref, refs[v]);
-    }
-#pragma unroll
-    for (int v = 0; v < 8; ++v)
-      if (refs[v] > kNone) j.exp = fmaxf(j.exp, ceilf(refs[v] - j.ref) + exps[v]);
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
-#pragma unroll
-    for (int v = 0; v < 8; ++v) {
-      if (v >= W) break;
-      const State<D> x = state<D>(states, v, p.rows);
-      const float f = factor(refs[v], exps[v], j);
-      sum += x.sum(rr) * exp2_(refs[v] - j.ref);
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) acc[c] += x.acc(rr)[lane * kPer + c] * f;
-    }
-    if (r.parts == 1) {
-      const int i = rr / p.a.G, hq = rr - i * p.a.G;
-      float* out = p.a.out +
-                   (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) out[c] = r.s.bad ? NAN : finished(acc[c], sum, j.exp);
-    } else {
-      if (lane == 0) {
-        record.ref(rr) = j.ref;
-        record.sum(rr) = sum;
-        record.exp(rr) = j.exp;
-      }
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) record.acc(rr)[lane * kPer + c] = acc[c];
-    }
+  for (int group = 0; group < R; ++group) {
+    __syncthreads();  // (what was in LDS has been read)
+    wv.store(group, state<D>(states, wave, rows16));
+    __syncthreads();
+    for (int rr16 = wave; rr16 < min(16, n_rows - 16 * group); rr16 += W)
+      finish_row<D, most_waves(R, D)>(p, r, group * 16 + rr16, rr16, state<D>(states, 0, rows16), record, W, lane);
   }
 }
 
@@ -675,7 +770,8 @@ __global__ __launch_bounds__(256) void merge_kernel(Args p) {
     uint64_t todo = __ballot(wl < p.parts && list[min(wl, p.parts - 1)].parts > 0);
     for (; todo; todo &= todo - 1) {
       const int w = w0 + (__ffsll((unsigned long long)todo) - 1) * gridDim.x;
-      const int parts = uni(list[w].parts), n_rows = uni(list[w].n_rows), row = uni(list[w].row),
+      // (no record behind the last one is read, whatever became of the lengths meanwhile)
+      const int parts = min(uni(list[w].parts), (p.parts - 1 - w) / p.a.H + 1), n_rows = uni(list[w].n_rows), row = uni(list[w].row),
                 h = uni(list[w].h);
       const int rows_apart = gridDim.y * (4 / WIDE);
       for (int rr = blockIdx.y * (4 / WIDE) + (WIDE > 1 ? 0 : wave); rr < n_rows; rr += rows_apart) {
@@ -771,12 +867,15 @@ Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pa
   // (an item's last part is half empty on the average)
   int64_t target = std::max(k * kCu - items / 2, items / 2);
   if (p.R == 2) target = kCu * held / 4;
-  p.waves = p.R == 1 && d == 64 ? 8 : 4;
+  p.waves = most_waves(p.R, d);
   if (p.R == 1)
     while (p.waves > 2 && (p.cut ? k : (items + kCu - 1) / kCu) * p.waves > held) p.waves /= 2;
-  p.least = !p.cut ? (int)room : items >= kCu ? 2048 : items >= kCu / 2 ? 1024 : 512;
+  else if (room <= 1024 && items >= 8 * kCu)
+    p.waves = 2;
+  p.least = !p.cut ? (int)std::max<int64_t>(room, 32) : items >= kCu ? 2048 : items >= kCu / 2 ? 1024 : 512;
   p.target = (float)target;
   p.parts = (int)(items + (p.cut ? target : 0));
+  while (p.waves > 1 && (int64_t)p.parts * p.waves >= 1 << 26) p.waves /= 2;  // (a grid's 2^32 threads)
   p.joins = std::min(p.parts, p.R == 1 ? 251 : 509);
   p.bytes = p.cut ? (size_t)p.parts * (state_floats(p.rows, d) * 4 + sizeof(Join)) : 0;
   return p;
@@ -784,7 +883,8 @@ Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pa
 
 template <typename T, int CODES, int D, int R>
 int launch(const Args& p, const Plan& pl, hipStream_t st) {
-  const size_t lds = std::max((size_t)pl.waves * state_floats(pl.rows, D), (size_t)part_lds(pl.waves)) * 4;
+  const size_t words = std::max((size_t)pl.waves * state_floats(std::min(pl.rows, 16), D), (size_t)part_lds(pl.waves)) * 4;
+  const size_t lds = R == 1 ? words : std::max(words, 256 + (size_t)R * D * (sizeof(T) == 4 ? 64 : 32) + 128 * R);
   main_kernel<T, CODES, D, R><<<pl.parts, 64 * pl.waves, lds, st>>>(p);
   int rc = (int)hipGetLastError();
   if (rc != 0 || !pl.cut) return rc;

@@ -789,11 +789,12 @@ PyObject* attn_cache8(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   int rc;
   {
     NoGil no_gil;
-    if (!ws.defined()) ws = empty(p.dev, at::kByte, {need > 1 ? need : 1});
+    if (!ws.defined() && need > 0) ws = empty(p.dev, at::kByte, {need});
     if (!out.defined()) out = empty(p.dev, at::kFloat, {n_rows, Hq, p.d});
     rc = g_attn8(pq, dt, kp, ks, vp, vs, p.codes, pt, pl, ps, n, n_rows, (int)p.H, G, max_pages, (int)p.page,
-                 p.n_pages, (int)p.d, causal, scale, static_cast<float*>(out.data_ptr()), ws.data_ptr(),
-                 (size_t)ws.numel(), reinterpret_cast<void*>(st));
+                 p.n_pages, (int)p.d, causal, scale, static_cast<float*>(out.data_ptr()),
+                 ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0,
+                 reinterpret_cast<void*>(st));
   }
   if (rc != FIBQ_OK) return raise_status(rc, "fibq_attn_cache8");
   return keep(a[11], out);

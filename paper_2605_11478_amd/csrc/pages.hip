@@ -42,7 +42,7 @@ __device__ __forceinline__ void store(T* p, const Vec<T, V>& v) {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeAngles = 1024;  // angles of a workgroup, at most
 
-template <typename T, int V, bool HALF>
+template <typename T, int V, int VT, bool HALF>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
   __shared__ float2 turn[kRopeAngles];
   const int tid = threadIdx.x, half = a.rot / 2;
@@ -61,24 +61,46 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
     turn[i] = make_float2(cs * a.scale, (a.inverse ? -sn : sn) * a.scale);
   }
   __syncthreads();
-  // A thread has one piece of V elements of every head that it visits, so a row's angles
-  // stay in its registers; kHeads loads are on their way at once.
-  constexpr int kHeads = HALF ? 2 : 4;
-  const int heads = a.q_heads + a.k_heads;
+  // A thread has one piece of V elements (or pairs) of every head that it visits, so a
+  // row's angles stay in its registers; kHeads loads are on their way at once.  What lies
+  // behind the turned part is copied VT elements at a time, the last piece over the one
+  // before it.
+  constexpr int kHeads = HALF && V > 1 ? 2 : 4;
+  const int heads = a.q_heads + a.k_heads, tail = a.d - a.rot;
   const int turned = HALF ? half / V : a.rot / V;
-  const int per_head = turned + (a.d - a.rot) / V;  // (rows are copied behind the turned part)
+  const int per_head = turned + (tail + VT - 1) / VT;
   for (int c0 = 0; c0 < per_head; c0 += kRopeThreads) {
     const int pieces = min(per_head - c0, kRopeThreads), at_once = kRopeThreads / pieces;
     const int slot = tid / pieces, c = c0 + tid - slot * pieces;
     if (slot >= at_once) continue;
     const bool turns = c < turned;
-    const int at = turns ? c * V : a.rot + (c - turned) * V;
+    const int at = turns ? c * V : min(a.rot + (c - turned) * VT, a.d - VT);
+    if (!turns) {
+      for (int i0 = slot; i0 < rows * heads; i0 += kHeads * at_once) {
+        Vec<T, VT> x[kHeads];
+        T* to[kHeads];
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u) {
+          const int i = min(i0 + u * at_once, rows * heads - 1), r = i / heads, h = i - r * heads;
+          const int64_t row = row0 + r;
+          const bool is_k = h >= a.q_heads;
+          x[u] = load<T, VT>((is_k ? (const T*)a.k + row * a.k_row + (h - a.q_heads) * a.k_head
+                                   : (const T*)a.q + row * a.q_row + h * a.q_head) + at);
+          to[u] = (is_k ? (T*)a.k_out + row * a.ko_row + (h - a.q_heads) * a.ko_head
+                        : (T*)a.q_out + row * a.qo_row + h * a.qo_head) + at;
+        }
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u)
+          if (i0 + u * at_once < rows * heads) store<T, VT>(to[u], x[u]);
+      }
+      continue;
+    }
     for (int r = 0; r < rows; ++r) {
       constexpr int kAngles = HALF ? V : V / 2;
       float2 w[kAngles];
 #pragma unroll
       for (int e = 0; e < kAngles; ++e)
-        w[e] = turns ? turn[r * half + (HALF ? at : at / 2) + e] : make_float2(1.0f, 0.0f);
+        w[e] = turn[r * half + (HALF ? at : at / 2) + e];
       const int64_t row = row0 + r;
       const T *q = (const T*)a.q + row * a.q_row, *k = (const T*)a.k + row * a.k_row;
       T *qo = (T*)a.q_out + row * a.qo_row, *ko = (T*)a.k_out + row * a.ko_row;
@@ -89,16 +111,14 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
           const int h = min(h0 + u * at_once, heads - 1);
           const T* x = (h < a.q_heads ? q + h * a.q_head : k + (h - a.q_heads) * a.k_head) + at;
           x0[u] = load<T, V>(x);
-          if constexpr (HALF) x1[u] = turns ? load<T, V>(x + half) : x0[u];
+          if constexpr (HALF) x1[u] = load<T, V>(x + half);
         }
 #pragma unroll
         for (int u = 0; u < kHeads; ++u) {
           const int h = h0 + u * at_once;
           if (h >= heads) break;
           T* y = (h < a.q_heads ? qo + h * a.qo_head : ko + (h - a.q_heads) * a.ko_head) + at;
-          if (!turns) {
-            store<T, V>(y, x0[u]);
-          } else if constexpr (HALF) {
+          if constexpr (HALF) {
             Vec<T, V> y0, y1;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -131,16 +151,23 @@ int rope_typed(const Rope& a, hipStream_t st) {
   int tile = std::min<int64_t>(std::max(1, kRopeAngles / half), std::max<int64_t>(1, a.n_rows / 1024));
   tile = std::min(tile, 16);
   const int64_t grid = (a.n_rows + tile - 1) / tile;
+  const int tail = a.d - a.rot;
+  auto go = [&](auto kernel) { kernel<<<grid, kRopeThreads, 0, st>>>(a, tile); };
+  const bool wide = tail == 0 || tail >= V;
   if (a.layout == FIBQ_ROPE_HALF) {
-    if (half % V == 0 && a.d % V == 0)
-      rope_kernel<T, V, true><<<grid, kRopeThreads, 0, st>>>(a, tile);
+    if (half % V == 0 && wide)
+      go(rope_kernel<T, V, V, true>);
+    else if (wide)
+      go(rope_kernel<T, 1, V, true>);
     else
-      rope_kernel<T, 1, true><<<grid, kRopeThreads, 0, st>>>(a, tile);
+      go(rope_kernel<T, 1, 1, true>);
   } else {
-    if (a.rot % V == 0 && a.d % V == 0)
-      rope_kernel<T, V, false><<<grid, kRopeThreads, 0, st>>>(a, tile);
+    if (a.rot % V == 0 && wide)
+      go(rope_kernel<T, V, V, false>);
+    else if (wide)
+      go(rope_kernel<T, 2, V, false>);
     else
-      rope_kernel<T, 2, false><<<grid, kRopeThreads, 0, st>>>(a, tile);
+      go(rope_kernel<T, 2, 1, false>);
   }
   return (int)hipGetLastError();
 }
@@ -391,9 +418,9 @@ __device__ __forceinline__ void value4(uint32_t w, int codes, float* x) {
 }
 
 // Rows of a run are read once, into registers, where they fit (kHeld pieces a thread).
-template <typename T, int D>
+template <typename T, int D, int kHeld>
 __global__ __launch_bounds__(256) void write_kernel(Write a, int shift, int chunk) {
-  constexpr int V = 8, kRow = D / V, kHeld = 4;
+  constexpr int V = 8, kRow = D / V;
   __shared__ uint32_t wave_max[4];
   const int tid = threadIdx.x, lane = tid & 63, n_threads = blockDim.x;
   const int h = blockIdx.y;
@@ -524,10 +551,20 @@ int write_typed(const Write& a, hipStream_t st) {
   const int64_t x = (a.n_rows + chunk - 1) / chunk;
   const dim3 grid((unsigned)x, a.H, 2);
   const int threads = chunk == 1 ? 64 : 256, shift = __builtin_ctz(a.page);
+  const bool few = a.page * a.d <= 2 * 8 * threads;  // pieces of a page for each thread
   switch (a.d) {
-    case 64: write_kernel<T, 64><<<grid, threads, 0, st>>>(a, shift, chunk); break;
-    case 128: write_kernel<T, 128><<<grid, threads, 0, st>>>(a, shift, chunk); break;
-    default: write_kernel<T, 256><<<grid, threads, 0, st>>>(a, shift, chunk); break;
+    case 64:
+      few ? write_kernel<T, 64, 2><<<grid, threads, 0, st>>>(a, shift, chunk)
+          : write_kernel<T, 64, 4><<<grid, threads, 0, st>>>(a, shift, chunk);
+      break;
+    case 128:
+      few ? write_kernel<T, 128, 2><<<grid, threads, 0, st>>>(a, shift, chunk)
+          : write_kernel<T, 128, 4><<<grid, threads, 0, st>>>(a, shift, chunk);
+      break;
+    default:
+      few ? write_kernel<T, 256, 2><<<grid, threads, 0, st>>>(a, shift, chunk)
+          : write_kernel<T, 256, 4><<<grid, threads, 0, st>>>(a, shift, chunk);
+      break;
   }
   return (int)hipGetLastError();
 }

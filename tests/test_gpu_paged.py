@@ -53,7 +53,8 @@ def check_rope(y, x, positions, freqs, layout, scale=1.0, inverse=False):
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("n,Hq,Hk,d,rot", [(1, 1, 1, 64, 64), (5, 8, 2, 64, 32), (33, 3, 0, 128, 128),
                                            (70, 12, 12, 128, 10), (3, 2, 1, 10, 6), (2, 1, 1, 2, 2),
-                                           (2100, 2, 1, 64, 48), (9, 4, 2, 512, 512), (7, 5, 3, 66, 34)])
+                                           (2100, 2, 1, 64, 48), (9, 4, 2, 512, 512), (7, 5, 3, 66, 34),
+                                           (1500, 9, 4, 30, 22), (40, 1, 1, 500, 10)])
 def test_rope(device, layout, dtype, n, Hq, Hk, d, rot):
     g = torch.Generator(device=device).manual_seed(n + d)
     q = torch.randn(n, Hq, d, generator=g, device=device).to(TYPES[dtype])
@@ -355,7 +356,7 @@ def run_attention(device, rng, lens, rows, H, G, page, d, kind, dtype, causal, o
 @pytest.mark.parametrize("kind", list(CODES))
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("H,G,page,d", [(1, 1, 16, 64), (2, 8, 16, 64), (2, 3, 32, 128), (1, 16, 64, 128),
-                                        (1, 5, 128, 256), (3, 2, 16, 256)])
+                                        (1, 5, 128, 256), (3, 2, 16, 256), (1, 16, 32, 256)])
 def test_attn_one_row(device, kind, dtype, H, G, page, d):
     rng = np.random.default_rng(d + G)
     lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 300, 1000, -1, 10 ** 9]
@@ -398,6 +399,84 @@ def test_attn_queries_of_any_size(device, q_times, scale):
     rng = np.random.default_rng(9)
     run_attention(device, rng, [200, 31], [1, 20], 1, 4, 16, 64, "e4m3", "fp32", True, scale=scale,
                   q_times=q_times)
+
+
+def test_attn_scales_farther_apart(device):
+    """A page of the largest scale whose weight is so small that it counts for as much as the others."""
+    rng = np.random.default_rng(14)
+    kp, ks, vp, vs, table = make_cache(rng, [64], 1, 16, 64, "int8")
+    kp[:] = 0
+    kp[table[0, :4], 0, :, 0] = np.array([10, 60, 35, 0], np.uint8)[:, None]  # scores, up to factors
+    ks[:], vs[:] = 1.0, 1.0
+    vs[table[0, :4], 0] = 2.0 ** np.array([40, -60, -10, 30])
+    for step in (0.5, 1.0, 1.5, 2.0):  # 2^(50 step / ln 2) between the first two pages' weights
+        q = torch.zeros(1, 1, 64, device=device)
+        q[0, 0, 0] = step * math.log(2)
+        t = lambda a: torch.from_numpy(a).to(device)
+        out = fq.attn_cache8(q, on(device, kp, "int8"), t(ks), on(device, vp, "int8"), t(vs), t(table),
+                             t(np.array([64], np.int32)), scale=1.0)
+        check_attention(host(out), host(q), kp, ks, vp, vs, table, [64], [0, 1], True, "int8", 1.0)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_attn_queries_that_are_no_numbers(device, rows, dtype):
+    """A row of queries with a NaN or an infinity is NaN, and no other row is."""
+    rng = np.random.default_rng(15)
+    lens = np.array([100, 77], np.int32)
+    kp, ks, vp, vs, table = make_cache(rng, lens, 1, 16, 64, "e4m3")
+    q = torch.randn(2 * rows, 3, 64, device=device).to(TYPES[dtype])
+    q[rows - 1, 1, 5], q[rows, 2, 63] = math.inf, math.nan
+    t = lambda a: torch.from_numpy(a).to(device)
+    starts = t(np.array([0, rows, 2 * rows], np.int32))
+    out = host(fq.attn_cache8(q, on(device, kp, "e4m3"), t(ks), on(device, vp, "e4m3"), t(vs), t(table), t(lens),
+                              starts))
+    bad = np.zeros((2 * rows, 3), bool)
+    bad[rows - 1, 1] = bad[rows, 2] = True
+    assert np.isnan(out[bad]).all() and np.isfinite(out[~bad]).all()
+
+
+def test_attn_without_pages(device):
+    """Tables of no page: rows that see nothing are zero, causal rows of no token NaN."""
+    rng = np.random.default_rng(16)
+    kp, ks, vp, vs, _ = make_cache(rng, [16], 1, 16, 64, "int8")
+    t = lambda a: torch.from_numpy(a).to(device)
+    args = (on(device, kp, "int8"), t(ks), on(device, vp, "int8"), t(vs),
+            torch.zeros(3, 0, dtype=torch.int32, device=device), torch.zeros(3, dtype=torch.int32, device=device))
+    starts = t(np.array([0, 2, 2, 50], np.int32))
+    q = torch.randn(50, 2, 64, device=device)
+    for s in (starts, None):
+        rows = q if s is not None else q[:3].contiguous()
+        assert (fq.attn_cache8(rows, *args, s, causal=False) == 0).all()
+        assert torch.isnan(fq.attn_cache8(rows, *args, s)).all()
+
+
+def test_attn_table_wider_than_its_sequences(device):
+    """Room for 65536 tokens, none of the sequences longer than 700: as in a narrow table."""
+    rng = np.random.default_rng(17)
+    lens = np.array([700, 3, 0, 512, 64, 333], np.int32)
+    for rows in (1, 30):
+        kp, ks, vp, vs, table = make_cache(rng, lens, 2, 16, 64, "int8")
+        wide = np.full((6, 4096), -1, np.int32)
+        wide[:, :table.shape[1]] = table
+        q = torch.randn(6 * rows, 8, 64, device=device)
+        t = lambda a: torch.from_numpy(a).to(device)
+        out = fq.attn_cache8(q, on(device, kp, "int8"), t(ks), on(device, vp, "int8"), t(vs), t(wide), t(lens),
+                             t(np.arange(0, 6 * rows + 1, rows, dtype=np.int32)), causal=False)
+        check_attention(host(out), host(q), kp, ks, vp, vs, wide, lens, np.arange(0, 6 * rows + 1, rows), False,
+                        "int8")
+
+
+@pytest.mark.parametrize("n,H", [(700, 2), (3000, 1)])
+def test_attn_many_sequences(device, n, H):
+    """More sequences than threads, a few long among short ones, in one call and in room for more."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 40, n).astype(np.int32)
+    lens[[5, n // 2, n - 1]] = 2500
+    run_attention(device, rng, lens, [1] * n, H, 2, 16, 64, "int8", "bf16", False, one=True)
+    rows = rng.integers(0, 3, n)
+    rows[n // 2] = 70
+    run_attention(device, rng, lens, rows, H, 2, 16, 64, "int8", "bf16", False)
 
 
 def test_attn_finite_for_the_largest(device):
@@ -475,6 +554,30 @@ def test_attn_layouts_streams_and_workspace(device):
             got = fq.attn_cache8(q, *pools_, tab, ln, st, workspace=ws)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def test_pools_beyond_32_bits(device):
+    """Pages whose bytes lie 5 GB into their pool."""
+    H, page, d, n_pages = 8, 128, 128, 40000  # 5.2 GB each
+    kp, vp = (torch.empty((n_pages, H, page, d), dtype=torch.int8, device=device) for _ in range(2))
+    ks, vs = (torch.empty((n_pages, H), device=device) for _ in range(2))
+    ids = [n_pages - 1, 0, n_pages - 2]
+    slots = torch.cat([torch.arange(page, device=device) + p * page for p in ids])[:300]
+    x = torch.randn(300, 2, H, d, device=device)
+    fq.cache8_write(x[:, 0], x[:, 1], slots, kp, ks, vp, vs)
+    small = [np.zeros((3, H, page, d), np.uint8), np.zeros((3, H), np.float32),
+             np.zeros((3, H, page, d), np.uint8), np.zeros((3, H), np.float32)]
+    near = np.arange(300)
+    opg.write(x[:, 0].cpu().numpy(), near, small[0], small[1], "int8")
+    opg.write(x[:, 1].cpu().numpy(), near, small[2], small[3], "int8")
+    for i, p in enumerate(ids):
+        m = min(page, 300 - i * page)
+        assert np.array_equal(raw(kp[p])[:, :m], small[0][i][:, :m])
+        assert np.array_equal(vs[p].cpu().numpy(), small[3][i])
+    q = torch.randn(5, H, d, device=device)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=device)
+    out = fq.attn_cache8(q, kp, ks, vp, vs, i32([ids]), i32([300]), i32([0, 5]))
+    check_attention(host(out), host(q), *small, np.array([[0, 1, 2]]), [300], [0, 5], True, "int8")
 
 
 # ------------------------------------------------------- as they are used --
@@ -585,6 +688,35 @@ def test_captured_step(device):
         assert torch.equal(out_e, out_c) and torch.equal(eager[1], captured[1])
         assert torch.equal(eager[2], captured[2]) and torch.equal(raw_t(eager[0][0]), raw_t(captured[0][0]))
         assert torch.equal(eager[0][1], captured[0][1])
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_captured_long_items(device, rows):
+    """Items cut into parts, their lengths changing between replays, with eager calls between."""
+    rng = np.random.default_rng(24)
+    lens = np.array([6000, 300, 2900], np.int32)
+    kp, ks, vp, vs, table = make_cache(rng, lens, 2, 16, 64, "e4m3")
+    t = lambda a: torch.from_numpy(a).to(device)
+    pools_ = (on(device, kp, "e4m3"), t(ks), on(device, vp, "e4m3"), t(vs))
+    tab, ln, st = t(table), t(lens), t(np.arange(0, 3 * rows + 1, rows, dtype=np.int32))
+    q = torch.randn(3 * rows, 8, 64, device=device)
+    ws = torch.empty(fq.attn_cache8_workspace_bytes(3, 3 * rows, 2, 4, table.shape[1], 16, 64), dtype=torch.uint8,
+                     device=device)
+    assert ws.numel() > 0
+    out, want = torch.zeros(3 * rows, 8, 64, device=device), torch.zeros(3 * rows, 8, 64, device=device)
+    call = lambda o, w: fq.attn_cache8(q, *pools_, tab, ln, st, workspace=w, out=o)
+    call(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    for now in ([6000, 300, 2900], [50, 300, 2900], [6000, 40, 41], [5999, -1, 2049], [6000, 300, 2900]):
+        ln.copy_(torch.tensor(now, dtype=torch.int32))
+        q.normal_()
+        call(want, None)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int32), want.view(torch.int32))
 
 
 def raw_t(t):
