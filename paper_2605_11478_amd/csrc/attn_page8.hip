@@ -54,6 +54,7 @@ struct Args {
   int rows;         // query rows of an item, at most
   int cut;          // items may be cut
   int parts;        // at most
+  uint32_t magic;   // ceil(2^16 / G): x / G = x magic >> 16 for the rows of an item
 };
 
 // ------------------------------------------------------------------- work --
@@ -100,29 +101,31 @@ __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds)
     g = (int)((uint32_t)w / H);
     first = g * (int)H;
   } else {
-    Seq s{};
-    float tokens = 0.0f;
-    for (int at = tid; at < n; at += 64 * W) {
-      s = sequence(p, at);
-      tokens += (float)s.tiles * (float)s.len;
+    Seq s = tid < n ? sequence(p, tid) : Seq{};
+    if (p.cut) {
+      float tokens = (float)s.tiles * (float)s.len;
+      for (int at = tid + 64 * W; at < n; at += 64 * W) {
+        const Seq more = sequence(p, at);
+        tokens += (float)more.tiles * (float)more.len;
+      }
+      tokens = wave_sum(tokens);
+      if (lane == 0) lds[wave] = __float_as_int(tokens);
+      __syncthreads();
+      tokens = 0.0f;
+      for (int v = 0; v < W; ++v) tokens += __int_as_float(lds[v]);
+      // (a little more than the exact quotient, so that rounding never makes a part too many)
+      const float share = tokens * (float)p.a.H * 1.001f / p.target;
+      part = (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
+      __syncthreads();
     }
-    tokens = wave_sum(tokens);
-    if (lane == 0) lds[wave] = __float_as_int(tokens);
-    __syncthreads();
-    tokens = 0.0f;
-    for (int v = 0; v < W; ++v) tokens += __int_as_float(lds[v]);
-    // (a little more than the exact quotient, so that rounding never makes a part too many)
-    const float share = tokens * (float)p.a.H * 1.001f / p.target;
-    part = (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
     int* found = lds + W;  // sequence, parts before it
     int* sums = found + 2;
-    __syncthreads();
     if (tid == 0) found[0] = -1;
     int before = 0;
     for (int g0 = 0; g0 < n; g0 += 64 * W) {
       const int at = g0 + tid;
-      if (n > 64 * W) s = at < n ? sequence(p, at) : Seq{};
-      const int parts = max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part));
+      if (g0 > 0) s = at < n ? sequence(p, at) : Seq{};
+      const int parts = part ? max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part)) : 1;
       const int mine = at < n ? s.tiles * parts * p.a.H : 0;
       int upto = mine;
 #pragma unroll
@@ -329,7 +332,7 @@ struct Wave {
   __device__ __forceinline__ const T* row_of(const Part& r, int rr, int* i) const {
     const PageAttn& a = p.a;
     const bool used = rr < r.n_tokens * a.G;
-    *i = used ? (int)((uint32_t)rr / (uint32_t)a.G) : 0;
+    *i = used ? (int)((uint32_t)rr * p.magic >> 16) : 0;
     const int hq = used ? rr - *i * a.G : 0;
     return (const T*)a.q + (((int64_t)(r.s.begin + r.i0 + *i) * a.H + r.h) * a.G + hq) * D;
   }
@@ -627,6 +630,33 @@ struct Wave {
     return h8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
   }
 
+  // The results of an item that one wavefront has whole.
+  __device__ __forceinline__ void finish(const Part& part) const {
+    const PageAttn& a = p.a;
+    const int n_rows = part.n_tokens * a.G;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float all = lost[r] && sum[r] > 0.0f ? NAN : sum[r];
+      const float over = part.s.bad ? NAN : all == 0.0f ? 0.0f : 1.0f / all;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int rr = r * 16 + group * 4 + i;
+        const float by = __shfl(over, group * 4 + i, 64);
+        const int ex = __shfl(e[r], group * 4 + i, 64);
+        if (rr >= n_rows) continue;
+        const int token = (int)((uint32_t)rr * p.magic >> 16), hq = rr - token * a.G;
+        float* out = a.out +
+                     (((int64_t)(part.s.begin + part.i0 + token) * a.H + part.h) * a.G + hq) * D +
+                     row16 * CB;
+#pragma unroll
+        for (int c = 0; c < CB; c += 4) {
+          const f4 x{ldexpf(acc[r][c][i] * by, ex), ldexpf(acc[r][c + 1][i] * by, ex),
+                     ldexpf(acc[r][c + 2][i] * by, ex), ldexpf(acc[r][c + 3][i] * by, ex)};
+          __builtin_memcpy(out + c, &x, 16);  // (any alignment)
+        }
+      }
+    }
+  }
   // rows 16 r .. 16 r + 15
   __device__ __forceinline__ void store(int r, const State<D>& to) const {
     if (group == 0 && row16 < to.rows) {
@@ -659,51 +689,72 @@ __device__ __forceinline__ float finished(float acc, float sum, float exp) {
 }
 
 
-// Row rr of an item from the W states of the workgroup's wavefronts: the result, or the
-// part's state.
-template <int D, int MOST>
-__device__ __forceinline__ void finish_row(const Args& p, const Part& r, int rr, int rr16,
-                                           const State<D>& states, const State<D>& record, int W,
-                                           int lane) {
+// 16 rows of an item from the W <= 8 states of the workgroup's wavefronts: the result, or
+// the part's state.  A lane has one row's statistics in states lane / 16 and 4 more; the
+// wavefronts take a row each then.
+template <int D>
+__device__ __forceinline__ void finish_rows(const Args& p, const Part& r, int row0, int n_rows,
+                                            const State<D>& states, const State<D>& record, int W,
+                                            int wave, int lane) {
   constexpr int kPer = D / 64;  // columns of a lane
-  // (of MOST states, the last one's again behind it: reads that wait for nothing)
-  Joined j{kNone, -0x1p30f};
-  float refs[MOST], exps[MOST], sum = 0.0f, acc[kPer];
+  const int mine = min(lane & 15, states.rows - 1);
+  float ref[2], exp[2], sum[2], f[2];
 #pragma unroll
-  for (int v = 0; v < MOST; ++v) {
+  for (int u = 0; u < 2; ++u) {
+    const int v = (lane >> 4) + 4 * u;
     const State<D> x = state<D>(states.at, min(v, W - 1), states.rows);
-    refs[v] = x.ref(rr16);
-    exps[v] = x.exp(rr16);
-    j.ref = fmaxf(j.ref, refs[v]);
+    ref[u] = v < W ? x.ref(mine) : kNone;
+    exp[u] = x.exp(mine);
+    sum[u] = x.sum(mine);
   }
+  Joined j{fmaxf(ref[0], ref[1]), -0x1p30f};
+  j.ref = fmaxf(j.ref, __shfl_xor(j.ref, 16, 64));
+  j.ref = fmaxf(j.ref, __shfl_xor(j.ref, 32, 64));
+  float all = 0.0f;
 #pragma unroll
-  for (int v = 0; v < MOST; ++v)
-    if (refs[v] > kNone) j.exp = fmaxf(j.exp, ceilf(refs[v] - j.ref) + exps[v]);
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
-#pragma unroll
-  for (int v = 0; v < MOST; ++v) {
-    if (v >= W) break;
-    const State<D> x = state<D>(states.at, v, states.rows);
-    const float f = factor(refs[v], exps[v], j);
-    sum += x.sum(rr16) * exp2_(refs[v] - j.ref);
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) acc[c] += x.acc(rr16)[lane * kPer + c] * f;
+  for (int u = 0; u < 2; ++u) {
+    if (ref[u] > kNone) j.exp = fmaxf(j.exp, ceilf(ref[u] - j.ref) + exp[u]);
+    all += (lane >> 4) + 4 * u < W ? sum[u] * exp2_(ref[u] - j.ref) : 0.0f;
   }
-  if (r.parts == 1) {
-    const int i = rr / p.a.G, hq = rr - i * p.a.G;
-    float* out = p.a.out +
-                 (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
+  j.exp = fmaxf(j.exp, __shfl_xor(j.exp, 16, 64));
+  j.exp = fmaxf(j.exp, __shfl_xor(j.exp, 32, 64));
+  all += __shfl_xor(all, 16, 64);
+  all += __shfl_xor(all, 32, 64);
 #pragma unroll
-    for (int c = 0; c < kPer; ++c) out[c] = r.s.bad ? NAN : finished(acc[c], sum, j.exp);
-  } else {
-    if (lane == 0) {
-      record.ref(rr) = j.ref;
-      record.sum(rr) = sum;
-      record.exp(rr) = j.exp;
+  for (int u = 0; u < 2; ++u) f[u] = factor(ref[u], exp[u], j);
+  const float over = r.s.bad ? NAN : all == 0.0f ? 0.0f : 1.0f / all;
+  auto of = [&](float x, int l) {  // lane l's x
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
+  };
+  for (int rr16 = wave; rr16 < n_rows; rr16 += W) {
+    float acc[kPer];
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) acc[c] = 0.0f;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+      if (v >= W) break;
+      const float fv = of(f[v / 4], rr16 + 16 * (v % 4));
+      const float* x = state<D>(states.at, v, states.rows).acc(rr16) + lane * kPer;
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) acc[c] += x[c] * fv;
     }
+    const int rr = row0 + rr16, e = (int)of(j.exp, rr16);
+    if (r.parts == 1) {
+      const float by = of(over, rr16);
+      const int i = (int)((uint32_t)rr * p.magic >> 16), hq = rr - i * p.a.G;
+      float* out = p.a.out +
+                   (((int64_t)(r.s.begin + r.i0 + i) * p.a.H + r.h) * p.a.G + hq) * D + lane * kPer;
 #pragma unroll
-    for (int c = 0; c < kPer; ++c) record.acc(rr)[lane * kPer + c] = acc[c];
+      for (int c = 0; c < kPer; ++c) out[c] = ldexpf(acc[c] * by, e);
+    } else {
+      if (lane == 0) {
+        record.ref(rr) = of(j.ref, rr16);
+        record.sum(rr) = of(all, rr16);
+        record.exp(rr) = of(j.exp, rr16);
+      }
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) record.acc(rr)[lane * kPer + c] = acc[c];
+    }
   }
 }
 
@@ -743,6 +794,10 @@ void main_kernel(Args p) {
     wv.begin(r, from, to, queries);
     wv.run(r, from, to);
   }
+  if (W == 1 && r.parts == 1) {
+    wv.finish(r);
+    return;
+  }
   const State<D> record = state<D>(p.a.ws, blockIdx.x, p.rows);
   const int n_rows = r.n_tokens * p.a.G, rows16 = min(p.rows, 16);
 #pragma unroll
@@ -750,8 +805,8 @@ void main_kernel(Args p) {
     __syncthreads();  // (what was in LDS has been read)
     wv.store(group, state<D>(states, wave, rows16));
     __syncthreads();
-    for (int rr16 = wave; rr16 < min(16, n_rows - 16 * group); rr16 += W)
-      finish_row<D, most_waves(R, D)>(p, r, group * 16 + rr16, rr16, state<D>(states, 0, rows16), record, W, lane);
+    finish_rows<D>(p, r, 16 * group, min(16, n_rows - 16 * group), state<D>(states, 0, rows16),
+                   record, W, wave, lane);
   }
 }
 
@@ -833,7 +888,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Args p) {
             for (int c = 0; c < kPer; ++c) acc[c] += joined[v][3 + lane * kPer + c] * f;
           }
         }
-        const int i = (int)((uint32_t)rr / (uint32_t)p.a.G), hq = rr - i * p.a.G;
+        const int i = (int)((uint32_t)rr * p.magic >> 16), hq = rr - i * p.a.G;
         float* out = p.a.out + (((int64_t)(row + i) * p.a.H + h) * p.a.G + hq) * D + lane * kPer;
 #pragma unroll
         for (int c = 0; c < kPer; ++c) out[c] = finished(acc[c], sum, j.exp);
@@ -870,8 +925,8 @@ Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pa
   p.waves = most_waves(p.R, d);
   if (p.R == 1)
     while (p.waves > 2 && (p.cut ? k : (items + kCu - 1) / kCu) * p.waves > held) p.waves /= 2;
-  else if (room <= 1024 && items >= 8 * kCu)
-    p.waves = 2;
+  else if (!p.cut && (2 * items >= 3 * kCu * held || (2 * items >= kCu * held && room <= 1024)))
+    p.waves = 1;
   p.least = !p.cut ? (int)std::max<int64_t>(room, 32) : items >= kCu ? 2048 : items >= kCu / 2 ? 1024 : 512;
   p.target = (float)target;
   p.parts = (int)(items + (p.cut ? target : 0));
@@ -923,7 +978,8 @@ int launch_page_attn(const PageAttn& a, void* stream) {
   const pa::Plan pl = pa::plan(a.n_seqs, a.n_rows, !a.starts, a.H, a.G, a.max_pages, a.page, a.d);
   const pa::Args p{a,        16 * pl.R / a.G, __builtin_ctz(a.page),
                    pl.least, pl.target,       a.scale * 1.44269504088896341f,
-                   pl.rows,  pl.cut,          pl.parts};
+                   pl.rows,  pl.cut,          pl.parts,
+                   (65536u + (uint32_t)a.G - 1) / (uint32_t)a.G};
   switch (a.q_dtype) {
     case FIBQ_F32: return pa::launch_codes<float>(p, pl, st);
     case FIBQ_F16: return pa::launch_codes<f16_t>(p, pl, st);

@@ -63,8 +63,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
   __syncthreads();
   // A thread has one piece of V elements (or pairs) of every head that it visits, so a
   // row's angles stay in its registers; kHeads loads are on their way at once.  What lies
-  // behind the turned part is copied VT elements at a time, the last piece over the one
-  // before it.
+  // behind the turned part is copied VT elements at a time (the last piece over the one
+  // before it): in the same loop where pieces are alike, so that a row is read as a whole.
   constexpr int kHeads = HALF && V > 1 ? 2 : 4;
   const int heads = a.q_heads + a.k_heads, tail = a.d - a.rot;
   const int turned = HALF ? half / V : a.rot / V;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
     if (slot >= at_once) continue;
     const bool turns = c < turned;
     const int at = turns ? c * V : min(a.rot + (c - turned) * VT, a.d - VT);
-    if (!turns) {
+    if (V != VT && !turns) {
       for (int i0 = slot; i0 < rows * heads; i0 += kHeads * at_once) {
         Vec<T, VT> x[kHeads];
         T* to[kHeads];
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
       float2 w[kAngles];
 #pragma unroll
       for (int e = 0; e < kAngles; ++e)
-        w[e] = turn[r * half + (HALF ? at : at / 2) + e];
+        w[e] = turns ? turn[r * half + (HALF ? at : at / 2) + e] : make_float2(1.0f, 0.0f);
       const int64_t row = row0 + r;
       const T *q = (const T*)a.q + row * a.q_row, *k = (const T*)a.k + row * a.k_row;
       T *qo = (T*)a.q_out + row * a.qo_row, *ko = (T*)a.k_out + row * a.ko_row;
@@ -111,14 +111,16 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
           const int h = min(h0 + u * at_once, heads - 1);
           const T* x = (h < a.q_heads ? q + h * a.q_head : k + (h - a.q_heads) * a.k_head) + at;
           x0[u] = load<T, V>(x);
-          if constexpr (HALF) x1[u] = load<T, V>(x + half);
+          if constexpr (HALF) x1[u] = turns ? load<T, V>(x + half) : x0[u];
         }
 #pragma unroll
         for (int u = 0; u < kHeads; ++u) {
           const int h = h0 + u * at_once;
           if (h >= heads) break;
           T* y = (h < a.q_heads ? qo + h * a.qo_head : ko + (h - a.q_heads) * a.ko_head) + at;
-          if constexpr (HALF) {
+          if (!turns) {
+            store<T, V>(y, x0[u]);
+          } else if constexpr (HALF) {
             Vec<T, V> y0, y1;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -153,16 +155,16 @@ int rope_typed(const Rope& a, hipStream_t st) {
   const int64_t grid = (a.n_rows + tile - 1) / tile;
   const int tail = a.d - a.rot;
   auto go = [&](auto kernel) { kernel<<<grid, kRopeThreads, 0, st>>>(a, tile); };
-  const bool wide = tail == 0 || tail >= V;
+  const bool wide = tail == 0 || tail >= V, whole = tail % V == 0;
   if (a.layout == FIBQ_ROPE_HALF) {
-    if (half % V == 0 && wide)
+    if (half % V == 0 && whole)
       go(rope_kernel<T, V, V, true>);
     else if (wide)
       go(rope_kernel<T, 1, V, true>);
     else
       go(rope_kernel<T, 1, 1, true>);
   } else {
-    if (a.rot % V == 0 && wide)
+    if (a.rot % V == 0 && whole)
       go(rope_kernel<T, V, V, false>);
     else if (wide)
       go(rope_kernel<T, 2, V, false>);
