@@ -54,6 +54,7 @@ struct Args {
   int rows;         // query rows of an item, at most
   int cut;          // items may be cut
   int parts;        // at most
+  int planned;      // the parts before each sequence are in the workspace
   uint32_t magic;   // ceil(2^16 / G): x / G = x magic >> 16 for the rows of an item
 };
 
@@ -90,6 +91,18 @@ struct Part {
   int i0, n_tokens;  // its query tokens
   int seen, from, to;
 };
+// A part's tokens from all items' tokens: about as many parts as fill the card.
+__device__ __forceinline__ int part_size(const Args& p, float tokens) {
+  // (a little more than the exact quotient, so that rounding never makes a part too many)
+  const float share = tokens * (float)p.a.H * 1.001f / p.target;
+  return (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
+}
+__device__ __forceinline__ int parts_of_item(const Seq& s, int part) {  // part 0: items are whole
+  return part ? max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part)) : 1;
+}
+// parts before each of the sequences, their number, and a part's tokens
+__device__ __forceinline__ int* plan_of(const Args& p);
+
 // Part w of all, in every thread of the workgroup.  Parts are in the order of sequences,
 // tiles from the last (a causal sequence's longest), parts, heads.  False: there is none.
 __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds) {
@@ -100,6 +113,18 @@ __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds)
   if (!p.cut && !p.a.starts) {  // one item, one part for each sequence and head
     g = (int)((uint32_t)w / H);
     first = g * (int)H;
+  } else if (p.planned) {  // the last sequence with at most w parts before it
+    const int* before = plan_of(p);
+    if (w >= before[n]) return false;
+    part = before[n + 1];
+    g = 0;
+    for (int width = n; width > 1;) {
+      const int step = (width + 63) >> 6, at = lane * step;
+      const int to = __popcll(__ballot(at < width && before[min(g + at, n)] <= w)) - 1;
+      g += to * step;
+      width = min(step, width - to * step);
+    }
+    first = before[g];
   } else {
     Seq s = tid < n ? sequence(p, tid) : Seq{};
     if (p.cut) {
@@ -113,9 +138,7 @@ __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds)
       __syncthreads();
       tokens = 0.0f;
       for (int v = 0; v < W; ++v) tokens += __int_as_float(lds[v]);
-      // (a little more than the exact quotient, so that rounding never makes a part too many)
-      const float share = tokens * (float)p.a.H * 1.001f / p.target;
-      part = (max(p.least_part, (int)fminf(share, 1073741760.0f)) + 31) & ~31;
+      part = part_size(p, tokens);
       __syncthreads();
     }
     int* found = lds + W;  // sequence, parts before it
@@ -125,8 +148,7 @@ __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds)
     for (int g0 = 0; g0 < n; g0 += 64 * W) {
       const int at = g0 + tid;
       if (g0 > 0) s = at < n ? sequence(p, at) : Seq{};
-      const int parts = part ? max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part)) : 1;
-      const int mine = at < n ? s.tiles * parts * p.a.H : 0;
+      const int mine = at < n ? s.tiles * parts_of_item(s, part) * p.a.H : 0;
       int upto = mine;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -153,11 +175,12 @@ __device__ __forceinline__ bool part_at(const Args& p, int w, Part* r, int* lds)
     first = uni(found[1]);
     part = uni(part);
   }
+  g = uni(g);
   const Seq s = uni(sequence(p, g));
   uint32_t i = (uint32_t)(w - first);
   r->s = s;
   r->g = g;
-  r->parts = part ? max(1, (int)((uint32_t)(s.len + part - 1) / (uint32_t)part)) : 1;
+  r->parts = parts_of_item(s, part);
   if (i >= (uint32_t)s.tiles * (uint32_t)r->parts * H) return false;  // (counts that overflowed)
   r->h = (int)(i % H);
   i /= H;
@@ -198,6 +221,59 @@ struct Join {
 };
 __device__ __forceinline__ Join* joins(const Args& p, int d) {
   return (Join*)((float*)p.a.ws + (int64_t)p.parts * state_floats(p.rows, d));
+}
+
+__device__ __forceinline__ int* plan_of(const Args& p) {
+  return p.cut ? (int*)(joins(p, p.a.d) + p.parts) : (int*)p.a.ws;
+}
+
+// The parts before every sequence, once for all workgroups where each would take longer to
+// sum them up itself: above 512 sequences (tables of 16384 tokens; 64 sequences to 2048
+// tokens 16.9 us without and 19.4 with this launch, 512 to 1000 42.6 and 44.7, 2048 to 500
+// 91.8 and 51.7).
+constexpr int kPlanned = 512;
+__global__ __launch_bounds__(1024) void plan_kernel(Args p) {
+  __shared__ float tokens_of[16];
+  __shared__ uint32_t sums[2][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)p.a.n_seqs;
+  int* before = plan_of(p);
+  float tokens = 0.0f;
+  if (p.cut) {
+    for (int g = tid; g < n; g += 1024) {
+      const Seq s = sequence(p, g);
+      tokens += (float)s.tiles * (float)s.len;
+    }
+    tokens = wave_sum(tokens);
+    if (lane == 0) tokens_of[wave] = tokens;
+    __syncthreads();
+    tokens = 0.0f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) tokens += tokens_of[v];
+  }
+  const int part = p.cut ? part_size(p, tokens) : 0;
+  auto plus = [](uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); };
+  uint32_t all = 0;
+  for (int g0 = 0, round = 0; g0 < n; g0 += 1024, round ^= 1) {
+    const int g = g0 + tid;
+    const Seq s = g < n ? sequence(p, g) : Seq{};
+    uint32_t upto = g < n ? (uint32_t)(s.tiles * parts_of_item(s, part) * p.a.H) : 0;
+    const uint32_t mine = upto;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto = plus(upto, y);
+    }
+    if (lane == 63) sums[round][wave] = upto;
+    __syncthreads();
+    uint32_t here = all;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      if (v < wave) here = plus(here, sums[round][v]);
+      all = plus(all, sums[round][v]);
+    }
+    if (g < n) before[g] = (int)(plus(here, upto) - mine);
+  }
+  if (tid == 0) before[n] = (int)all, before[n + 1] = part;
 }
 
 // -------------------------------------------------------------- operators --
@@ -905,7 +981,7 @@ struct Plan {
   int parts, joins;     // parts, at most; workgroups that join
   int least;            // tokens of a part, at least
   float target;
-  bool cut;
+  bool cut, planned;
   size_t bytes;
 };
 Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pages, int page, int d) {
@@ -920,7 +996,8 @@ Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pa
   // workgroups for each compute unit: parts, or items that are not cut
   int64_t k = std::min<int64_t>(4, (items + kCu / 2 - 1) / (kCu / 2));
   // (an item's last part is half empty on the average)
-  int64_t target = std::max(k * kCu - items / 2, items / 2);
+  int64_t target = k * kCu - items / 2;
+  if (target < kCu / 2) target = kCu;  // (items enough: only those far above the average are cut)
   if (p.R == 2) target = kCu * held / 4;
   p.waves = most_waves(p.R, d);
   if (p.R == 1)
@@ -932,7 +1009,9 @@ Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pa
   p.parts = (int)(items + (p.cut ? target : 0));
   while (p.waves > 1 && (int64_t)p.parts * p.waves >= 1 << 26) p.waves /= 2;  // (a grid's 2^32 threads)
   p.joins = std::min(p.parts, p.R == 1 ? 251 : 509);
+  p.planned = n_seqs > kPlanned && (p.cut || !one);
   p.bytes = p.cut ? (size_t)p.parts * (state_floats(p.rows, d) * 4 + sizeof(Join)) : 0;
+  if (p.planned) p.bytes += (size_t)(n_seqs + 2) * 4;
   return p;
 }
 
@@ -940,8 +1019,13 @@ template <typename T, int CODES, int D, int R>
 int launch(const Args& p, const Plan& pl, hipStream_t st) {
   const size_t words = std::max((size_t)pl.waves * state_floats(std::min(pl.rows, 16), D), (size_t)part_lds(pl.waves)) * 4;
   const size_t lds = R == 1 ? words : std::max(words, 256 + (size_t)R * D * (sizeof(T) == 4 ? 64 : 32) + 128 * R);
+  int rc = 0;
+  if (pl.planned) {
+    plan_kernel<<<1, 1024, 0, st>>>(p);
+    if ((rc = (int)hipGetLastError()) != 0) return rc;
+  }
   main_kernel<T, CODES, D, R><<<pl.parts, 64 * pl.waves, lds, st>>>(p);
-  int rc = (int)hipGetLastError();
+  rc = (int)hipGetLastError();
   if (rc != 0 || !pl.cut) return rc;
   constexpr int kWide = R == 1 ? 4 : 1;
   merge_kernel<D, kWide><<<dim3(pl.joins, kWide > 1 ? pl.rows : 1), 256, 0, st>>>(p);
@@ -979,6 +1063,7 @@ int launch_page_attn(const PageAttn& a, void* stream) {
   const pa::Args p{a,        16 * pl.R / a.G, __builtin_ctz(a.page),
                    pl.least, pl.target,       a.scale * 1.44269504088896341f,
                    pl.rows,  pl.cut,          pl.parts,
+                   pl.planned,
                    (65536u + (uint32_t)a.G - 1) / (uint32_t)a.G};
   switch (a.q_dtype) {
     case FIBQ_F32: return pa::launch_codes<float>(p, pl, st);
