@@ -490,8 +490,13 @@ size_t fibq_attn_cache8_workspace_bytes(int64_t n_seqs, int64_t n_rows, int H, i
  * tokens NaN.  Rows that belong to no sequence are left as they are; a sequence
  * whose starts are not 0 <= starts[g] <= starts[g + 1] <= n_rows has none, and rows
  * that two sequences claim are open.  What
- * lies behind a sequence's last token is never used, whatever it holds.  Scores
- * are limited to +-2^126, so that finite queries and elements give finite rows.
+ * lies behind a sequence's last token is never used, whatever it holds.  A score's
+ * factors (scale, K scale, the row's power of two) are limited to 2^94 in magnitude, so
+ * that finite queries and elements give finite rows; a row of queries that holds a NaN
+ * or an infinity is NaN, and so are rows that see a page whose scale (times `scale`, for
+ * K) is no finite number.  Codes 0x7f and 0xff of E4M3 (NaN) among a sequence's tokens
+ * make the rows of that sequence open.  lens, starts and table are not written while the
+ * call runs (else nothing is accessed out of range, but rows are open).
  * 1 <= G <= 16.  workspace: device, at least
  * fibq_attn_cache8_workspace_bytes(...) bytes, 256-byte aligned, else
  * FIBQ_EWORKSPACE; calls that overlap in time need one each. */

@@ -20,6 +20,14 @@
 // largest weight) move only when a weight leaves its range, so the common path has no
 // exchange between lanes.  Parts of an item that was cut leave a state each, which a
 // second launch joins.
+//
+// What bounds it.  Single tokens over long sequences: memory (48 sequences to 32768 tokens
+// x 4 heads, 425 MB: 92 us, 4.6 TB/s; one of 131072 x 8 heads, d = 128, 269 MB: 56 us, 4.8
+// TB/s; a large copy moves 4.9).  Row tiles: vector and matrix instructions (8 chunks to
+// 512 tokens over up to 4096, 67 GFLOP: 148 us; vector instructions, matrix ones among them,
+// are issued in 55 % of the SIMDs' cycles).  Few short items: the chain of launch,
+// lengths, table, pages and the wait for each next tile (64 sequences to 2048 tokens: 12
+// us for 35 MB).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -404,7 +412,8 @@ struct Wave {
                          CB);
   }
 
-  // Row rr's queries, and its tokens' number if it is none of the item's.
+  // Row rr's queries and which of the item's tokens it belongs to (the first row's, if the
+  // item has no such row).
   __device__ __forceinline__ const T* row_of(const Part& r, int rr, int* i) const {
     const PageAttn& a = p.a;
     const bool used = rr < r.n_tokens * a.G;
@@ -413,12 +422,12 @@ struct Wave {
     return (const T*)a.q + (((int64_t)(r.s.begin + r.i0 + *i) * a.H + r.h) * a.G + hq) * D;
   }
   // x 2^-e in QP binary16 parts
-  __device__ __forceinline__ void parts_of(const T* y, bool used, int e, h8* to, int stride) const {
+  __device__ __forceinline__ void parts_of(const T* y, bool used, int e, h8* to) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float z = used ? ldexpf(to_float(y[i]), -e) : 0.0f;
       to[0][i] = (_Float16)z;
-      if constexpr (QP == 2) to[stride][i] = (_Float16)(z - (float)to[0][i]);
+      if constexpr (QP == 2) to[1][i] = (_Float16)(z - (float)to[0][i]);
     }
   }
   __device__ __forceinline__ void look(const T* y, float* big, int* lost_) const {
@@ -461,7 +470,7 @@ struct Wave {
     for (int m = 0; m < KJ; ++m) {
       const int d8 = s * KJ + m, j = d8 >> 3, kg = (d8 & 7) >> 1;
       h8 part[QP];
-      parts_of(y[m], used, e, part, 1);
+      parts_of(y[m], used, e, part);
 #pragma unroll
       for (int u = 0; u < QP; ++u)
         to[(((rr >> 4) * 2 * KJ + 2 * j + (d8 & 1)) * QP + u) * 64 + kg * 16 + (rr & 15)] = part[u];
@@ -513,7 +522,7 @@ struct Wave {
       lost[0] = l;
       qe[0] = exponent(big, l);
 #pragma unroll
-      for (int c = 0; c < 2 * KJ; ++c) parts_of(y[c], row16 < n_rows && !l, qe[0], q[0][c], 1);
+      for (int c = 0; c < 2 * KJ; ++c) parts_of(y[c], row16 < n_rows && !l, qe[0], q[0][c]);
     }
   }
   __device__ __forceinline__ void clear() {
@@ -888,7 +897,9 @@ void main_kernel(Args p) {
 
 // Joins the states of the items that were cut: a wavefront for each row or, where items
 // have few rows and many parts, four (WIDE).  What it reads has just been written by
-// other XCDs, so each read takes long: many are on their way at once.
+// other XCDs, so each read takes long: many are on their way at once.  Bound by that chain
+// (list, headers, values) and its launch: 6.7 us for 192 items to 32768 tokens, 4.8 for 8 of
+// 131072, d = 128.
 template <int D, int WIDE>
 __global__ __launch_bounds__(256) void merge_kernel(Args p) {
   constexpr int kPer = D / 64, kBatch = 8;
@@ -984,21 +995,39 @@ struct Plan {
   bool cut, planned;
   size_t bytes;
 };
+// What the host knows: sizes, and how long sequences may be (`room`), not how long they
+// are.  Times below are in us, e4m3 codes, bfloat16 queries, G = 8 (d = 64) or 4 (128).
 Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pages, int page, int d) {
   Plan p{};
+  // Tiles of 32 rows where a sequence has more than 16 (64 sequences of 2048 tokens x 4
+  // heads, d = 64; rows of a head, then with 16-row and with 32-row tiles: 16 17.2 and
+  // 23.3, 24 26.3 and 24.1, 32 26.6 and 24.9, 64 34.5 and 32.0; d = 128: 30.5 and 32.6,
+  // 37.8 and 33.3, 38.3 and 34.1, 61.0 and 44.1).
   p.R = n_rows * G >= 24 * std::max<int64_t>(1, n_seqs) ? 2 : 1;
   const int64_t room = max_pages * page, tile = 16 * p.R / G;
   p.rows = one ? G : (int)tile * G;
   const int64_t items = (one ? n_rows : n_rows / tile + std::min(n_seqs, n_rows)) * H;
-  p.cut = room > (items >= kCu ? 4096 : 2048);
+  // Items are cut only where they may be long or are few, since cutting costs a sum over
+  // the lengths in every workgroup and a launch (whole and cut: 4 items to 2048 tokens
+  // 11.6 and 13.2, to 4096 17.6 and 13.5; 64 to 2048 12.2 and 14.8, to 4096 18.4 and 16.1;
+  // 256 to 4096 19.0 and 27.7, to 8192 37.3 and 43.3, to 16384 70.3 and 73.5).
+  p.cut = room > (items >= kCu ? 8192 : 2048);
   // wavefronts that a compute unit holds at once
   const int64_t held = 4 * waves_of_simd(p.R, d);
-  // workgroups for each compute unit: parts, or items that are not cut
+  // Workgroups for each compute unit: all parts run at once, and each compute unit has as
+  // many.  An item's last part is half empty on the average, so half as many parts as
+  // items are kept back, and k grows with the items to keep that small (192 items to
+  // 32768 tokens, 1, 2 and 3 for a compute unit: 141, 94 and 94; 8 items of 131072, d = 128: 57.6, 58.9 and 61.0.)
   int64_t k = std::min<int64_t>(4, (items + kCu / 2 - 1) / (kCu / 2));
-  // (an item's last part is half empty on the average)
   int64_t target = k * kCu - items / 2;
   if (target < kCu / 2) target = kCu;  // (items enough: only those far above the average are cut)
   if (p.R == 2) target = kCu * held / 4;
+  // Wavefronts: as many to a workgroup as keep a compute unit's places filled by its
+  // items (64 sequences to 2048 tokens x 4 heads, 4, 8 and 16: 15.7, 13.5 and 14.2; 8
+  // items of 131072 tokens, d = 128, 2, 4 and 8: 69.3, 56.1 and 57.1); one for row tiles
+  // that fill the card by themselves, whose states then need no joining (4 prompts of 1000
+  // tokens x 4 heads, 1, 2 and 4: 72.9, 77.6 and 90.1; 8 chunks to 512 tokens over up to
+  // 4096, d = 128: 161, 173 and 149).
   p.waves = most_waves(p.R, d);
   if (p.R == 1)
     while (p.waves > 2 && (p.cut ? k : (items + kCu - 1) / kCu) * p.waves > held) p.waves /= 2;
@@ -1008,6 +1037,7 @@ Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pa
   p.target = (float)target;
   p.parts = (int)(items + (p.cut ? target : 0));
   while (p.waves > 1 && (int64_t)p.parts * p.waves >= 1 << 26) p.waves /= 2;  // (a grid's 2^32 threads)
+  // (a prime number of them: first parts lie at regular distances in the list)
   p.joins = std::min(p.parts, p.R == 1 ? 251 : 509);
   p.planned = n_seqs > kPlanned && (p.cut || !one);
   p.bytes = p.cut ? (size_t)p.parts * (state_floats(p.rows, d) * 4 + sizeof(Join)) : 0;
