@@ -181,7 +181,7 @@ int rope_typed(const Rope& a, hipStream_t st) {
 // workgroup runs them; pages given back are placed first, since what it may hand out
 // depends on their number.  Sums stop at 2^31 - 1, which is more than any bound here.
 // Bound by that workgroup's sums and barriers and the launch: 256 requests 8.1 us (the
-// kernel 5.8), 64 requests of 262144 rows 10.1 (5.8, and 3.4 for the rows' launch); 13.6
+// kernel 7.8), 64 requests of 262144 rows 10.1 (5.9, and 4.3 for the rows' launch); 13.6
 // and 15.6 before sums over up to 1024 requests took one pass.
 constexpr int kScan = 1024;
 constexpr int kStaged = 4096;  // requests whose results stay in LDS for the rows' search
@@ -380,9 +380,11 @@ __global__ __launch_bounds__(256) void place_kernel(Resize a, int stage) {
 // the codes' range; a page keeps the larger of that and of its scale so far,
 // and where that grows, the codes before the run are rounded again.  With
 // powers of two x / s and code * s_old / s are exact, so each value is rounded
-// once per growth of its page's scale.  36000 rows x 8 heads, d = 128, 224 MB: 60 us,
-// 3.7 TB/s of the 4.9 that a large copy moves; 104 before rows were held in registers
-// between the search for the largest and the rounding.  64 rows x 4 heads: 6.8 us, the call.
+// once per growth of its page's scale.  36000 rows x 8 heads, d = 128, pages of 32, 224 MB:
+// 58 us, 3.9 TB/s of the 4.9 that a large copy moves; 104 before rows were held in registers
+// between the search for the largest and the rounding.  Vector instructions take much of
+// it, but fewer of them (integer maxima of two at once, a rounding by one fused operation)
+// changed nothing.  64 rows x 4 heads: 6.8 us, the call.
 __device__ __forceinline__ float least_scale(uint32_t amax_bits, int codes) {
   if (amax_bits == 0) return 0.0f;
   if (amax_bits >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
@@ -559,7 +561,11 @@ int write_typed(const Write& a, hipStream_t st) {
                                            std::max<int64_t>(1, a.n_rows * a.H * 2 / 4096));
   const int64_t x = (a.n_rows + chunk - 1) / chunk;
   const dim3 grid((unsigned)x, a.H, 2);
-  const int threads = chunk == 1 ? 64 : 256, shift = __builtin_ctz(a.page);
+  // Threads: four pieces of a page for each, so that a small page has one wavefront, which
+  // looks over its slots once and waits at no barrier (16 prompts to 4096 tokens x 8 heads,
+  // int8 or e4m3; 256 threads always, then so: pages of 16, d = 64 83 and 33 us, of 16, d =
+  // 128 88 and 57, of 32, d = 128 64 and 59, of 64, d = 64 31 and 28; 64 and 128 alike).
+  const int threads = chunk == 1 ? 64 : std::min(256, std::max(64, a.page * a.d / 32)), shift = __builtin_ctz(a.page);
   const bool few = a.page * a.d <= 2 * 8 * threads;  // pieces of a page for each thread
   switch (a.d) {
     case 64:

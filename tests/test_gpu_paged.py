@@ -280,6 +280,34 @@ def test_cache8_write_token_by_token(device, kind):
         run_write(device, x[:, 0], x[:, 1], [32 + t], kind, kp, ks, vp, vs)
 
 
+@pytest.mark.parametrize("kind", list(CODES))
+@pytest.mark.parametrize("H,page,d,n,dtype", [
+    (8, 16, 64, 3000, "bf16"), (16, 16, 128, 2100, "fp16"), (8, 32, 128, 2500, "fp32"),
+    (32, 128, 64, 4100, "bf16"), (4, 64, 256, 6000, "fp16"), (8, 64, 64, 1500, "fp32"), (2, 16, 256, 5000, "bf16")])
+def test_cache8_write_many_rows(device, kind, H, page, d, n, dtype):
+    """Prompts of all lengths, from the middle of a page on, with rows and tokens left out."""
+    rng = np.random.default_rng(n + d)
+    slots, n_pages = [], 0
+    while len(slots) < n:
+        begin = int(rng.integers(page)) if rng.random() < 0.7 else 0
+        tokens = np.arange(begin, begin + int(rng.integers(1, 5 * page)))
+        if rng.random() < 0.3:  # slots of a run need not follow on each other
+            tokens = tokens[rng.random(len(tokens)) < 0.8]
+        slots += [(n_pages, int(t)) for t in tokens]
+        n_pages += 6
+        if rng.random() < 0.4:
+            slots += [None] * int(rng.integers(1, 4))
+    perm = rng.permutation(n_pages)
+    slots = [-1 if s is None else int(perm[s[0] + s[1] // page]) * page + s[1] % page for s in slots[:n]]
+    kp, ks = pools(device, rng, n_pages, H, page, d, kind)
+    vp, vs = pools(device, rng, n_pages, H, page, d, kind)
+    g = torch.Generator(device=device).manual_seed(d)
+    x = torch.randn(n, 2, H, d, generator=g, device=device) * 2.0 ** torch.randint(
+        -6, 6, (n, 1, 1, 1), generator=g, device=device)
+    x = x.to(TYPES[dtype])
+    run_write(device, x[:, 0], x[:, 1], slots, kind, kp, ks, vp, vs)
+
+
 # ------------------------------------------------------------ attn_cache8 --
 def make_cache(rng, lens, H, page, d, kind, spare=3, spread=0):
     """Pages in no order; what no token owns holds codes and scales that are no numbers."""
