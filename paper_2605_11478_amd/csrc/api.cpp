@@ -504,7 +504,7 @@ static bool strides_known(int64_t row, int64_t head) {
 }
 // ... and no element twice (outputs).
 static bool strides_apart(int64_t n, int heads, int d, int64_t row, int64_t head) {
-  return (head >= d && row >= (heads - 1) * head + d) || (row >= d && head >= (n - 1) * row + d);
+  return (head >= d && row >= (heads - 1) * head + d) || (row >= d && head >= d && (head - d) / row >= n - 1);
 }
 
 int fibq_rope(const void* q, const void* k, int dtype, int64_t n_rows, int q_heads, int k_heads,

@@ -164,6 +164,13 @@ def test_rope_status(kw):
     assert _status("fibq_rope", ROPE, kw) == fq.FIBQ_EINVAL
 
 
+@pytest.mark.parametrize("kw", [dict(n=(1 << 24) + 1, qoh=15, qor=1 << 39),
+                                dict(n=(1 << 24) + 1, koh=15, kor=1 << 39)], ids=str)
+def test_rope_status_far_strides(kw):
+    """An output that holds elements twice, whose extent is more than 64 bits take."""
+    assert _status("fibq_rope", ROPE, kw) == fq.FIBQ_EINVAL
+
+
 RESIZE = dict(table=256, lens=512, grow=768, n=2, mp=4, page=16, n_pages=9, free=1024, cap=9, n_free=1280,
               n_rows=3, new_lens=4096, starts=4352, slots=4608, pos=4864, new_free=5120, ws=8192, wsb=1 << 20)
 
