@@ -413,7 +413,7 @@ int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t*
  * and strides) and has no memory in common with any other tensor.  positions:
  * device int32 [n_rows], any value; freqs: device double [rot / 2], radians per
  * position.  d even, 2 <= d <= 512, rot even, 2 <= rot <= d; heads in all at
- * most 2048; fewer than 2^31 rows. */
+ * most 2048; at most 2^25 rows. */
 int fibq_rope(const void* q, const void* k, int dtype, int64_t n_rows, int q_heads, int k_heads,
               int d, int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride,
               int64_t k_head_stride, const int32_t* positions, const double* freqs, int rot,

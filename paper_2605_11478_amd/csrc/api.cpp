@@ -513,7 +513,7 @@ int fibq_rope(const void* q, const void* k, int dtype, int64_t n_rows, int q_hea
               int layout, float scale, int inverse, void* q_out, void* k_out,
               int64_t q_out_row_stride, int64_t q_out_head_stride, int64_t k_out_row_stride,
               int64_t k_out_head_stride, void* stream) {
-  if (!dtype_known(dtype) || n_rows < 0 || n_rows >= (1LL << 31) || q_heads < 1 || k_heads < 0 ||
+  if (!dtype_known(dtype) || n_rows < 0 || n_rows > (1LL << 25) || q_heads < 1 || k_heads < 0 ||
       q_heads > 2048 || k_heads > 2048 || q_heads + k_heads > 2048)
     return FIBQ_EINVAL;
   if (d < 2 || d > 512 || d % 2 != 0 || rot < 2 || rot > d || rot % 2 != 0) return FIBQ_EINVAL;

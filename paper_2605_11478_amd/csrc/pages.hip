@@ -151,6 +151,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
 template <typename T, int V>
 int rope_typed(const Rope& a, hipStream_t st) {
   // rows of a workgroup: as many as its angles fit, but workgroups for every compute unit
+  // (4 to 16 of 2^25 rows, so 2^23 workgroups at most: a grid has fewer than 2^32 threads)
   const int half = a.rot / 2;
   int tile = std::min<int64_t>(std::max(1, kRopeAngles / half), std::max<int64_t>(1, a.n_rows / 1024));
   tile = std::min(tile, 16);

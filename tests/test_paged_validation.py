@@ -171,6 +171,12 @@ def test_rope_status_far_strides(kw):
     assert _status("fibq_rope", ROPE, kw) == fq.FIBQ_EINVAL
 
 
+def test_rope_status_most_rows():
+    """More workgroups than a grid holds are no valid problem."""
+    for n in ((1 << 25) + 1, (1 << 26) + 1, 1 << 30):
+        assert _status("fibq_rope", ROPE, dict(n=n)) == fq.FIBQ_EINVAL
+
+
 RESIZE = dict(table=256, lens=512, grow=768, n=2, mp=4, page=16, n_pages=9, free=1024, cap=9, n_free=1280,
               n_rows=3, new_lens=4096, starts=4352, slots=4608, pos=4864, new_free=5120, ws=8192, wsb=1 << 20)
 
