@@ -48,6 +48,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 constexpr float kLag = 0x1p8f;      // exp2 of what a score may exceed its row's reference by
 constexpr float kTop = 0x1p15f;     // weights stay below (binary16)
 constexpr int kTopBits = 7;         // exponent of a row's largest weight when e is set
+constexpr int kLeast = -160;        // e of a row without weights: any weight that comes leaves its range
 constexpr float kLimit = 0x1p94f;   // of a score's factors: scores stay below 2^126, codes' products being below 2^32
 constexpr float kMost = 0x1p126f;   // of a weight's factor: never infinite, so that 0 stays 0
 constexpr float kNone = -0x1p127f;  // reference of a row that has seen nothing
@@ -531,7 +532,7 @@ struct Wave {
       ref[s] = kNone;
       sum[s] = 0.0f;
       top[s] = 0.0f;
-      e[s] = 0;
+      e[s] = kLeast;
       lost[s] = false;
 #pragma unroll
       for (int c = 0; c < CB; ++c) acc[s][c] = f4{0, 0, 0, 0};
@@ -553,8 +554,8 @@ struct Wave {
     w = fmaxf(w, __shfl_xor(w, 32, 64));
     w = ldexpf(w * a, e[r]);
     w = fmaxf(w, fmaxf(exp2_(big[0] - to) * fabsf(v0), exp2_(big[1] - to) * fabsf(v1)));
-    int ew = e[r];
-    if (w > 0.0f) ew = max(__builtin_amdgcn_frexp_expf(w) - 1 - kTopBits, -100);
+    // (no weight but zeros so far, as of pages of zeros: the first one sets e)
+    const int ew = w > 0.0f ? max(__builtin_amdgcn_frexp_expf(w) - 1 - kTopBits, kLeast) : kLeast;
     const float by = ldexpf(a, e[r] - ew);
     sum[r] *= a;
     top[r] = ldexpf(w, -ew);

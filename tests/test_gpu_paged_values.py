@@ -1,0 +1,46 @@
+"""Attention over the paged 8-bit cache on pages, weights and scores far apart; tolerance
+as in test_gpu_paged.py, derived there.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_11478_amd as fq
+from oracle import paged as opg
+from test_gpu_paged import CODES, TYPES, check_attention, host, make_cache, on
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(device, q, cache, lens, rows, kind, causal=True, scale=0.0):
+    """Attention of q (rows of every sequence) over `cache`; rows None: one each, no starts."""
+    kp, ks, vp, vs, table = cache
+    t = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(device)
+    starts = np.concatenate([[0], np.cumsum([1] * len(lens) if rows is None else rows)]).astype(np.int32)
+    out = fq.attn_cache8(q, on(device, kp, kind), t(ks), on(device, vp, kind), t(vs), t(table),
+                         t(np.asarray(lens, np.int32)), None if rows is None else t(starts), causal=causal,
+                         scale=scale)
+    return host(out), starts
+
+
+# lens, rows (None: one each), H, G, page, d: whole and cut items, one row and row tiles
+FORMS = [([300, 512, 33], None, 2, 8, 16, 64), ([129, 600], [40, 70], 1, 4, 16, 64),
+         ([700, 90], [33, 50], 1, 2, 32, 128), ([200], None, 1, 3, 64, 256), ([9000], None, 1, 4, 64, 128),
+         ([2600, 40], [30, 40], 1, 4, 16, 64), ([5000, 700], None, 2, 8, 16, 64)]
+
+
+@pytest.mark.parametrize("kind", list(CODES))
+@pytest.mark.parametrize("lens,rows,H,G,page,d", FORMS, ids=str)
+@pytest.mark.parametrize("exponent", [0, -12, -20, -100])
+def test_pages_of_zeros_first(device, kind, lens, rows, H, G, page, d, exponent):
+    """Pages of zeros, whose scale is 0, before and between pages of small values."""
+    rng = np.random.default_rng(d - exponent)
+    cache = kp, ks, vp, vs, table = make_cache(rng, lens, H, page, d, kind)
+    for g, t in enumerate(lens):
+        for j in range(-(-t // page)):
+            vs[table[g, j]] *= np.float32(2.0 ** exponent)
+            if (j + 1) * page < t and (j * page < 64 or rng.random() < 0.6):
+                vp[table[g, j]], vs[table[g, j]] = 0, 0
+    q = torch.randn(len(lens) if rows is None else sum(rows), H * G, d, device=device) * 0.1
+    out, starts = attend(device, q, cache, lens, rows, kind)
+    check_attention(out, host(q), *cache, lens, starts, True, kind)
