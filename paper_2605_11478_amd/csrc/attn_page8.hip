@@ -10,8 +10,11 @@
 //                                     (exact), B = queries, scaled by a power of two per
 //                                     row; two binary16 parts for float queries
 //   p = exp2(S f - ref), w = p v 2^-e  f: scale log2(e) and the page's K scale, v: its V
-//                                     scale; w in two binary16 parts (22 bits)
-//   O[r][:] += w[r][t] V[t][:]        the same instruction, B = codes as binary16
+//                                     scale
+//   O[r][:] += w[r][t] V[t][:]        v_mfma_f32_16x16x32_bf16, A = w in three bfloat16
+//                                     parts (its 24 bits, at any exponent: two binary16
+//                                     parts lose those of a weight far below its row's
+//                                     largest, whose values may be 0), B = codes (exact)
 //
 // Four tokens of S^T that a lane holds are consecutive, so its weights are the A operand
 // of the second product as they are: the tokens of a lane group are 4 of each half tile,
@@ -42,15 +45,16 @@ namespace pa {
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef float f2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLag = 0x1p8f;      // exp2 of what a score may exceed its row's reference by
-constexpr float kTop = 0x1p15f;     // weights stay below (binary16)
-constexpr int kTopBits = 7;         // exponent of a row's largest weight when e is set
-constexpr int kLeast = -160;        // e of a row without weights: any weight that comes leaves its range
+constexpr float kTop = 0x1p40f;     // weights stay below, so that sums of 2^30 codes do not overflow
+constexpr int kTopBits = 24;        // exponent of a row's largest weight when e is set: one of 2^-126 is 2^-102
+constexpr int kLeast = -176;        // e of a row without weights: any weight that comes leaves its range or keeps its bits
 constexpr float kLimit = 0x1p94f;   // of a score's factors: scores stay below 2^126, codes' products being below 2^32
-constexpr float kMost = 0x1p126f;   // of a weight's factor: never infinite, so that 0 stays 0
+constexpr float kMost = 0x1.fffffep127f;  // of a weight's factor: never infinite, so that 0 stays 0
 constexpr float kNone = -0x1p127f;  // reference of a row that has seen nothing
 
 struct Args {
@@ -312,15 +316,12 @@ __device__ __forceinline__ h8 halves<FIBQ_INT8>(uint32_t lo, uint32_t hi) {
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// w less half HALF of x, in one instruction (exact: the half is w rounded)
-template <int HALF>
-__device__ __forceinline__ float rest(h2 x, float w) {
-  float r;
-  if constexpr (HALF == 0)
-    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(x), "v"(w));
-  else
-    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(x), "v"(w));
-  return r;
+// A pair of weights' leading 8 bits as bfloat16, cut off and taken from them (exact).
+__device__ __forceinline__ uint32_t leading(float* x, float* y) {
+  const uint32_t a = __float_as_uint(*x), b = __float_as_uint(*y);
+  *x -= __uint_as_float(a & 0xffff0000u);
+  *y -= __uint_as_float(b & 0xffff0000u);
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
 __device__ __forceinline__ float limited(float x) {
   return __builtin_amdgcn_fmed3f(x, -kLimit, kLimit);
@@ -609,7 +610,7 @@ struct Wave {
       t[1] = half(min(next + 16, to - 1) & ~15);
       load_k(t);
       const bool masked = t0 + 32 > least || lost_page[0] || lost_page[1];
-      h8 hi[R], lo[R];
+      uint4 parts[R][3];  // of weights: pairs of tokens
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float f[2] = {limited(ldexpf(ks[0], qe[r])), limited(ldexpf(ks[1], qe[r]))};
@@ -621,7 +622,10 @@ struct Wave {
             if (t0 + (i / 4) * 16 + group * 4 + i % 4 >= vis[r]) x[i] = -INFINITY;
           }
         };
-        auto weigh = [&]() {  // whether all weights are in their range
+        // Whether all weights are in their range.  (A factor c0 beyond its type belongs to
+        // exponentials of 0, or to weights out of range; behind a move, to exponentials of
+        // less than 2^-75 that weigh most: those take 2^64 of it.)
+        auto weigh = [&](bool moved) {
           float x[8], top_p[2];
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s[r][i / 4][i % 4], f[i / 4], -ref[r]);
@@ -629,20 +633,23 @@ struct Wave {
           more = 0.0f;
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const float c = __builtin_amdgcn_fmed3f(ldexpf(vs[u], -e[r]), -kMost, kMost);
+            const float c0 = ldexpf(vs[u], -e[r]);
+            const int far = moved && !(fabsf(c0) < 0x1p100f) ? 64 : 0;
+            const float c = __builtin_amdgcn_fmed3f(moved ? ldexpf(vs[u], -e[r] - far) : c0, -kMost, kMost);
             top_p[u] = 0.0f;
 #pragma unroll
             for (int i = 4 * u; i < 4 * u + 4; ++i) {
               x[i] = exp2_(x[i]);
               top_p[u] = fmaxf(top_p[u], x[i]);
               more += x[i];
-              w[i] = x[i] * c;
+              w[i] = (moved ? ldexpf(x[i], far) : x[i]) * c;
             }
-            largest = u ? fmaxf(largest, top_p[u] * fabsf(c)) : top_p[u] * fabsf(c);
+            const float most_w = moved ? ldexpf(top_p[u], far) * fabsf(c) : top_p[u] * fabsf(c0);
+            largest = u ? fmaxf(largest, most_w) : most_w;
           }
           return !__any(fmaxf(top_p[0], top_p[1]) > kLag || largest >= kTop);
         };
-        if (!weigh()) {
+        if (!weigh(false)) {
           float x[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -653,16 +660,16 @@ struct Wave {
           if (masked) hide(x);
           move(r, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])), vs[0], vs[1]);
-          weigh();
+          weigh(true);
         }
         sum[r] += more;
         top[r] = fmaxf(top[r], largest);
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          const h2 x = __builtin_convertvector(f2{w[i], w[i + 1]}, h2);
-          const h2 y = __builtin_convertvector(f2{rest<0>(x, w[i]), rest<1>(x, w[i + 1])}, h2);
-          hi[r][i] = x[0], hi[r][i + 1] = x[1];
-          lo[r][i] = y[0], lo[r][i + 1] = y[1];
+        for (int i = 0; i < 3; ++i) {
+          parts[r][i].x = leading(&w[0], &w[1]);
+          parts[r][i].y = leading(&w[2], &w[3]);
+          parts[r][i].z = leading(&w[4], &w[5]);
+          parts[r][i].w = leading(&w[6], &w[7]);
         }
       }
       if (t0 + 32 > most) {  // what lies behind the last token may hold anything
@@ -675,23 +682,14 @@ struct Wave {
 #pragma unroll
       for (int c = 0; c < CB / 4; ++c)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          // columns 4 c + 2 m and the next: pairs of tokens side by side
-          const uint32_t sel = m ? 0x07030602u : 0x05010400u;
-          const uint32_t a = __builtin_amdgcn_perm(v[1][c], v[0][c], sel),
-                         b = __builtin_amdgcn_perm(v[3][c], v[2][c], sel),
-                         d = __builtin_amdgcn_perm(v[5][c], v[4][c], sel),
-                         f = __builtin_amdgcn_perm(v[7][c], v[6][c], sel);
+        for (int n = 0; n < 4; ++n) {
+          const b8 x = column(c, n);
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const h8 x = pairs(a, b, d, f, n);
-            const int at = 4 * c + 2 * m + n;
+          for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-              acc[r][at] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[r], x, acc[r][at], 0, 0, 0);
-              acc[r][at] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[r], x, acc[r][at], 0, 0, 0);
-            }
-          }
+            for (int i = 2; i >= 0; --i)
+              acc[r][4 * c + n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, parts[r][i]), x,
+                                                                          acc[r][4 * c + n], 0, 0, 0);
         }
       load_v(t);
     }
@@ -701,19 +699,24 @@ struct Wave {
       sum[r] += __shfl_xor(sum[r], 32, 64);
     }
   }
-  // 8 tokens' codes of one column: the low or high halves of four words
-  __device__ __forceinline__ h8 pairs(uint32_t a, uint32_t b, uint32_t c, uint32_t d, int n) {
-    h2 x[4];
-    const uint32_t w[4] = {a, b, c, d};
+  // The 8 tokens' codes of column 4 c + n of the lane's.
+  __device__ __forceinline__ b8 column(int c, int n) const {
+    uint4 x;
+    uint32_t* w = (uint32_t*)&x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (CODES == FIBQ_E4M3)
-        x[i] = n ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, true)
-                 : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, false);
-      else
-        x[i] = biased(w[i] ^ 0x80808080u, n ? 0x04030402u : 0x04010400u);
+    for (int i = 0; i < 8; i += 2) {
+      if constexpr (CODES == FIBQ_E4M3) {
+        // columns 4 c + 2 m and the next: pairs of tokens side by side
+        const uint32_t two = __builtin_amdgcn_perm(v[i + 1][c], v[i][c], n & 2 ? 0x07030602u : 0x05010400u);
+        const b2 y = n & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(two, 1.0f, true)
+                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(two, 1.0f, false);
+        w[i / 2] = __builtin_bit_cast(uint32_t, y);
+      } else {
+        const float lo = (float)(int8_t)(v[i][c] >> (8 * n)), hi = (float)(int8_t)(v[i + 1][c] >> (8 * n));
+        w[i / 2] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+      }
     }
-    return h8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+    return __builtin_bit_cast(b8, x);
   }
 
   // The results of an item that one wavefront has whole.

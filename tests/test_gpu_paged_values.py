@@ -44,3 +44,41 @@ def test_pages_of_zeros_first(device, kind, lens, rows, H, G, page, d, exponent)
     q = torch.randn(len(lens) if rows is None else sum(rows), H * G, d, device=device) * 0.1
     out, starts = attend(device, q, cache, lens, rows, kind)
     check_attention(out, host(q), *cache, lens, starts, True, kind)
+
+
+@pytest.mark.parametrize("kind", list(CODES))
+@pytest.mark.parametrize("lens,rows,H,G,page,d", FORMS + [([20, 2, 32, 33], None, 1, 2, 16, 64)], ids=str)
+@pytest.mark.parametrize("bits", [10, 20, 40, 100])
+def test_token_of_much_weight_and_no_value(device, kind, lens, rows, H, G, page, d, bits):
+    """The first token's score is `bits` bits above all others and its values are 0: the
+    others keep their bits."""
+    rng = np.random.default_rng(d + bits)
+    cache = kp, ks, vp, vs, table = make_cache(rng, lens, H, page, d, kind)
+    big = opg.to_codes(np.array([96.0]), kind)[0]
+    for g in range(len(lens)):
+        first = table[g, 0]
+        kp[first, :, 0], vp[first, :, 0] = 0, 0
+        kp[first, :, 0, 0] = big
+        for j in range(-(-lens[g] // page)):
+            ks[table[g, j]] = 1.0
+            kp[table[g, j], :, (1 if j == 0 else 0):, 0] = 0
+    q = torch.randn(len(lens) if rows is None else sum(rows), H * G, d, device=device) * 1e-5
+    q[:, :, 0] = bits * float(np.log(2)) / 96
+    out, starts = attend(device, q, cache, lens, rows, kind, scale=1.0)
+    check_attention(out, host(q), *cache, lens, starts, True, kind, 1.0)
+
+
+@pytest.mark.parametrize("rows", [None, [40]])
+def test_values_of_the_least_weight(device, rows):
+    """Values so large, with a weight so small, that they count for as much as the others."""
+    rng = np.random.default_rng(3)
+    cache = kp, ks, vp, vs, table = make_cache(rng, [128], 1, 16, 64, "int8")
+    kp[:], ks[:] = 0, 1.0
+    kp[table[0, :8], 0, :, 0] = np.array([100, 0, 50, 0, 100, 50, 100, 100], np.uint8)[:, None]
+    for bits in (60, 90, 110, 118):
+        # weights 1, 2^-bits, 2^-bits/2; values 2^-60 on the heavy ones
+        vs[table[0, :8], 0] = np.exp2([-60.0, bits - 60, bits / 2 - 60, -60, -60, -90, -90, -60])
+        q = torch.zeros(1 if rows is None else 40, 2, 64, device=device)
+        q[..., 0] = bits * float(np.log(2)) / 100
+        out, starts = attend(device, q, cache, [128], rows, "int8", causal=False, scale=1.0)
+        check_attention(out, host(q), *cache, [128], starts, False, "int8", 1.0)
