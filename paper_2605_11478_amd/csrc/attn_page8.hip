@@ -55,6 +55,7 @@ constexpr int kTopBits = 24;        // exponent of a row's largest weight when e
 constexpr int kLeast = -176;        // e of a row without weights: any weight that comes leaves its range or keeps its bits
 constexpr float kLimit = 0x1p94f;   // of a score's factors: scores stay below 2^126, codes' products being below 2^32
 constexpr float kMost = 0x1.fffffep127f;  // of a weight's factor: never infinite, so that 0 stays 0
+constexpr float kFine = 0x1p22f;    // of references: the exact product less one is what the rounded score is less it, to 2^-2
 constexpr float kNone = -0x1p127f;  // reference of a row that has seen nothing
 
 struct Args {
@@ -345,6 +346,7 @@ struct Wave {
   int e[R];
   f4 acc[R][CB];
   bool lost[R];  // queries that are no numbers
+  float base[R];  // the reference, or kNone from kFine on: each tile's weights leave their range then
 
   uint4 k[2][KJ];
   uint32_t v[8][CB / 4];
@@ -535,6 +537,7 @@ struct Wave {
       top[s] = 0.0f;
       e[s] = kLeast;
       lost[s] = false;
+      base[s] = kNone;
 #pragma unroll
       for (int c = 0; c < CB; ++c) acc[s][c] = f4{0, 0, 0, 0};
     }
@@ -561,6 +564,7 @@ struct Wave {
     sum[r] *= a;
     top[r] = ldexpf(w, -ew);
     ref[r] = to;
+    base[r] = fabsf(to) < kFine ? to : kNone;
     e[r] = ew;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -570,6 +574,15 @@ struct Wave {
     }
   }
 
+  // A score in units of a row's reference, rounded by itself: a row whose scores lie far
+  // from 0 has to take off its reference from what that was taken from.  (Behind the branch
+  // that needs it.)
+  __device__ __forceinline__ float score(float s, float f) const {
+    asm volatile("" : "+v"(s));
+    float x = s * f;
+    asm volatile("" : "+v"(x));
+    return x;
+  }
   // Tokens [from, to) of the item, from a multiple of 32.
   __device__ __forceinline__ void run(const Part& r_, int from, int to) {
     const int last = (to - 1) & ~31;
@@ -628,23 +641,31 @@ struct Wave {
         auto weigh = [&](bool moved) {
           float x[8], top_p[2];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(s[r][i / 4][i % 4], f[i / 4], -ref[r]);
+          for (int i = 0; i < 8; ++i)
+            x[i] = __builtin_fmaf(s[r][i / 4][i % 4], f[i / 4], moved ? -ref[r] : -base[r]);
+          if (moved && __any(base[r] != ref[r])) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float y = score(s[r][i / 4][i % 4], f[i / 4]) - ref[r];
+              x[i] = base[r] != ref[r] ? y : x[i];
+            }
+          }
           if (masked) hide(x);
           more = 0.0f;
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const float c0 = ldexpf(vs[u], -e[r]);
-            const int far = moved && !(fabsf(c0) < 0x1p100f) ? 64 : 0;
-            const float c = __builtin_amdgcn_fmed3f(moved ? ldexpf(vs[u], -e[r] - far) : c0, -kMost, kMost);
+            const int up = moved && !(fabsf(c0) < 0x1p100f) ? 64 : 0;
+            const float c = __builtin_amdgcn_fmed3f(moved ? ldexpf(vs[u], -e[r] - up) : c0, -kMost, kMost);
             top_p[u] = 0.0f;
 #pragma unroll
             for (int i = 4 * u; i < 4 * u + 4; ++i) {
               x[i] = exp2_(x[i]);
               top_p[u] = fmaxf(top_p[u], x[i]);
               more += x[i];
-              w[i] = (moved ? ldexpf(x[i], far) : x[i]) * c;
+              w[i] = (moved ? ldexpf(x[i], up) : x[i]) * c;
             }
-            const float most_w = moved ? ldexpf(top_p[u], far) * fabsf(c) : top_p[u] * fabsf(c0);
+            const float most_w = moved ? ldexpf(top_p[u], up) * fabsf(c) : top_p[u] * fabsf(c0);
             largest = u ? fmaxf(largest, most_w) : most_w;
           }
           return !__any(fmaxf(top_p[0], top_p[1]) > kLag || largest >= kTop);
@@ -652,11 +673,7 @@ struct Wave {
         if (!weigh(false)) {
           float x[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[i] = s[r][i / 4][i % 4];
-            asm volatile("" : "+v"(x[i]));  // (nothing of this before the branch)
-            x[i] *= f[i / 4];
-          }
+          for (int i = 0; i < 8; ++i) x[i] = score(s[r][i / 4][i % 4], f[i / 4]);
           if (masked) hide(x);
           move(r, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])), vs[0], vs[1]);

@@ -82,3 +82,34 @@ def test_values_of_the_least_weight(device, rows):
         q[..., 0] = bits * float(np.log(2)) / 100
         out, starts = attend(device, q, cache, [128], rows, "int8", causal=False, scale=1.0)
         check_attention(out, host(q), *cache, [128], starts, False, "int8", 1.0)
+
+
+@pytest.mark.parametrize("kind", list(CODES))
+@pytest.mark.parametrize("lens,rows,H,G,page,d", FORMS, ids=str)
+@pytest.mark.parametrize("size", [1e4, 1e6, 1e8, 1e10, 1e20, 1e30, 2e37])
+def test_scores_of_any_size(device, kind, lens, rows, H, G, page, d, size):
+    """Rows stay within the values that they see; where one token's score is above all others
+    by more than rounding and 40 nats, they are that token's."""
+    rng = np.random.default_rng(d)
+    cache = kp, ks, vp, vs, table = make_cache(rng, lens, H, page, d, kind)
+    vp &= np.uint8(0x7f)  # (values from 0 up)
+    q = torch.randn(len(lens) if rows is None else sum(rows), H * G, d, device=device) * size
+    q.clamp_(-3e38, 3e38)
+    out, starts = attend(device, q, cache, lens, rows, kind)
+    assert np.isfinite(out).all()
+    x, alone = host(q), 0
+    for g, L in enumerate(lens):
+        M = starts[g + 1] - starts[g]
+        seen = np.tri(M, L, L - M, dtype=bool)
+        for h in range(H):
+            K, V = (opg.rows_of(a, b, table[g], L, h, kind) for a, b in ((kp, ks), (vp, vs)))
+            for j in range(G):
+                y, o = x[starts[g]:starts[g + 1], h * G + j], out[starts[g]:starts[g + 1], h * G + j]
+                s = np.where(seen, y @ K.T / np.sqrt(d), -np.inf)
+                off = (np.abs(y) @ np.abs(K).T).max(1) / np.sqrt(d) * ((d + 8) * 2.0 ** -24 + 2.0 ** -21)
+                for i in range(M):
+                    near = s[i] >= (s[i].max() - 2 * off[i] - 40 if size < 1e32 else -1e300)  # (factors are limited)
+                    room = 2.0 ** -18 * V[seen[i]].max(0)
+                    assert (o[i] >= V[near].min(0) - room).all() and (o[i] <= V[near].max(0) + room).all(), (g, h, j, i)
+                    alone += near.sum() == 1
+    assert alone > 0 or size < 1e6 or size > 1e32
