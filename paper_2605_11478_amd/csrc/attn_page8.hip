@@ -689,10 +689,11 @@ struct Wave {
           parts[r][i].w = leading(&w[6], &w[7]);
         }
       }
-      if (t0 + 32 > most) {  // what lies behind the last token may hold anything
+      // What lies behind the last token, or is read in an unknown page's place, may hold anything.
+      if (t0 + 32 > most || lost_page[0] || lost_page[1]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (t0 + (i / 4) * 16 + group * 4 + i % 4 >= most)
+          if (lost_page[i / 4] || t0 + (i / 4) * 16 + group * 4 + i % 4 >= most)
 #pragma unroll
             for (int c = 0; c < CB / 4; ++c) v[i][c] = 0;
       }

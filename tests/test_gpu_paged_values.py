@@ -113,3 +113,26 @@ def test_scores_of_any_size(device, kind, lens, rows, H, G, page, d, size):
                     assert (o[i] >= V[near].min(0) - room).all() and (o[i] <= V[near].max(0) + room).all(), (g, h, j, i)
                     alone += near.sum() == 1
     assert alone > 0 or size < 1e6 or size > 1e32
+
+
+@pytest.mark.parametrize("kind", list(CODES))
+@pytest.mark.parametrize("rows", [40, 17])
+@pytest.mark.parametrize("page,d", [(16, 64), (32, 128), (16, 256)])
+@pytest.mark.parametrize("unknown", [-1, 10 ** 6])
+def test_unknown_page_beside_no_numbers(device, kind, rows, page, d, unknown):
+    """The pool's first page belongs to no sequence and holds codes that are no numbers: rows
+    that do not see an unknown page do not see that one either."""
+    rng = np.random.default_rng(5)
+    L = 4 * page
+    kp, ks, vp, vs, table = make_cache(rng, [L], 1, page, d, kind)
+    first = lambda a, x: np.concatenate([np.full_like(a[:1], x), a])
+    kp, vp, ks, vs = first(kp, 0x7f), first(vp, 0x7f), first(ks, 1), first(vs, 1)
+    vp[0, :, ::2] = 0xff
+    table += 1
+    table[0, 3] = unknown
+    n = min(rows, L)
+    q = torch.randn(n, 2, d, device=device)
+    out, starts = attend(device, q, (kp, ks, vp, vs, table), [L], [n], kind)
+    blind = max(0, n - page)  # rows that see tokens before the unknown page only
+    assert np.isnan(out[blind:]).all()
+    check_attention(out[:blind], host(q)[:blind], kp, ks, vp, vs, table, [L - page], [0, blind], True, kind)
