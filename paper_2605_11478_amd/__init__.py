@@ -11,6 +11,7 @@ Tensors passed to device functions must be CUDA (HIP) tensors, contiguous,
 on the current device; work is enqueued on torch's current stream.
 """
 import ctypes
+import functools
 import math
 import os
 
@@ -841,6 +842,39 @@ def _apart_from_itself(t, name):
         raise ValueError(f"{name} holds an element twice")
 
 
+@functools.lru_cache(maxsize=None)
+def _rope_function():
+    torch = _torch()
+
+    class Rope(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, positions, freqs, layout, scale, inverse):
+            ctx.save_for_backward(positions, freqs)
+            ctx.how = (layout, scale)
+            ctx.inverse = bool(inverse)
+            ctx.set_materialize_grads(False)
+            out = rope(q, k, positions, freqs, layout, scale, inverse)
+            ctx.mark_non_differentiable(*(y for y, x in zip(out, (q, k)) if x is not None and not x.requires_grad))
+            return out
+
+        @staticmethod
+        def backward(ctx, *grads):
+            positions, freqs = ctx.saved_tensors
+            at = [i for i in range(2) if grads[i] is not None and ctx.needs_input_grad[i]]
+            if not at:
+                return (None,) * 7
+            g = [grads[i] if grads[i].stride(2) == 1
+                 else grads[i].clone(memory_format=torch.contiguous_format) for i in at]
+            turned = rope(g[0], g[1] if len(g) > 1 else None, positions, freqs, *ctx.how,
+                          inverse=not ctx.inverse)
+            to = [None] * 7
+            for i, x in zip(at, turned):
+                to[i] = x
+            return tuple(to)
+
+    return Rope
+
+
 def rope(q, k, positions, freqs, layout="half", scale=1.0, inverse=False, out=None):
     """Rotary positions of queries and keys in one call.
 
@@ -851,6 +885,10 @@ def rope(q, k, positions, freqs, layout="half", scale=1.0, inverse=False, out=No
     i + rot / 2, "interleaved" 2 i and 2 i + 1.  ``scale`` multiplies the turned
     elements; ``inverse`` turns back, which with the same scale is the gradient.
     -> (q, k) turned, new and dense, or in ``out``, a pair; out=(q, k) works in place.
+
+    Where q or k requires a gradient (and torch records one), the results carry it;
+    positions and freqs must then stay as they are until the backward pass has run, and
+    ``out`` is refused, as is a freqs that requires a gradient.
     """
     fast = _compiled(q)
     if fast is not None:
@@ -861,6 +899,14 @@ def rope(q, k, positions, freqs, layout="half", scale=1.0, inverse=False, out=No
             return done
     torch = _torch()
     types = (torch.float32, torch.float16, torch.bfloat16)
+    if torch.is_grad_enabled():
+        records = lambda x: getattr(x, "requires_grad", False)
+        if records(freqs):
+            raise ValueError("freqs must not require a gradient: none is computed")
+        if out is not None and any(map(records, (q, k, *out))):
+            raise ValueError("out takes no part in gradients: call without it, or under torch.no_grad()")
+        if records(q) or records(k):
+            return _rope_function().apply(q, k, positions, freqs, layout, scale, inverse)
     if layout not in ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(ROPE_LAYOUTS)}")
     _head_rows(q, "q", types, (None, None, None))

@@ -14,6 +14,7 @@
 #include <torch/csrc/utils/python_arg_parser.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 
 #include <cmath>
 #include <cstdint>
@@ -555,7 +556,8 @@ bool meets(const HeadRows& a, const Tensor* t) {
 }
 
 // rope(q, k, positions, freqs, layout, scale, inverse, out, stream, device) -> (q, k);
-// out: None or (q, k) themselves
+// out: None or (q, k) themselves.  Calls that torch would record a gradient of are left
+// to the Python code.
 PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (!g_rope || n_args != 10) FIBQ_NONE;
@@ -566,6 +568,8 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (!q || (has_k && !k) || !at_ || !freqs || !PyFloat_CheckExact(a[5]) || !PyBool_Check(a[6]) ||
       !PyBool_Check(a[4]) || !int_arg(a[8], &st) || !int_arg(a[9], &index) ||
       q->device().index() != index || freqs->dim() != 1)
+    FIBQ_NONE;
+  if (c10::GradMode::is_enabled() && (q->requires_grad() || (has_k && k->requires_grad()) || freqs->requires_grad()))
     FIBQ_NONE;
   const at::Device dev = q->device();
   const int dt = dtype_code(*q);
