@@ -397,10 +397,11 @@ __device__ __forceinline__ float least_scale(uint32_t amax_bits, int codes) {
 }
 
 // x / s rounded to float: the remainder of x r corrects it once, r = 1 / s rounded
-// (Markstein's theorem; x r itself is exact where s is a power of two).
+// (Markstein's theorem; x r itself is exact where s is a power of two).  s may be
+// any scale that a page had: of zeros below 2^-128 too, and infinite, where all is 0.
 struct Quotient {
   float s, r;
-  __device__ __forceinline__ explicit Quotient(float s_) : s(s_), r(1.0f / s_) {}
+  __device__ __forceinline__ explicit Quotient(float s_) : s(fminf(s_, 0x1.fffffep127f)), r(fminf(1.0f / s_, 0x1p127f)) {}
   __device__ __forceinline__ float operator()(float x) const {
     const float q = x * r;
     return copysignf(__builtin_fmaf(__builtin_fmaf(-q, s, x), r, q), q);  // (of -0 as well)
