@@ -34,15 +34,17 @@ __device__ __forceinline__ void store(T* p, const Vec<T, V>& v) {
 }
 
 // ------------------------------------------------------------------- rope --
-// Pair i of a row at position p turns by p f_i.  The angle is reduced in
-// double (p f_i / 2 pi to quarter turns, exact from there on), so that a far
-// position loses nothing; sine and cosine of the remaining eighth of a turn are
-// computed in float.  A workgroup computes the angles of its rows once, into
+// Pair i of a row at position p turns by p f_i.  The angle is reduced in double, with
+// what the roundings of 2 / pi and of its product with f_i leave and with an exact product
+// by p, so that the farthest position loses nothing; sine and cosine of the remaining eighth of a
+// turn are computed in float.  A workgroup computes the angles of its rows once, into
 // LDS, and applies them to all their heads.  Bound by memory: 16384 rows x 40 heads,
 // d = 128, 336 MB, 67 to 71 us (4.7 to 5.0 TB/s; a large copy moves 4.9), 105 before a
 // row's angles stayed in registers.  64 rows x 36 heads: 6.2 us, the call.
 constexpr int kRopeThreads = 256;
 constexpr int kRopeAngles = 1024;  // angles of a workgroup, at most
+// 2 / pi, quarter turns of a radian: a double and what it leaves
+constexpr double kQuarters = 0x1.45f306dc9c883p-1, kQuartersRest = -0x1.6b01ec5417056p-55;
 
 template <typename T, int V, int VT, bool HALF>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
@@ -52,11 +54,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(Rope a, int tile) {
   const int rows = (int)min((int64_t)tile, a.n_rows - row0);
   for (int i = tid; i < rows * half; i += kRopeThreads) {
     const int r = i / half;
-    const double quarters =
-        (double)a.positions[row0 + r] * (a.freqs[i - r * half] * 0.63661977236758134308);
-    const double n = rint(quarters);
+    const double at = (double)a.positions[row0 + r], f = a.freqs[i - r * half];
+    const double unit = f * kQuarters, rest = fma(f, kQuarters, -unit) + f * kQuartersRest;
+    const double n = rint(at * unit);
     float s, c;
-    sincospif((float)(quarters - n) * 0.5f, &s, &c);
+    sincospif((float)(fma(at, unit, -n) + at * rest) * 0.5f, &s, &c);
     const int turns = (int)(n - 4.0 * floor(n * 0.25));
     float cs = turns & 1 ? -s : c, sn = turns & 1 ? c : s;
     if (turns & 2) cs = -cs, sn = -sn;
