@@ -445,7 +445,10 @@ size_t fibq_page_resize_workspace_bytes(int64_t n_seqs);
  *   *new_free = the pages that are left.
  * A slot is a row of a cache of n_pages * page rows; fibq_decode takes slots as
  * token_ids.  new_lens may be lens, and new_free n_free; outputs overlap nothing
- * otherwise.  lens, grow, table and free_pages are not written by others while
+ * otherwise.  A refused request still holds lens[g] tokens and their pages: only
+ * lens says so, so where requests may be refused new_lens is another tensor, and
+ * lens takes the entries that are not -1 (in place the length is lost, and the
+ * request's pages with it).  lens, grow, table and free_pages are not written by others while
  * the call runs.  1 <= page <= 65536 here; free_cap < 2^30, n_rows < 2^31. */
 int fibq_page_resize(int32_t* table, const int32_t* lens, const int32_t* grow, int64_t n_seqs,
                      int64_t max_pages, int page, int64_t n_pages, int32_t* free_pages,

@@ -971,7 +971,9 @@ def page_resize(table, lens, grow, page, n_pages, free, n_free, n_rows, out=None
     one behind the other, has slot page id * page + offset and its position; a request
     that cannot be served has new length -1, and its rows and those behind the last
     slot and position -1.  In ``out``, new_lens may be ``lens`` and new_free ``n_free``;
-    nothing else may share memory.  ``slots`` are rows of a flat cache as well
+    nothing else may share memory.  A refused request still holds lens[g] tokens and
+    their pages, and only ``lens`` says so: where requests may be refused, give new_lens
+    a tensor of its own and go on with ``torch.where(new_lens < 0, lens, new_lens)``.  ``slots`` are rows of a flat cache as well
     (``token_ids`` of ``decode``).
     """
     fast = _compiled(lens)
