@@ -380,9 +380,9 @@ int fibq_evict(const uint8_t* k_payload, const uint16_t* k_norms, const uint8_t*
                void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------- paged 8-bit cache --
- * Keys and values in 8 bits with one scale per page and head, for layers or
- * tokens that are not coded, with the block tables, the rotary positions and
- * the attention of a serving loop.  A page holds `page` tokens of one sequence;
+ * Keys and values in 8 bits with one scale per page and head, for layers that
+ * are not coded, with the block tables, the rotary positions and the attention
+ * of a serving loop.  A page holds `page` tokens of one sequence;
  * sequence g's token t is row t % page of page table[g][t / page].
  * k_pages, v_pages: device [n_pages][H][page][d] bytes, 16-byte aligned, of
  * codes FIBQ_INT8 (-127 .. 127) or FIBQ_E4M3 (1-4-3 floating point, largest 448,

@@ -25,12 +25,14 @@
 // second launch joins.
 //
 // What bounds it.  Single tokens over long sequences: memory (48 sequences to 32768 tokens
-// x 4 heads, 425 MB: 92 us, 4.6 TB/s; one of 131072 x 8 heads, d = 128, 269 MB: 56 us, 4.8
+// x 4 heads, 425 MB: 94 us, 4.5 TB/s; one of 131072 x 8 heads, d = 128, 269 MB: 56 us, 4.8
 // TB/s; a large copy moves 4.9).  Row tiles: vector and matrix instructions (8 chunks to
-// 512 tokens over up to 4096, 67 GFLOP: 148 us; vector instructions, matrix ones among them,
-// are issued in 55 % of the SIMDs' cycles).  Few short items: the chain of launch,
-// lengths, table, pages and the wait for each next tile (64 sequences to 2048 tokens: 12
-// us for 35 MB).
+// 512 tokens over up to 4096, 67 GFLOP: 170 us; vector instructions, matrix ones among them,
+// are issued in 57 % of the SIMDs' cycles, the matrix units are busy in 31 %).  Few short
+// items: the chain of launch, lengths, table, pages and the wait for each next tile (64
+// sequences to 2048 tokens: 13 us for 35 MB).  Two binary16 parts of a weight took
+// 92, 55, 147 and 12 us there; choosing between both forms tile by tile 94, 57, 193 and 15
+// (registers).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -243,8 +245,8 @@ __device__ __forceinline__ int* plan_of(const Args& p) {
 
 // The parts before every sequence, once for all workgroups where each would take longer to
 // sum them up itself: above 512 sequences (tables of 16384 tokens; 64 sequences to 2048
-// tokens 16.9 us without and 19.4 with this launch, 512 to 1000 42.6 and 44.7, 2048 to 500
-// 91.8 and 51.7).
+// tokens 17.9 us without and 20.3 with this launch, 512 to 1000 44.7 and 45.0, 2048 to 500
+// 78.6 and 56.1).
 constexpr int kPlanned = 512;
 __global__ __launch_bounds__(1024) void plan_kernel(Args p) {
   __shared__ float tokens_of[16];
@@ -920,7 +922,7 @@ void main_kernel(Args p) {
 // Joins the states of the items that were cut: a wavefront for each row or, where items
 // have few rows and many parts, four (WIDE).  What it reads has just been written by
 // other XCDs, so each read takes long: many are on their way at once.  Bound by that chain
-// (list, headers, values) and its launch: 6.7 us for 192 items to 32768 tokens, 4.8 for 8 of
+// (list, headers, values) and its launch: 7.0 us for 192 items to 32768 tokens, 4.8 for 8 of
 // 131072, d = 128.
 template <int D, int WIDE>
 __global__ __launch_bounds__(256) void merge_kernel(Args p) {
@@ -1022,34 +1024,34 @@ struct Plan {
 Plan plan(int64_t n_seqs, int64_t n_rows, bool one, int H, int G, int64_t max_pages, int page, int d) {
   Plan p{};
   // Tiles of 32 rows where a sequence has more than 16 (64 sequences of 2048 tokens x 4
-  // heads, d = 64; rows of a head, then with 16-row and with 32-row tiles: 16 17.2 and
-  // 23.3, 24 26.3 and 24.1, 32 26.6 and 24.9, 64 34.5 and 32.0; d = 128: 30.5 and 32.6,
-  // 37.8 and 33.3, 38.3 and 34.1, 61.0 and 44.1).
+  // heads, d = 64; rows of a head, then with 16-row and with 32-row tiles: 16 17.6 and
+  // 25.5, 24 26.8 and 26.2, 32 27.0 and 27.1, 64 39.1 and 35.8; d = 128: 30.5 and 34.0,
+  // 45.8 and 35.5, 46.5 and 36.3, 62.6 and 53.7).
   p.R = n_rows * G >= 24 * std::max<int64_t>(1, n_seqs) ? 2 : 1;
   const int64_t room = max_pages * page, tile = 16 * p.R / G;
   p.rows = one ? G : (int)tile * G;
   const int64_t items = (one ? n_rows : n_rows / tile + std::min(n_seqs, n_rows)) * H;
   // Items are cut only where they may be long or are few, since cutting costs a sum over
   // the lengths in every workgroup and a launch (whole and cut: 4 items to 2048 tokens
-  // 11.6 and 13.2, to 4096 17.6 and 13.5; 64 to 2048 12.2 and 14.8, to 4096 18.4 and 16.1;
-  // 256 to 4096 19.0 and 27.7, to 8192 37.3 and 43.3, to 16384 70.3 and 73.5).
+  // 12.5 and 13.5, to 4096 19.8 and 13.6; 64 to 2048 13.2 and 15.1, to 4096 20.6 and 16.3;
+  // 256 to 4096 20.9 and 28.9, to 8192 38.7 and 43.7, to 16384 73.3 and 75.8).
   p.cut = room > (items >= kCu ? 8192 : 2048);
   // wavefronts that a compute unit holds at once
   const int64_t held = 4 * waves_of_simd(p.R, d);
   // Workgroups for each compute unit: all parts run at once, and each compute unit has as
   // many.  An item's last part is half empty on the average, so half as many parts as
   // items are kept back, and k grows with the items to keep that small (192 items to
-  // 32768 tokens, 1, 2 and 3 for a compute unit: 141, 94 and 94; 8 items of 131072, d = 128: 57.6, 58.9 and 61.0.)
+  // 32768 tokens, 1, 2 and 3 for a compute unit: 146, 96 and 97; 8 items of 131072, d = 128: 56.6, 60.1 and 61.8.)
   int64_t k = std::min<int64_t>(4, (items + kCu / 2 - 1) / (kCu / 2));
   int64_t target = k * kCu - items / 2;
   if (target < kCu / 2) target = kCu;  // (items enough: only those far above the average are cut)
   if (p.R == 2) target = kCu * held / 4;
   // Wavefronts: as many to a workgroup as keep a compute unit's places filled by its
-  // items (64 sequences to 2048 tokens x 4 heads, 4, 8 and 16: 15.7, 13.5 and 14.2; 8
-  // items of 131072 tokens, d = 128, 2, 4 and 8: 69.3, 56.1 and 57.1); one for row tiles
-  // that fill the card by themselves, whose states then need no joining (4 prompts of 1000
-  // tokens x 4 heads, 1, 2 and 4: 72.9, 77.6 and 90.1; 8 chunks to 512 tokens over up to
-  // 4096, d = 128: 161, 173 and 149).
+  // items (64 sequences to 2048 tokens x 4 heads, 2, 4 and 8: 26.3, 15.5 and 13.7; 8
+  // items of 131072 tokens, d = 128, 2 and 4: 71.6 and 56.6); one for row tiles that fill
+  // the card by themselves, whose states then need no joining (4 prompts of 1000 tokens x 4
+  // heads, 1, 2 and 4: 82.5, 84.8 and 96.7; 8 chunks to 512 tokens over up to 4096, d = 128:
+  // 191, 200 and 170; cross attention of 48 rows over 1500 tokens: 58, 38 and 23).
   p.waves = most_waves(p.R, d);
   if (p.R == 1)
     while (p.waves > 2 && (p.cut ? k : (items + kCu - 1) / kCu) * p.waves > held) p.waves /= 2;
